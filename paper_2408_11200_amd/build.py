@@ -26,18 +26,24 @@ def bench_sources():
     return sorted(glob.glob(os.path.join(HERE, "csrc_bench", "*.hip")))
 
 
-def autograd_command(out):
-    """Host compiler command of the autograd nodes; libkan_hip.so has to be there."""
+def autograd_sources():
+    return sorted(glob.glob(os.path.join(HERE, "csrc_torch", "*.cpp")))
+
+
+def autograd_commands(out, objs):
+    """Host compiler commands of the autograd nodes: one for each source (to its object file), and the link; libkan_hip.so has to be there."""
     import sysconfig
     from torch.utils import cpp_extension
     torch_lib = os.path.join(os.path.dirname(os.path.abspath(cpp_extension.torch.__file__)), "lib")
     include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/opt/rocm/include", os.path.join(ROOT, "include")]
-    return (["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-             "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(cpp_extension.torch._C._GLIBCXX_USE_CXX11_ABI),
-             '-DKAN_TORCH_VERSION="%s"' % cpp_extension.torch.__version__] +
-            [a for d in include for a in ("-isystem", d)] +
-            [os.path.join(HERE, "csrc_torch", "kan_autograd.cpp"), "-o", out, "-L", torch_lib, "-ltorch", "-ltorch_cpu", "-ltorch_python",
-             "-lc10", "-lc10_hip", "-L", HERE, "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN"])
+    flags = (["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+              "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(cpp_extension.torch._C._GLIBCXX_USE_CXX11_ABI),
+              '-DKAN_TORCH_VERSION="%s"' % cpp_extension.torch.__version__] +
+             [a for d in include for a in ("-isystem", d)])
+    link = (["g++", "-shared"] + objs +
+            ["-o", out, "-L", torch_lib, "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_hip", "-L", HERE,
+             "-l:" + os.path.basename(LIB_PATH), "-Wl,-rpath,$ORIGIN"])
+    return [flags + ["-c", src, "-o", obj] for src, obj in zip(autograd_sources(), objs)], link
 
 
 def build(verbose=False, jobs=None):
@@ -63,9 +69,12 @@ def build(verbose=False, jobs=None):
     with tempfile.TemporaryDirectory(prefix="kan_build_") as tmp:
         objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in sources()]
         bench_objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in bench_sources()]
+        node_objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in autograd_sources()]
+        compile_nodes, link_nodes = autograd_commands(AUTOGRAD_PATH, node_objs)
         with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as pool:
-            results = list(pool.map(lambda so: run([hipcc] + flags + inc + ["-c", so[0], "-o", so[1]]),
-                                    zip(sources() + bench_sources(), objs + bench_objs)))
+            # the autograd nodes take the longest: first
+            results = list(pool.map(run, compile_nodes + [[hipcc] + flags + inc + ["-c", src, "-o", obj]
+                                                          for src, obj in zip(sources() + bench_sources(), objs + bench_objs)]))
         failed = [out for rc, out in results if rc != 0]
         log += [out for rc, out in results if out]
         link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"]
@@ -80,7 +89,7 @@ def build(verbose=False, jobs=None):
             if rc != 0:
                 failed.append(out)
         if not failed:
-            rc, out = run(autograd_command(AUTOGRAD_PATH))
+            rc, out = run(link_nodes)
             if rc != 0:
                 failed.append(out)
                 log.append(out)

@@ -44,6 +44,18 @@ class UkanLayerSpec:
 
 
 @dataclass
+class BlockNormSpec:
+    """One boundary between blocks of a residual network (include/kan_net.h): channels, "rms" or "layer" norm, eps, scale of the residual,
+    rows that share a row of the gate (0: all), and the type of h where no branch says it ("f32" or "bf16")."""
+    n: int
+    norm: str = "rms"
+    eps: float = 1e-5
+    residual_scale: float = 1.0
+    gate_rows: int = 0
+    branch: str = "f32"
+
+
+@dataclass
 class Workload:
     name: str
     B: int
