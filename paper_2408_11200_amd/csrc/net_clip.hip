@@ -67,7 +67,7 @@ __device__ __forceinline__ double chunk_squares(const T *p, int64_t count)
     double t = 0.0;
     for (int64_t i = threadIdx.x * 8; i < count; i += kThreads * 8) {
         float v[8];
-        load_some(p + i, (int)(count - i < 8 ? count - i : 8), v);
+        load_at(p, i, count, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) t += (double)v[k] * (double)v[k];
     }
@@ -104,11 +104,10 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *to, int64_t count, fl
 {
     for (int64_t i = threadIdx.x * 8; i < count; i += kThreads * 8) {
         float v[8];
-        const int cols = (int)(count - i < 8 ? count - i : 8);
-        load_some(p + i, cols, v);
+        load_at(p, i, count, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= factor;
-        store_some(to + i, cols, v);
+        store_at(to, i, count, v);
     }
 }
 

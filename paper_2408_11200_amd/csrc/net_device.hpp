@@ -27,7 +27,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));     // rows of odd length start at any element: the wide accesses of global memory need
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));     // no more than the element's alignment
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -41,30 +40,124 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)       // rounde
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16 *p, float v) { p->bits = (uint16_t)two_bf16(v, v); }
 
-// eight consecutive elements
+// Eight consecutive elements as they lie in memory: what a thread holds of a row it will need later.
+template <class T>
+struct Raw;
+template <>
+struct Raw<float> { u32x4 a, b; };
+template <>
+struct Raw<bf16> { u32x4 a; };
+
 template <bool NT = false>
-__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+__device__ __forceinline__ Raw<float> raw8(const float *p)
 {
     const u32x4_a4 *q = (const u32x4_a4 *)p;
-    const u32x4 a = NT ? __builtin_nontemporal_load(q) : q[0], b = NT ? __builtin_nontemporal_load(q + 1) : q[1];
+    if constexpr (NT) return Raw<float>{__builtin_nontemporal_load(q), __builtin_nontemporal_load(q + 1)};
+    else return Raw<float>{q[0], q[1]};
+}
+
+template <bool NT = false>
+__device__ __forceinline__ Raw<bf16> raw8(const bf16 *p)
+{
+    const u32x4_a2 *q = (const u32x4_a2 *)p;
+    if constexpr (NT) return Raw<bf16>{__builtin_nontemporal_load(q)};
+    else return Raw<bf16>{q[0]};
+}
+
+__device__ __forceinline__ Raw<float> no_raw(const float *) { return Raw<float>{u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}}; }
+__device__ __forceinline__ Raw<bf16> no_raw(const bf16 *) { return Raw<bf16>{u32x4{0u, 0u, 0u, 0u}}; }
+
+// fewer than eight, one by one: only where a whole row is that short
+__device__ __forceinline__ Raw<float> raw_few(const float *p, int count)
+{
+    Raw<float> r = no_raw(p);
+    const uint32_t *q = (const uint32_t *)p;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t lo = a[k], hi = b[k];      // a bit cast of the vector's element itself takes element 0 (hipcc 7.2)
+        if (k < count) r.a[k] = q[k];
+        if (4 + k < count) r.b[k] = q[4 + k];
+    }
+    return r;
+}
+
+__device__ __forceinline__ Raw<bf16> raw_few(const bf16 *p, int count)
+{
+    Raw<bf16> r = no_raw(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (2 * k < count) r.a[k] = p[2 * k].bits;
+        if (2 * k + 1 < count) r.a[k] |= (uint32_t)p[2 * k + 1].bits << 16;
+    }
+    return r;
+}
+
+// The elements c .. c + 7 of a row of n, c a multiple of 8.  Where the row ends among them, its last eight are read instead, with the same
+// access as everywhere (element by element, a row's end costs as many waits as it has elements: 771 channels 60 us, 768 42 us), and settle()
+// brings them to their places, zeros behind them: once they are needed, so that a read ahead is not waited for.
+template <bool NT = false, class T, class I>
+__device__ __forceinline__ Raw<T> raw_at(const T *row, I c, I n)
+{
+    const I left = n - c;
+    if (left <= 0) return no_raw(row);
+    if (left < 8 && c == 0) return raw_few(row, (int)left);
+    return raw8<NT>(row + (left < 8 ? n - 8 : c));
+}
+
+__device__ __forceinline__ void move_down(Raw<float> &r, int by)
+{
+    if (by & 4) {
+        r.a = r.b;
+        r.b = u32x4{0u, 0u, 0u, 0u};
+    }
+    if (by & 2) {
+        r.a = u32x4{r.a.z, r.a.w, r.b.x, r.b.y};
+        r.b = u32x4{r.b.z, r.b.w, 0u, 0u};
+    }
+    if (by & 1) {
+        r.a = u32x4{r.a.y, r.a.z, r.a.w, r.b.x};
+        r.b = u32x4{r.b.y, r.b.z, r.b.w, 0u};
+    }
+}
+
+__device__ __forceinline__ void move_down(Raw<bf16> &r, int by)
+{
+    if (by & 4) r.a = u32x4{r.a.z, r.a.w, 0u, 0u};
+    if (by & 2) r.a = u32x4{r.a.y, r.a.z, r.a.w, 0u};
+    if (by & 1)
+        r.a = u32x4{r.a.x >> 16 | r.a.y << 16, r.a.y >> 16 | r.a.z << 16, r.a.z >> 16 | r.a.w << 16, r.a.w >> 16};
+}
+
+template <class T, class I>
+__device__ __forceinline__ void settle(Raw<T> &r, I c, I n)
+{
+    const I left = n - c;
+    if (left < 8 && left > 0 && c > 0) move_down(r, 8 - (int)left);
+}
+
+__device__ __forceinline__ void unpack(const Raw<float> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = r.a[k], hi = r.b[k];      // a bit cast of the vector's element itself takes element 0 (hipcc 7.2)
         v[k] = __builtin_bit_cast(float, lo);
         v[4 + k] = __builtin_bit_cast(float, hi);
     }
 }
 
-template <bool NT = false>
-__device__ __forceinline__ void load8(const bf16 *p, float (&v)[8])
+__device__ __forceinline__ void unpack(const Raw<bf16> &r, float (&v)[8])
 {
-    const u32x4_a2 *q = (const u32x4_a2 *)p;
-    const u32x4 a = NT ? __builtin_nontemporal_load(q) : q[0];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        v[2 * k] = __builtin_bit_cast(float, a[k] << 16);
-        v[2 * k + 1] = __builtin_bit_cast(float, a[k] & 0xFFFF0000u);
+        const uint32_t w = r.a[k];
+        v[2 * k] = __builtin_bit_cast(float, w << 16);
+        v[2 * k + 1] = __builtin_bit_cast(float, w & 0xFFFF0000u);
     }
+}
+
+template <bool NT = false, class T>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8])
+{
+    unpack(raw8<NT>(p), v);
 }
 
 template <bool NT = false>
@@ -97,36 +190,25 @@ __device__ __forceinline__ void store8(bf16 *p, const float (&v)[8])
     else *q = a;
 }
 
-// the first `cols` of eight consecutive elements (8 or more: all, 0 or fewer: none); the others are `rest`
-template <bool NT = false, class T>
-__device__ __forceinline__ void load_some(const T *p, int cols, float (&v)[8], float rest = 0.0f)
+template <bool NT = false, class T, class I>
+__device__ __forceinline__ void load_at(const T *row, I c, I n, float (&v)[8])
 {
-    // a vector by value: of an array that two branches fill, the compiler makes a choice between two addresses, one of them in scratch
-    f32x8 r = {rest, rest, rest, rest, rest, rest, rest, rest};
-    if (cols >= 8) {
-        float w[8];
-        load8<NT>(p, w);
-        r = f32x8{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
-    } else if (cols > 0) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float there = widen(p[k < cols ? k : 0]);
-            r[k] = k < cols ? there : rest;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = r[k];
+    Raw<T> r = raw_at<NT>(row, c, n);
+    settle(r, c, n);
+    unpack(r, v);
 }
 
-template <bool NT = false, class T>
-__device__ __forceinline__ void store_some(T *p, int cols, const float (&v)[8])
+template <bool NT = false, class T, class I>
+__device__ __forceinline__ void store_at(T *row, I c, I n, const float (&v)[8])
 {
-    if (cols >= 8) {
+    const I left = n - c;
+    T *p = row + c;
+    if (left >= 8) {
         store8<NT>(p, v);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k < cols) put(p + k, v[k]);
+            if (k < left) put(p + k, v[k]);
     }
 }
 
@@ -185,7 +267,7 @@ struct RowSum {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = lane_sum<64>(v[i]);
-                if ((threadIdx.x & 63) == 0) s[(threadIdx.x >> 6) * kMost + i] = v[i];
+                if ((threadIdx.x & 63) == 0) s[(threadIdx.x % TPR >> 6) * kMost + i] = v[i];
             }
             __syncthreads();
 #pragma unroll

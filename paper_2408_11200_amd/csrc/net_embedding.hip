@@ -26,14 +26,14 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(const int64_t *ids,
     const int64_t id = ids[t];
     float v[8];
     if (id >= 0 && id < V) {
-        load_some(table + id * n + c, n - c, v);
+        load_at(table + id * n, c, n, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= scale;
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 0.0f;
     }
-    store_some(y + t * n + c, n - c, v);
+    store_at(y + t * n, c, n, v);
 }
 
 // ---- the sort -------------------------------------------------------------------------------
@@ -135,7 +135,7 @@ template <class Y>
 __device__ __forceinline__ void add_row(const Y *gy, int64_t place, int n, int c, float (&t)[8])
 {
     float v[8];
-    load_some(gy + place * n + c, n - c, v);
+    load_at(gy + place * n, c, n, v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) t[k] += v[k];
 }
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(const uint32_t *ke
         float t[8] = {};
 #pragma unroll 8
         for (int i = 0; i < kPiece; ++i) add_row(gy, places[p * kPiece + i], n, c, t);
-        store_some(sums + p * n + c, n - c, t);
+        store_at(sums + p * n, c, n, t);
     }
 }
 
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void embedding_piece2_kernel(const uint32_t *k
         float t[8] = {};
 #pragma unroll 8
         for (int i = 0; i < kPiece; ++i) add_row(sums, q * kPiece + i, n, c, t);
-        store_some(sums2 + q * n + c, n - c, t);
+        store_at(sums2 + q * n, c, n, t);
     }
 }
 
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t *keys
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[k] *= scale;
-            store_some(gtable + (first + r) * n + c, n - c, t);
+            store_at(gtable + (first + r) * n, c, n, t);
         }
     }
 }

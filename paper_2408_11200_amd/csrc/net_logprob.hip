@@ -106,7 +106,10 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
     int64_t most_at = tid;
     for (int64_t p = tid; p < pieces; p += NT) {
         float v[8];
-        load_some(z + p * 8, (int)(V - p * 8 < 8 ? V - p * 8 : 8), v, -INFINITY);
+        load_at(z, p * 8, V, v);
+        if (V - p * 8 < 8)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p * 8 + k < V ? v[k] : -INFINITY;
         float m = v[0];
 #pragma unroll
         for (int k = 1; k < 8; ++k) m = fmaxf(m, v[k]);
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
             if (k) p = (all ? src : (int64_t)(uint32_t)~(uint32_t)k % NT) + i % each * NT;
         }
         float v[8];
-        load_some(z + (p < pieces ? p * 8 : 0), p < pieces ? (int)(V - p * 8 < 8 ? V - p * 8 : 8) : 0, v);
+        load_at(z, p * 8, V, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int64_t index = p * 8 + k;
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(256) void logprob_back_kernel(LogprobCall a)
     const float shift = a.g_entropy ? a.entropy[row] - logf(sum) : 0.0f;
     const float inv_sum = 1.0f / sum;
     float v[8];
-    load_some((const T *)a.logits + row * a.row_stride + c, (int)(V - c < 8 ? V - c : 8), v);
+    load_at((const T *)a.logits + row * a.row_stride, c, V, v);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const float y = (v[k] - m) * a.scale, p = __builtin_amdgcn_exp2f(y) * inv_sum;
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(256) void logprob_back_kernel(LogprobCall a)
         v[k] *= a.inv_temperature;
         if (m == -INFINITY) v[k] = 0.0f;
     }
-    store_some((T *)a.glogits + row * V + c, (int)(V - c < 8 ? V - c : 8), v);
+    store_at((T *)a.glogits + row * V, c, V, v);
 }
 
 int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, float temperature)

@@ -25,8 +25,12 @@ struct NormCall {
     float eps, residual_scale, inv_n;
 };
 
+// threads of a workgroup: the forward pass has one worker where rows take several waves; the backward pass joins the parameters' sums of
+// as many workers as 512 threads hold
 template <int TPR>
-constexpr int threads_of() { return TPR < 256 ? (TPR > 64 ? TPR : 256) : TPR; }
+constexpr int forward_threads() { return TPR > 64 ? TPR : 256; }
+template <int TPR>
+constexpr int backward_threads() { return TPR > 512 ? TPR : 512; }
 
 template <int P>
 __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, int n, float none, float (&v)[P][8])
@@ -35,7 +39,7 @@ __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, in
     for (int q = 0; q < P; ++q) {
         const int c = (q * tpr + lane) * 8;
         if (w) {
-            load_some(w + c, n - c, v[q]);
+            load_at(w, c, n, v[q]);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[q][k] = none;
@@ -49,7 +53,7 @@ __device__ __forceinline__ void load_row(const void *base, int64_t row, int lane
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         const int c = (q * tpr + lane) * 8;
-        load_some((const T *)base + row * n + c, n - c, v[q]);
+        load_at((const T *)base + row * n, c, n, v[q]);
     }
 }
 
@@ -59,7 +63,7 @@ __device__ __forceinline__ void store_row(void *base, int64_t row, int lane, int
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         const int c = (q * tpr + lane) * 8;
-        store_some((T *)base + row * n + c, n - c, v[q]);
+        store_at((T *)base + row * n, c, n, v[q]);
     }
 }
 
@@ -94,9 +98,9 @@ __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int n, flo
 }
 
 template <class X, class F, int TPR, int P, bool LAYER>
-__global__ __launch_bounds__(threads_of<TPR>()) void norm_forward_kernel(NormCall a)
+__global__ __launch_bounds__(forward_threads<TPR>()) void norm_forward_kernel(NormCall a)
 {
-    constexpr int kWorkers = threads_of<TPR>() / TPR;
+    constexpr int kWorkers = forward_threads<TPR>() / TPR;
     __shared__ float slots[RowSum<TPR>::kSlots];
     RowSum<TPR> total{slots};
     const int lane = threadIdx.x % TPR, n = a.n;
@@ -160,69 +164,110 @@ __device__ __forceinline__ void norm_back(float (&q)[P][8], const float (&vhat)[
         for (int k = 0; k < 8; ++k) q[p][k] = (q[p][k] - vhat[p][k] * c1 - c0) * r;
 }
 
-// Gradients of the rows, and of the parameters summed over a worker's rows (consecutive ones).  With one gate for all rows the worker's
-// sums of d and d * norm(f) are kept as they are: gate, w_post and b_post are common factors, put in when the workgroups' sums are added.
-// Gates of groups: `parts` > 0, a worker has a part of one group, else whole groups.
-template <class X, class F, int TPR, int P, bool LAYER, bool GROUPED>
-__global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormCall a)
+// A worker's rows of the backward pass as they lie in memory, read while the rows before are worked on
+template <class X, class F, int P>
+struct RowsAhead {
+    Raw<X> x[P], gx_out[P];
+    Raw<F> f[P], gh[P];
+    float st[4];
+};
+
+template <class X, class F, int TPR, int P>
+__device__ __forceinline__ void read_ahead(RowsAhead<X, F, P> &r, const NormCall &a, int64_t row, bool live, int lane)
 {
-    constexpr int NT = threads_of<TPR>(), kWorkers = NT / TPR;
-    __shared__ float slots[RowSum<TPR>::kSlots];
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        const int c = (q * TPR + lane) * 8, n = live ? a.n : 0;
+        const int64_t at = row * a.n;
+        r.x[q] = raw_at((const X *)a.x + at, c, n);
+        r.f[q] = raw_at((const F *)a.f + at, c, a.f ? n : 0);
+        r.gx_out[q] = raw_at((const X *)a.gx_out + at, c, a.gx_out ? n : 0);
+        r.gh[q] = raw_at((const F *)a.gh + at, c, a.gh ? n : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.st[i] = live ? a.stats[row * 4 + i] : 0.0f;
+}
+
+// Gradients of the rows, and of the parameters summed over a worker's rows (consecutive ones).
+//
+// WHOLE false: all rows of a worker share a gate row (the only one, or that of the group the worker has a part of).  Gate, w_post and b_post
+// are then common factors of the sums of d and d * norm(f), put in at the end: here for a part of a group, when the workgroups' sums are
+// added for a gate that all rows share.  WHOLE true: a worker has whole groups, and writes a group's gate gradient at its end.
+// BIAS false: nobody asks for the gradient of a bias, and none is in the way of the gate's; their sums are left out.
+template <class X, class F, int TPR, int P, bool LAYER, bool WHOLE, bool BIAS>
+__global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(NormCall a)
+{
+    constexpr int NT = backward_threads<TPR>(), kWorkers = NT / TPR;
+    __shared__ float slots[RowSum<TPR>::kSlots * (TPR > 64 ? kWorkers : 1)];
     __shared__ float joined[kWorkers > 1 ? NT * 8 : 1];
-    RowSum<TPR> total{slots};
+    RowSum<TPR> total{slots + (TPR > 64 ? threadIdx.x / TPR * RowSum<TPR>::kSlots : 0)};
     const int lane = threadIdx.x % TPR, n = a.n;
     const int64_t worker = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
     int64_t row, end, group = 0;
-    if (GROUPED && a.parts) {
+    if (a.parts) {
         group = worker / a.parts;
         row = group * a.gate_rows + worker % a.parts * a.span;
         end = row + a.span < (group + 1) * a.gate_rows ? row + a.span : (group + 1) * a.gate_rows;
     } else {
         row = worker * a.span;
         end = row + a.span;
-        if (GROUPED) group = row / a.gate_rows;
+        if (WHOLE) group = row / a.gate_rows;
     }
     if (end > a.B) end = a.B;
-    const bool any = row < end;
+    const bool there = row < a.B;
+    const float *gate_row = a.f && a.p.gate && there ? a.p.gate + group * n : nullptr;
 
-    float w_post[P][8], b_post[P][8], gate[P][8], w_pre[P][8];
+    // gate * w_post and gate * b_post; gate and the other two by themselves where the gate changes on the way
+    float w_pre[P][8], w_post[P][8], b_post[P][8], gate[P][8];
     load_param<P>(a.p.w_pre, lane, TPR, n, 1.0f, w_pre);
     load_param<P>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
-    load_param<P>(a.f ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
-    load_param<P>(a.f && !GROUPED ? a.p.gate : nullptr, lane, TPR, n, 1.0f, gate);
-    float pre1[P][8] = {}, pre0[P][8] = {}, s1[P][8] = {}, s0[P][8] = {}, post1[P][8] = {}, post0[P][8] = {};
-    bool fresh = true;          // the gate's row is still to be read
-    for (; row < end; ++row) {
-        if (GROUPED && fresh) {
-            if (a.f && a.p.gate) load_param<P>(a.p.gate + group * n, lane, TPR, n, 1.0f, gate);
-            fresh = false;
-        }
-        const float *st = a.stats + row * 4;
-        const float mean_f = st[0], r_f = st[1], mean_x = st[2], r_x = st[3];
-        float v[P][8], fhat[P][8], d[P][8];
-        load_row<P, X>(a.x, row, lane, TPR, n, v);
-        if (a.gx_out) {
-            load_row<P, X>(a.gx_out, row, lane, TPR, n, d);
-        } else {
+    load_param<P>(a.f && BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
+    load_param<P>(gate_row, lane, TPR, n, 1.0f, gate);
+    if (!WHOLE)
 #pragma unroll
-            for (int q = 0; q < P; ++q)
+        for (int q = 0; q < P; ++q)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) d[q][k] = 0.0f;
+            for (int k = 0; k < 8; ++k) {
+                w_post[q][k] *= gate[q][k];
+                b_post[q][k] *= gate[q][k];
+            }
+    // of w_pre and b_pre; of w_post and b_post, without their common factors if not WHOLE; of the gate of a group if WHOLE
+    float pre1[P][8] = {}, pre0[P][8] = {}, post1[P][8] = {}, post0[P][8] = {}, gates[P][8] = {};
+    RowsAhead<X, F, P> next;
+    read_ahead<X, F, TPR, P>(next, a, row, row < end, lane);
+    // workers of several waves share their barriers: each goes through all rounds
+    for (int64_t i = 0; i < a.span; ++i, ++row) {
+        const bool live = row < end;
+        if (TPR <= 64 && !live) break;
+        // out of the registers the next row is read into
+        const float mean_f = next.st[0], r_f = next.st[1], mean_x = next.st[2], r_x = next.st[3];
+        float v[P][8], fhat[P][8], d[P][8], g[P][8];
+        Raw<X> gx_out[P];
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int c = (q * TPR + lane) * 8;
+            settle(next.x[q], c, n);
+            settle(next.f[q], c, n);
+            settle(next.gh[q], c, n);
+            settle(next.gx_out[q], c, n);
+            unpack(next.x[q], v[q]);
+            unpack(next.f[q], fhat[q]);
+            unpack(next.gh[q], g[q]);
+            gx_out[q] = next.gx_out[q];
         }
+        read_ahead<X, F, TPR, P>(next, a, row + 1, row + 1 < end, lane);
         if (a.f) {
-            load_row<P, F>(a.f, row, lane, TPR, n, fhat);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
                     fhat[q][k] = in ? (fhat[q][k] - mean_f) * r_f : 0.0f;
-                    v[q][k] = a.residual_scale * v[q][k] + gate[q][k] * (fhat[q][k] * w_post[q][k] + b_post[q][k]);
+                    const float u = fhat[q][k] * w_post[q][k] + b_post[q][k];
+                    v[q][k] = a.residual_scale * v[q][k] + (WHOLE ? gate[q][k] * u : u);
                 }
         }
         if (a.gh) {
-            float g[P][8];
-            load_row<P, F>(a.gh, row, lane, TPR, n, g);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -230,17 +275,18 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormCa
                     const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
                     v[q][k] = in ? (v[q][k] - mean_x) * r_x : 0.0f;
                     pre1[q][k] += g[q][k] * v[q][k];
-                    pre0[q][k] += g[q][k];
+                    if (BIAS) pre0[q][k] += g[q][k];
                     g[q][k] *= w_pre[q][k];
                 }
             norm_back<TPR, P, LAYER>(g, v, r_x, a.inv_n, total);
-#pragma unroll
-            for (int q = 0; q < P; ++q)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) d[q][k] += g[q][k];
         }
-        if (a.gx) {
-            float g[P][8];
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            unpack(gx_out[q], d[q]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d[q][k] += g[q][k];        // without gh: zeros
+        }
+        if (a.gx && live) {
             const float scale = a.f ? a.residual_scale : 1.0f;
 #pragma unroll
             for (int q = 0; q < P; ++q)
@@ -253,41 +299,51 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormCa
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    s1[q][k] += d[q][k] * fhat[q][k];
-                    s0[q][k] += d[q][k];
-                    d[q][k] = !LAYER || (q * TPR + lane) * 8 + k < n ? d[q][k] * gate[q][k] * w_post[q][k] : 0.0f;
+                    const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
+                    float gu = d[q][k];
+                    if (WHOLE) {
+                        gates[q][k] += gu * (fhat[q][k] * w_post[q][k] + b_post[q][k]);
+                        gu *= gate[q][k];
+                    }
+                    post1[q][k] += gu * fhat[q][k];
+                    if (BIAS) post0[q][k] += gu;
+                    d[q][k] = in ? gu * w_post[q][k] : 0.0f;
                 }
             if (a.gf) {
                 norm_back<TPR, P, LAYER>(d, fhat, r_f, a.inv_n, total);
-                store_row<P, F>(a.gf, row, lane, TPR, n, d);
+                if (live) store_row<P, F>(a.gf, row, lane, TPR, n, d);
             }
-            if (GROUPED && (row + 1 == end || (!a.parts && (row + 1) % a.gate_rows == 0))) {
-                float g[P][8];
+            if (WHOLE && live && (row + 1 == end || (row + 1) % a.gate_rows == 0)) {
+                if (a.ggate) store_row<P, float>(a.ggate, group, lane, TPR, n, gates);
+                ++group;
 #pragma unroll
                 for (int q = 0; q < P; ++q)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        g[q][k] = s1[q][k] * w_post[q][k] + s0[q][k] * b_post[q][k];
-                        post1[q][k] += gate[q][k] * s1[q][k];
-                        post0[q][k] += gate[q][k] * s0[q][k];
-                        s1[q][k] = s0[q][k] = 0.0f;
-                    }
-                if (a.ggate) store_row<P, float>(a.parts ? a.gate_part : a.ggate, a.parts ? worker : group, lane, TPR, n, g);
-                ++group;
-                fresh = true;
+                    for (int k = 0; k < 8; ++k) gates[q][k] = 0.0f;
+                if (a.p.gate && row + 1 < end) load_param<P>(a.p.gate + group * n, lane, TPR, n, 1.0f, gate);
             }
         }
     }
-    // a part without rows (the last group's, cut short by the end of the batch) still has its place among the parts
-    if (GROUPED && a.parts && !any && a.ggate && a.f && group * a.gate_rows < a.B) {
-        float g[P][8] = {};
-        store_row<P, float>(a.gate_part, worker, lane, TPR, n, g);
-    }
     if (!a.part) return;
+    if (a.parts && a.f) {
+        // a part of a group: its share of the gate's gradient, and the gate's factor of the others
+        load_param<P>(a.p.w_post, lane, TPR, n, 1.0f, w_post);
+        load_param<P>(BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
+        load_param<P>(gate_row, lane, TPR, n, 1.0f, gate);
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                gates[q][k] = post1[q][k] * w_post[q][k] + post0[q][k] * b_post[q][k];
+                post1[q][k] *= gate[q][k];
+                post0[q][k] *= gate[q][k];
+            }
+        if (a.ggate && group * a.gate_rows < a.B) store_row<P, float>(a.gate_part, worker, lane, TPR, n, gates);
+    }
     const auto leave = [&](float (&v)[P][8], int which) {
         float *to = a.part + ((int64_t)blockIdx.x * 4 + which) * n;
         if constexpr (kWorkers > 1) {
-            static_assert(P == 1, "rows within a wave");
+            static_assert(P == 1, "one piece a lane");
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < 8; ++k) joined[(threadIdx.x / TPR * 8 + k) * TPR + lane] = v[0][k];
@@ -299,7 +355,7 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormCa
                 for (int w = 0; w < kWorkers; ++w)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) t[k] += joined[(w * 8 + k) * TPR + lane];
-                store_some(to + lane * 8, n - lane * 8, t);
+                store_at(to, lane * 8, n, t);
             }
         } else {
             store_row<P, float>(to, 0, lane, TPR, n, v);
@@ -307,44 +363,52 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormCa
     };
     if (a.gh) {
         leave(pre1, 0);
-        leave(pre0, 1);
+        if (BIAS) leave(pre0, 1);
     }
     if (a.f) {
-        leave(GROUPED ? post1 : s1, 2);
-        leave(GROUPED ? post0 : s0, 3);
+        leave(post1, 2);
+        if (BIAS) leave(post0, 3);
     }
 }
 
+// which kernel a call takes
+struct NormPick {
+    bool layer, backward, whole, bias;
+    int blocks;
+};
+
 template <class X, class F, bool LAYER, int TPR, int P>
-hipError_t launch_norm(const NormCall &a, bool backward, bool grouped, int blocks, hipStream_t st)
+hipError_t launch_norm(const NormCall &a, const NormPick &p, hipStream_t st)
 {
-    prof::Timed timed(backward ? "block_norm_backward" : "block_norm_forward", st);
-    if (!backward) norm_forward_kernel<X, F, TPR, P, LAYER><<<blocks, threads_of<TPR>(), 0, st>>>(a);
-    else if (grouped) norm_backward_kernel<X, F, TPR, P, LAYER, true><<<blocks, threads_of<TPR>(), 0, st>>>(a);
-    else norm_backward_kernel<X, F, TPR, P, LAYER, false><<<blocks, threads_of<TPR>(), 0, st>>>(a);
+    prof::Timed timed(p.backward ? "block_norm_backward" : "block_norm_forward", st);
+    constexpr int NT = backward_threads<TPR>();
+    if (!p.backward) norm_forward_kernel<X, F, TPR, P, LAYER><<<p.blocks, forward_threads<TPR>(), 0, st>>>(a);
+    else if (p.whole && p.bias) norm_backward_kernel<X, F, TPR, P, LAYER, true, true><<<p.blocks, NT, 0, st>>>(a);
+    else if (p.whole) norm_backward_kernel<X, F, TPR, P, LAYER, true, false><<<p.blocks, NT, 0, st>>>(a);
+    else if (p.bias) norm_backward_kernel<X, F, TPR, P, LAYER, false, true><<<p.blocks, NT, 0, st>>>(a);
+    else norm_backward_kernel<X, F, TPR, P, LAYER, false, false><<<p.blocks, NT, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <class X, class F, bool LAYER>
-hipError_t launch_norm_types(const NormCall &a, bool backward, bool grouped, int blocks, hipStream_t st)
+hipError_t launch_norm_types(const NormCall &a, const NormPick &p, hipStream_t st)
 {
     switch (lanes_of_row(a.n)) {
-    case 8: return launch_norm<X, F, LAYER, 8, 1>(a, backward, grouped, blocks, st);
-    case 16: return launch_norm<X, F, LAYER, 16, 1>(a, backward, grouped, blocks, st);
-    case 32: return launch_norm<X, F, LAYER, 32, 1>(a, backward, grouped, blocks, st);
-    case 64: return launch_norm<X, F, LAYER, 64, 1>(a, backward, grouped, blocks, st);
-    case 128: return launch_norm<X, F, LAYER, 128, 1>(a, backward, grouped, blocks, st);
-    case 256: return launch_norm<X, F, LAYER, 256, 1>(a, backward, grouped, blocks, st);
-    case 512: return launch_norm<X, F, LAYER, 512, 1>(a, backward, grouped, blocks, st);
+    case 8: return launch_norm<X, F, LAYER, 8, 1>(a, p, st);
+    case 16: return launch_norm<X, F, LAYER, 16, 1>(a, p, st);
+    case 32: return launch_norm<X, F, LAYER, 32, 1>(a, p, st);
+    case 64: return launch_norm<X, F, LAYER, 64, 1>(a, p, st);
+    case 128: return launch_norm<X, F, LAYER, 128, 1>(a, p, st);
+    case 256: return launch_norm<X, F, LAYER, 256, 1>(a, p, st);
+    case 512: return launch_norm<X, F, LAYER, 512, 1>(a, p, st);
     default: break;
     }
-    return a.n <= 8192 ? launch_norm<X, F, LAYER, 1024, 1>(a, backward, grouped, blocks, st)
-                       : launch_norm<X, F, LAYER, 1024, 2>(a, backward, grouped, blocks, st);
+    return a.n <= 8192 ? launch_norm<X, F, LAYER, 1024, 1>(a, p, st) : launch_norm<X, F, LAYER, 1024, 2>(a, p, st);
 }
 
 // one translation unit for each: the kernels of both passes for these types
-hipError_t launch_norm_f32(const NormCall &a, bool layer, bool backward, bool grouped, int blocks, hipStream_t st);
-hipError_t launch_norm_bf16_f32(const NormCall &a, bool layer, bool backward, bool grouped, int blocks, hipStream_t st);
-hipError_t launch_norm_bf16(const NormCall &a, bool layer, bool backward, bool grouped, int blocks, hipStream_t st);
+hipError_t launch_norm_f32(const NormCall &a, const NormPick &p, hipStream_t st);
+hipError_t launch_norm_bf16_f32(const NormCall &a, const NormPick &p, hipStream_t st);
+hipError_t launch_norm_bf16(const NormCall &a, const NormPick &p, hipStream_t st);
 
 }  // namespace kannet

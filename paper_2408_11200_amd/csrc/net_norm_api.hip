@@ -5,54 +5,60 @@
 namespace kannet {
 namespace {
 
-constexpr int kColumns = 64, kSegments = 16;     // a workgroup of the reduction: columns, and threads that share one
+constexpr int kColumns = 32, kSegments = 32;     // a workgroup of the reduction: columns, and threads that share one
 
 struct NormReduce {
     const float *part, *gate_part;
     kan_block_norm_params p;
     kan_block_norm_grads g;
-    int64_t B, gate_rows;
     int n, blocks, parts;
-    bool grouped, pre, post;
+    bool by_group, bias, pre, post;
 };
 
+// sum over `count` rows of partial sums, in a fixed order: segments of rows a thread each, several loads in flight
 __device__ __forceinline__ float column_sum(const float *from, int64_t stride, int count, int column, int n, float (*lds)[kColumns])
 {
     const int s = threadIdx.x / kColumns, c = threadIdx.x % kColumns;
-    float t = 0.0f;
-    if (column < n)
-        for (int i = s; i < count; i += kSegments) t += from[i * stride + column];
+    float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (column < n) {
+        int i = s;
+        for (; i + 3 * kSegments < count; i += 4 * kSegments)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] += from[(i + k * kSegments) * stride + column];
+        for (; i < count; i += kSegments) t[0] += from[i * stride + column];
+    }
     __syncthreads();
-    lds[s][c] = t;
+    lds[s][c] = (t[0] + t[1]) + (t[2] + t[3]);
     __syncthreads();
     float total = 0.0f;
-    for (int i = 0; i < kSegments; ++i) total += lds[i][c];
+    if (s == 0)
+        for (int i = 0; i < kSegments; ++i) total += lds[i][c];
     return total;
 }
 
-// blockIdx.y: 0 w_pre, 1 b_pre, 2 w_post (and the gate, where there is one), 3 b_post, 4 + group: a group's gate
+// blockIdx.y: 0 w_pre, 1 b_pre, 2 w_post, b_post and a gate that all rows share, 3 + group: a group's gate from its parts
 __global__ __launch_bounds__(kColumns *kSegments) void norm_reduce_kernel(NormReduce a)
 {
     __shared__ float lds[kSegments][kColumns];
     const int which = blockIdx.y, n = a.n, c = blockIdx.x * kColumns + threadIdx.x % kColumns;
     const bool mine = threadIdx.x < kColumns && c < n;
-    if (which >= 4) {
-        const int64_t group = which - 4;
+    if (which >= 3) {
+        const int64_t group = which - 3;
         const float t = column_sum(a.gate_part + group * a.parts * n, n, a.parts, c, n, lds);
         if (mine) a.g.ggate[group * n + c] = t;
         return;
     }
-    const bool there = which < 2 ? a.pre : a.post;
+    const bool there = which < 2 ? a.pre && (which == 0 || a.bias) : a.post;
     const float t = there ? column_sum(a.part + (int64_t)which * n, 4ll * n, a.blocks, c, n, lds) : 0.0f;
-    const float gate = mine && !a.grouped && a.post && a.p.gate ? a.p.gate[c] : 1.0f;
     if (which == 0 && mine && a.g.gw_pre) a.g.gw_pre[c] = t;
     if (which == 1 && mine && a.g.gb_pre) a.g.gb_pre[c] = t;
-    if (which == 2 && mine && a.g.gw_post) a.g.gw_post[c] = t * gate;
-    if (which == 3 && mine && a.g.gb_post) a.g.gb_post[c] = t * gate;
-    if (which == 2 && a.g.ggate && !a.grouped) {
-        const float t0 = there && a.p.b_post ? column_sum(a.part + 3ll * n, 4ll * n, a.blocks, c, n, lds) : 0.0f;
-        if (mine) a.g.ggate[c] = t * (a.post && a.p.w_post ? a.p.w_post[c] : 1.0f) + (a.post && a.p.b_post ? t0 * a.p.b_post[c] : 0.0f);
-    }
+    if (which < 2) return;
+    const float t0 = there && a.bias ? column_sum(a.part + 3ll * n, 4ll * n, a.blocks, c, n, lds) : 0.0f;
+    if (!mine) return;
+    const float gate = !a.by_group && there && a.p.gate ? a.p.gate[c] : 1.0f;
+    if (a.g.gw_post) a.g.gw_post[c] = t * gate;
+    if (a.g.gb_post) a.g.gb_post[c] = t0 * gate;
+    if (a.g.ggate && !a.by_group) a.g.ggate[c] = t * (there && a.p.w_post ? a.p.w_post[c] : 1.0f) + (there && a.p.b_post ? t0 * a.p.b_post[c] : 0.0f);
 }
 
 struct Cut {
@@ -61,27 +67,32 @@ struct Cut {
     int64_t workers;
 };
 
-int workers_of_block(int n) { return lanes_of_row(n) > 64 ? 1 : 256 / lanes_of_row(n); }
+int forward_workers(int n) { return lanes_of_row(n) > 64 ? 1 : 256 / lanes_of_row(n); }
+int backward_workers(int n) { return lanes_of_row(n) > 512 ? 1 : 512 / lanes_of_row(n); }
 
-// Rows of a worker in the backward pass: about two workgroups a CU (1024 threads: one), four rows at least, so that the partial sums of
-// the parameters stay below what the rows themselves cost.
+// Rows of a worker in the backward pass: two workgroups a CU (of 1024 threads: one), two rows at least, so that the partial sums of the
+// parameters stay below what the rows themselves cost.
 Cut cut_rows(const kan_block_norm_desc *d, int64_t B)
 {
-    const int per_block = workers_of_block(d->n);
-    const int64_t most = (int64_t)per_block * (lanes_of_row(d->n) >= 1024 ? 256 : 512);
+    const int per_block = backward_workers(d->n);
+    const int64_t most = (int64_t)per_block * 256;
     Cut c;
     c.span = div_up(B, most);
-    if (c.span < 4) c.span = 4;
+    if (c.span < 2) c.span = 2;
     c.parts = 0;
-    if (d->gate_rows > 0) {
-        if (d->gate_rows >= c.span && d->gate_rows < B) {
+    if (d->gate_rows > 0 && d->gate_rows < B) {
+        if (d->gate_rows >= c.span) {
+            // as many parts as leave all workers in one round
+            const int64_t groups = div_up(B, d->gate_rows), room = most / groups > 1 ? most / groups : 1;
+            int64_t parts = div_up(d->gate_rows, c.span);
+            if (parts > room) parts = room;
+            c.span = div_up(d->gate_rows, parts);
             c.parts = (int)div_up(d->gate_rows, c.span);
-            c.span = div_up(d->gate_rows, (int64_t)c.parts);
-            c.workers = div_up(B, d->gate_rows) * c.parts;
+            c.workers = groups * c.parts;
             c.blocks = (int)div_up(c.workers, (int64_t)per_block);
             return c;
         }
-        if (d->gate_rows < c.span) c.span = c.span / d->gate_rows * d->gate_rows;
+        c.span = c.span / d->gate_rows * d->gate_rows;
     }
     c.workers = div_up(B, c.span);
     c.blocks = (int)div_up(c.workers, (int64_t)per_block);
@@ -112,12 +123,9 @@ int check_pointers(const kan_block_norm_desc *d, std::initializer_list<const voi
     return KAN_OK;
 }
 
-hipError_t launch(const kan_block_norm_desc *d, const NormCall &a, bool backward, bool by_group, int blocks, hipStream_t st)
+hipError_t launch(const kan_block_norm_desc *d, const NormCall &a, const NormPick &p, hipStream_t st)
 {
-    const bool layer = d->norm == KAN_NORM_LAYER;
-    return d->stream_type == KAN_F32 ? launch_norm_f32(a, layer, backward, by_group, blocks, st)
-         : d->branch_type == KAN_F32 ? launch_norm_bf16_f32(a, layer, backward, by_group, blocks, st)
-                                     : launch_norm_bf16(a, layer, backward, by_group, blocks, st);
+    return d->stream_type == KAN_F32 ? launch_norm_f32(a, p, st) : d->branch_type == KAN_F32 ? launch_norm_bf16_f32(a, p, st) : launch_norm_bf16(a, p, st);
 }
 
 NormCall call_of(const kan_block_norm_desc *d, int64_t B, const void *x, const void *f, const kan_block_norm_params *p)
@@ -158,9 +166,10 @@ extern "C" int kan_block_norm_forward(const kan_block_norm_desc *desc, int64_t B
     a.x_out = x_out;
     a.h = h;
     a.stats = stats;
-    const int64_t blocks = div_up(B, (int64_t)workers_of_block(desc->n));
+    const int64_t blocks = div_up(B, (int64_t)forward_workers(desc->n));
     const int64_t most = lanes_of_row(desc->n) >= 512 ? 1024 : 2048;
-    return status_of(launch(desc, a, false, false, (int)(blocks < most ? blocks : most), (hipStream_t)stream));
+    const NormPick pick = {desc->norm == KAN_NORM_LAYER, false, false, false, (int)(blocks < most ? blocks : most)};
+    return status_of(launch(desc, a, pick, (hipStream_t)stream));
 }
 
 extern "C" size_t kan_block_norm_workspace_bytes(const kan_block_norm_desc *desc, int64_t B)
@@ -189,7 +198,8 @@ extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t 
     hipStream_t st = (hipStream_t)stream;
     const Cut c = B > 0 ? cut_rows(desc, B) : Cut{0, 0, 0, 0};
     if (B > 0 && params && bad_workspace(ws, ws_bytes, kan_block_norm_workspace_bytes(desc, B))) return KAN_ERR_WORKSPACE;
-    const bool by_group = grouped(desc, B > 0 ? B : 1);
+    const bool by_group = B > 0 ? grouped(desc, B) : desc->gate_rows > 0;
+    const bool bias = q->b_post || w->gb_post || w->gb_pre;
     if (B > 0) {
         NormCall a = call_of(desc, B, x, f, p);
         a.stats = const_cast<float *>(stats);
@@ -202,7 +212,8 @@ extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t 
         a.gate_part = params ? (float *)((char *)ws + part_bytes(desc, c)) : nullptr;
         a.span = c.span;
         a.parts = c.parts;
-        const hipError_t e = launch(desc, a, true, by_group, c.blocks, st);
+        const NormPick pick = {desc->norm == KAN_NORM_LAYER, true, by_group && !c.parts, bias, c.blocks};
+        const hipError_t e = launch(desc, a, pick, st);
         if (e != hipSuccess) return KAN_ERR_HIP;
     }
     if (!params) return KAN_OK;
@@ -211,16 +222,15 @@ extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t 
     r.gate_part = (const float *)((const char *)ws + (B > 0 ? part_bytes(desc, c) : 0));
     r.p = *q;
     r.g = *w;
-    r.B = B;
-    r.gate_rows = desc->gate_rows;
     r.n = desc->n;
     r.blocks = c.blocks;
     r.parts = c.parts;
-    r.grouped = B > 0 ? by_group : desc->gate_rows > 0;
+    r.by_group = by_group;
+    r.bias = bias;
     r.pre = B > 0 && gh;
     r.post = B > 0 && f;
     const unsigned groups = c.parts && w->ggate && f ? (unsigned)div_up(B, desc->gate_rows) : 0;
     prof::Timed timed("block_norm_reduce", st);
-    norm_reduce_kernel<<<dim3((unsigned)div_up(desc->n, kColumns), 4 + groups), kColumns * kSegments, 0, st>>>(r);
+    norm_reduce_kernel<<<dim3((unsigned)div_up(desc->n, kColumns), 3 + groups), kColumns * kSegments, 0, st>>>(r);
     return status_of(hipGetLastError());
 }

@@ -3,10 +3,9 @@
 
 namespace kannet {
 
-hipError_t launch_norm_f32(const NormCall &a, bool layer, bool backward, bool grouped, int blocks, hipStream_t st)
+hipError_t launch_norm_f32(const NormCall &a, const NormPick &p, hipStream_t st)
 {
-    return layer ? launch_norm_types<float, float, true>(a, backward, grouped, blocks, st)
-                 : launch_norm_types<float, float, false>(a, backward, grouped, blocks, st);
+    return p.layer ? launch_norm_types<float, float, true>(a, p, st) : launch_norm_types<float, float, false>(a, p, st);
 }
 
 }  // namespace kannet
