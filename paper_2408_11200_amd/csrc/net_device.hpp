@@ -27,6 +27,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));     // rows of odd length start at any element: the wide accesses of global memory need
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));     // no more than the element's alignment
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float widen(float v) { return v; }

@@ -47,23 +47,15 @@ __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, in
     }
 }
 
-template <int P, class T>
-__device__ __forceinline__ void load_row(const void *base, int64_t row, int lane, int tpr, int n, float (&v)[P][8])
-{
-#pragma unroll
-    for (int q = 0; q < P; ++q) {
-        const int c = (q * tpr + lane) * 8;
-        load_at((const T *)base + row * n, c, n, v[q]);
-    }
-}
-
-template <int P, class T>
+// Past the caches where it is written once and read by other launches: of 16384 x 4096 bf16 the backward pass took 151 us with such stores and
+// 171 without, of 16384 x 512 fp32 the forward pass 25 and 30.  (Such loads cost more than they gave: x and f are read by both passes.)
+template <int P, class T, bool NT = true>
 __device__ __forceinline__ void store_row(void *base, int64_t row, int lane, int tpr, int n, const float (&v)[P][8])
 {
 #pragma unroll
     for (int q = 0; q < P; ++q) {
         const int c = (q * tpr + lane) * 8;
-        store_at((T *)base + row * n, c, n, v[q]);
+        store_at<NT>((T *)base + row * n, c, n, v[q]);
     }
 }
 
@@ -111,12 +103,30 @@ __global__ __launch_bounds__(forward_threads<TPR>()) void norm_forward_kernel(No
     load_param<P>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
     load_param<P>(a.f ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
     load_param<P>(a.f && !a.gate_rows ? a.p.gate : nullptr, lane, TPR, n, 1.0f, gate);
-    for (int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR; row < a.B; row += step) {
-        float v[P][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        load_row<P, X>(a.x, row, lane, TPR, n, v);
+    int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
+    Raw<X> next_x[P];
+    Raw<F> next_f[P];
+    const auto read_ahead = [&](int64_t r) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int c = (q * TPR + lane) * 8, m = r < a.B ? n : 0;
+            next_x[q] = raw_at((const X *)a.x + r * n, c, m);
+            next_f[q] = raw_at((const F *)a.f + r * n, c, a.f ? m : 0);
+        }
+    };
+    read_ahead(row);
+    for (; row < a.B; row += step) {
+        float v[P][8], u[P][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            const int c = (q * TPR + lane) * 8;
+            settle(next_x[q], c, n);
+            settle(next_f[q], c, n);
+            unpack(next_x[q], v[q]);
+            unpack(next_f[q], u[q]);
+        }
+        read_ahead(row + step);
         if (a.f) {
-            float u[P][8];
-            load_row<P, F>(a.f, row, lane, TPR, n, u);
             if (a.gate_rows && a.p.gate) load_param<P>(a.p.gate + row / a.gate_rows * n, lane, TPR, n, 1.0f, gate);
             normalise<TPR, P, LAYER>(u, lane, n, a.inv_n, a.eps, total, st[0], st[1]);
 #pragma unroll
@@ -199,7 +209,8 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
 {
     constexpr int NT = backward_threads<TPR>(), kWorkers = NT / TPR;
     __shared__ float slots[RowSum<TPR>::kSlots * (TPR > 64 ? kWorkers : 1)];
-    __shared__ float joined[kWorkers > 1 ? NT * 8 : 1];
+    constexpr int kJoin = TPR < 64 ? NT / 64 : kWorkers;       // workers of one wave are joined by shuffles first
+    __shared__ float joined[kWorkers > 1 ? kJoin * TPR * 8 : 1];
     RowSum<TPR> total{slots + (TPR > 64 ? threadIdx.x / TPR * RowSum<TPR>::kSlots : 0)};
     const int lane = threadIdx.x % TPR, n = a.n;
     const int64_t worker = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
@@ -231,6 +242,29 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 w_post[q][k] *= gate[q][k];
                 b_post[q][k] *= gate[q][k];
             }
+    // 1024 threads have 128 registers: the parameters wait in LDS, each lane's own, until they are needed.  8192 channels in fp32, layer norm
+    // with biases: 323 us with what did not fit in scratch, 221 so; the smallest kernel has 44 bytes in scratch and is faster with them (150, 174).
+    constexpr bool kAside = TPR == 1024 && P == 1 && (LAYER || WHOLE || BIAS || sizeof(F) == 4);
+    __shared__ f32x4 aside[kAside ? 6 : 1][kAside ? 1024 : 1];
+    const auto put_aside = [&](int which, const float (&v)[P][8]) {
+        aside[2 * which][threadIdx.x] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
+        aside[2 * which + 1][threadIdx.x] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
+    };
+    const auto fetch = [&](int which, float (&v)[P][8]) {
+        if constexpr (kAside) {
+            const f32x4 lo = aside[2 * which][threadIdx.x], hi = aside[2 * which + 1][threadIdx.x];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[0][k] = lo[k];
+                v[0][4 + k] = hi[k];
+            }
+        }
+    };
+    if constexpr (kAside) {
+        put_aside(0, w_pre);
+        put_aside(1, w_post);
+        if (BIAS) put_aside(2, b_post);
+    }
     // of w_pre and b_pre; of w_post and b_post, without their common factors if not WHOLE; of the gate of a group if WHOLE
     float pre1[P][8] = {}, pre0[P][8] = {}, post1[P][8] = {}, post0[P][8] = {}, gates[P][8] = {};
     RowsAhead<X, F, P> next;
@@ -257,6 +291,8 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
         }
         read_ahead<X, F, TPR, P>(next, a, row + 1, row + 1 < end, lane);
         if (a.f) {
+            fetch(1, w_post);
+            if (BIAS) fetch(2, b_post);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -268,6 +304,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 }
         }
         if (a.gh) {
+            fetch(0, w_pre);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -295,6 +332,8 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             store_row<P, X>(a.gx, row, lane, TPR, n, g);
         }
         if (a.f) {
+            fetch(1, w_post);
+            if (WHOLE && BIAS) fetch(2, b_post);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -314,7 +353,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 if (live) store_row<P, F>(a.gf, row, lane, TPR, n, d);
             }
             if (WHOLE && live && (row + 1 == end || (row + 1) % a.gate_rows == 0)) {
-                if (a.ggate) store_row<P, float>(a.ggate, group, lane, TPR, n, gates);
+                if (a.ggate) store_row<P, float, false>(a.ggate, group, lane, TPR, n, gates);
                 ++group;
 #pragma unroll
                 for (int q = 0; q < P; ++q)
@@ -338,27 +377,32 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 post1[q][k] *= gate[q][k];
                 post0[q][k] *= gate[q][k];
             }
-        if (a.ggate && group * a.gate_rows < a.B) store_row<P, float>(a.gate_part, worker, lane, TPR, n, gates);
+        if (a.ggate && group * a.gate_rows < a.B) store_row<P, float, false>(a.gate_part, worker, lane, TPR, n, gates);
     }
     const auto leave = [&](float (&v)[P][8], int which) {
         float *to = a.part + ((int64_t)blockIdx.x * 4 + which) * n;
         if constexpr (kWorkers > 1) {
             static_assert(P == 1, "one piece a lane");
-            __syncthreads();
+            for (int by = TPR; by < 64; by *= 2)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) joined[(threadIdx.x / TPR * 8 + k) * TPR + lane] = v[0][k];
+                for (int k = 0; k < 8; ++k) v[0][k] += __shfl_xor(v[0][k], by, 64);
+            __syncthreads();
+            const int part = threadIdx.x / (TPR < 64 ? 64 : TPR);
+            if (threadIdx.x % 64 < TPR)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) joined[(part * 8 + k) * TPR + lane] = v[0][k];
             __syncthreads();
             if (threadIdx.x < TPR) {
                 float t[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) t[k] = 0.0f;
-                for (int w = 0; w < kWorkers; ++w)
+                for (int w = 0; w < kJoin; ++w)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) t[k] += joined[(w * 8 + k) * TPR + lane];
                 store_at(to, lane * 8, n, t);
             }
         } else {
-            store_row<P, float>(to, 0, lane, TPR, n, v);
+            store_row<P, float, false>(to, 0, lane, TPR, n, v);
         }
     };
     if (a.gh) {
