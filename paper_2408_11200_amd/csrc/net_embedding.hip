@@ -42,7 +42,7 @@ struct SortPass {
     const int64_t *ids;                 // first pass: keys come from here (ids outside the table: V), places are 0, 1, 2, ...
     const uint32_t *key_in, *place_in;
     uint32_t *key_out, *place_out;
-    uint32_t *counts;                   // [digits][blocks]
+    uint32_t *counts;                   // [blocks][digits]
     int64_t V;
     uint32_t T, per_block;
     int blocks, shift, bits;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(SortPass 
     const uint32_t from = blockIdx.x * a.per_block, to = from + a.per_block < a.T ? from + a.per_block : a.T;
     for (uint32_t i = from + threadIdx.x; i < to; i += kSortThreads) atomicAdd(&count[key_at(a, i) >> a.shift & (digits - 1)], 1u);
     __syncthreads();
-    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.counts[d * a.blocks + blockIdx.x] = count[d];
+    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.counts[blockIdx.x * digits + d] = count[d];
 }
 
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass a)
@@ -82,11 +82,12 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass 
     // of each digit (one a thread): entries in all blocks, and in the blocks before this one
     uint32_t all = 0, before = 0;
     if (threadIdx.x < digits) {
-        const uint32_t *row = a.counts + threadIdx.x * a.blocks;
-        for (int b = 0; b < a.blocks; ++b) {
-            const uint32_t v = row[b];
+        const uint32_t *column = a.counts + threadIdx.x;
+#pragma unroll 8
+        for (uint32_t b = 0; b < (uint32_t)a.blocks; ++b) {
+            const uint32_t v = column[b * digits];
             all += v;
-            if (b < (int)blockIdx.x) before += v;
+            before += b < blockIdx.x ? v : 0u;
         }
     }
     // entries of smaller digits: a running sum over the threads
@@ -130,57 +131,91 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass 
 
 // ---- sums -----------------------------------------------------------------------------------
 
-// adds eight channels of row `place`
-template <class Y>
-__device__ __forceinline__ void add_row(const Y *gy, int64_t place, int n, int c, float (&t)[8])
+// Adds eight channels of `count` rows to t, one after the other, as many of them in flight as fit the registers: the rows `first`, first + 1, ...
+// of a table, or those that `places` names.
+template <int AHEAD, class Y>
+__device__ __forceinline__ void add_rows(const Y *rows, const uint32_t *places, uint32_t first, uint32_t count, int n, int c, float (&t)[8])
 {
-    float v[8];
-    load_at(gy + place * n, c, n, v);
+    uint32_t i = 0;
+    for (; i + AHEAD <= count; i += AHEAD) {
+        Raw<Y> r[AHEAD];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) t[k] += v[k];
+        for (int k = 0; k < AHEAD; ++k) r[k] = raw_at(rows + (int64_t)(places ? places[first + i + k] : first + i + k) * n, c, n);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            float v[8];
+            settle(r[k], c, n);
+            unpack(r[k], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] += v[j];
+        }
+    }
+    for (; i < count; ++i) {
+        float v[8];
+        load_at(rows + (int64_t)(places ? places[first + i] : first + i) * n, c, n, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] += v[j];
+    }
 }
 
-// piece p: sorted places 32 p .. 32 p + 31, summed where all have the same id
+// Pieces of 32 consecutive entries that have one id: of the sorted list (`places` names rows of gy), or of the pieces themselves (`step` = 32
+// entries of the list each).  Narrow rows leave the workgroup several workers, which take a share of the 32 each.
 template <class Y>
-__global__ __launch_bounds__(256) void embedding_piece_kernel(const uint32_t *keys, const uint32_t *places, const Y *gy, float *sums, int64_t V, int n)
+__global__ __launch_bounds__(256) void embedding_piece_kernel(const uint32_t *keys, const uint32_t *places, const Y *rows, float *sums, int64_t V, int n, int lanes,
+                                                              int step)
 {
-    const int64_t p = blockIdx.x;
-    const uint32_t id = keys[p * kPiece];
-    if (id >= V || keys[p * kPiece + kPiece - 1] != id) return;
-    for (int c = (blockIdx.y * 256 + threadIdx.x) * 8; c < n; c += gridDim.y * 256 * 8) {
-        float t[8] = {};
-#pragma unroll 8
-        for (int i = 0; i < kPiece; ++i) add_row(gy, places[p * kPiece + i], n, c, t);
-        store_at(sums + p * n, c, n, t);
+    __shared__ float lds[256 * 8];
+    const uint32_t p = blockIdx.x, width = kPiece * step;
+    const uint32_t id = keys[p * width];
+    if (id >= V || keys[(p + 1) * width - 1] != id) return;
+    const int workers = 256 / lanes < kPiece ? 256 / lanes : kPiece, each = kPiece / workers;
+    const int w = threadIdx.x / lanes, lane = threadIdx.x % lanes, c = (blockIdx.y * lanes + lane) * 8;
+    float t[8] = {};
+    if (w < workers) add_rows<8>(rows, places, p * kPiece + w * each, each, n, c, t);
+    if (workers > 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) lds[k * 256 + threadIdx.x] = t[k];
+        __syncthreads();
+        if (w > 0) return;
+        for (int o = 1; o < workers; ++o)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] += lds[k * 256 + o * lanes + lane];
     }
-}
-
-// piece q of the second level: 32 pieces
-__global__ __launch_bounds__(256) void embedding_piece2_kernel(const uint32_t *keys, const float *sums, float *sums2, int64_t V, int n)
-{
-    const int64_t q = blockIdx.x;
-    const uint32_t id = keys[q * kPiece * kPiece];
-    if (id >= V || keys[(q + 1) * kPiece * kPiece - 1] != id) return;
-    for (int c = (blockIdx.y * 256 + threadIdx.x) * 8; c < n; c += gridDim.y * 256 * 8) {
-        float t[8] = {};
-#pragma unroll 8
-        for (int i = 0; i < kPiece; ++i) add_row(sums, q * kPiece + i, n, c, t);
-        store_at(sums2 + q * n, c, n, t);
-    }
+    store_at(sums + (int64_t)p * n, c, n, t);
 }
 
 constexpr int kRows = 32;       // table rows of a workgroup
+
+// the number of keys below `row` among `count` of them, by the whole workgroup: 256 samples at a time
+__device__ __forceinline__ uint32_t keys_below(const uint32_t *keys, uint32_t count, int64_t row, uint32_t *lds)
+{
+    uint32_t from = 0;
+    while (count > 0) {
+        // a sample ends each of (up to) 256 equal stretches: those whose last key is below lie in front
+        const uint32_t stretch = (count + 255) / 256, at = (threadIdx.x + 1) * stretch - 1;
+        const bool below = at < count && (int64_t)keys[from + at] < row;
+        const uint64_t votes = __ballot(below);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = (uint32_t)__popcll(votes);
+        __syncthreads();
+        const uint32_t skip = (lds[0] + lds[1] + lds[2] + lds[3]) * stretch;
+        from += skip;
+        count = count - skip < stretch - 1 ? count - skip : stretch - 1;
+    }
+    return from;
+}
 
 template <class Y, class G>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t *keys, const uint32_t *places, const Y *gy, const float *sums, const float *sums2,
                                                             G *gtable, uint32_t T, int64_t V, int n, int lanes, float scale)
 {
-    __shared__ uint32_t start[kRows + 1];
+    __shared__ uint32_t start[kRows + 1], lds[4];
     const int64_t first = (int64_t)blockIdx.x * kRows;
+    const uint32_t begin = keys_below(keys, T, first, lds), rest = keys_below(keys + begin, T - begin, first + kRows, lds);
     if (threadIdx.x <= kRows) {
         // the first sorted place whose id is not below this row
         const int64_t row = first + threadIdx.x;
-        uint32_t lo = 0, hi = T;
+        uint32_t lo = begin, hi = begin + rest;
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2;
             if ((int64_t)keys[mid] < row) lo = mid + 1;
@@ -192,24 +227,29 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t *keys
     const int workers = 256 / lanes;
     for (int r = threadIdx.x / lanes; r < kRows && first + r < V; r += workers) {
         const uint32_t from = start[r], to = start[r + 1];
+        // the run in whole pieces and what lies before and behind them, and these again in pieces of pieces
+        uint32_t p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;
+        if (p1 <= p0) p0 = p1 = 0;
+        uint32_t q0 = (p0 + kPiece - 1) / kPiece, q1 = p1 / kPiece;
+        if (!sums2 || q1 <= q0) q0 = q1 = 0;
         for (int c = threadIdx.x % lanes * 8; c < n; c += lanes * 8) {
             float t[8] = {};
-            uint32_t i = from;
-            while (i < to) {
-                if (sums2 && i % (kPiece * kPiece) == 0 && to - i >= kPiece * kPiece) {
-                    add_row(sums2, i / (kPiece * kPiece), n, c, t);
-                    i += kPiece * kPiece;
-                } else if (i % kPiece == 0 && to - i >= kPiece) {
-                    add_row(sums, i / kPiece, n, c, t);
-                    i += kPiece;
+            if (p1 > 0) {
+                add_rows<4>(gy, places, from, p0 * kPiece - from, n, c, t);
+                if (q1 > 0) {
+                    add_rows<4>(sums, nullptr, p0, q0 * kPiece - p0, n, c, t);
+                    add_rows<4>(sums2, nullptr, q0, q1 - q0, n, c, t);
+                    add_rows<4>(sums, nullptr, q1 * kPiece, p1 - q1 * kPiece, n, c, t);
                 } else {
-                    add_row(gy, places[i], n, c, t);
-                    ++i;
+                    add_rows<4>(sums, nullptr, p0, p1 - p0, n, c, t);
                 }
+                add_rows<4>(gy, places, p1 * kPiece, to - p1 * kPiece, n, c, t);
+            } else {
+                add_rows<4>(gy, places, from, to - from, n, c, t);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[k] *= scale;
-            store_at(gtable + (first + r) * n, c, n, t);
+            store_at<true>(gtable + (first + r) * n, c, n, t);
         }
     }
 }
@@ -279,17 +319,17 @@ hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint3
                        char *ws, hipStream_t st)
 {
     const int lanes = lanes_of_row(n) < 256 ? lanes_of_row(n) : 256;
-    const unsigned wide = (unsigned)div_up(n, 2048);
+    const unsigned wide = (unsigned)div_up(n, lanes * 8);
     float *sums = (float *)(ws + l.sums), *sums2 = (float *)(ws + l.sums2);
     hipError_t e = hipSuccess;
     if (T >= kPiece) {
         prof::Timed timed("embedding_pieces", st);
-        embedding_piece_kernel<Y><<<dim3((unsigned)(T / kPiece), wide), 256, 0, st>>>(keys, places, (const Y *)gy, sums, V, n);
+        embedding_piece_kernel<Y><<<dim3((unsigned)(T / kPiece), wide), 256, 0, st>>>(keys, places, (const Y *)gy, sums, V, n, lanes, 1);
         e = hipGetLastError();
     }
     if (e == hipSuccess && l.second) {
         prof::Timed timed("embedding_pieces", st);
-        embedding_piece2_kernel<<<dim3((unsigned)(T / (kPiece * kPiece)), wide), 256, 0, st>>>(keys, sums, sums2, V, n);
+        embedding_piece_kernel<float><<<dim3((unsigned)(T / (kPiece * kPiece)), wide), 256, 0, st>>>(keys, nullptr, sums, sums2, V, n, lanes, kPiece);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
