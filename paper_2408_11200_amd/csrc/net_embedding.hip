@@ -2,11 +2,12 @@
 //
 // Forward: a copy of rows, bound by HBM (by latency for a few tokens).
 //
-// Backward: tokens are sorted by id, stably (least significant digit first, up to ten bits a pass), and each table row adds up its run of the
-// sorted list: no atomics on values, so a row's sum has one order, and rows without a token are written as zeros in the same pass, so the
-// table's gradient is written once.  A run may hold a good part of the batch (frequent tokens): pieces of 32 sorted places that lie
-// wholly within a run are summed beforehand by workgroups of their own, and pieces of 32 such pieces again, so that a run of N tokens
-// takes at most about 62 rows, 62 sums of 32 and N / 1024 sums of 1024, from as many workgroups as there are pieces.
+// Backward: tokens are sorted by id, stably (least significant digit first, up to ten bits a pass), and the sorted list is cut into pieces
+// of 16 entries, each worked on by the lanes of one row with its sixteen rows of gy in flight together.  A run of equal ids within a piece is a
+// row of the table, written at once; a run that goes on into the next piece leaves its sum there as a fragment, and a workgroup for
+// the piece it starts in joins them (of long runs, sixteen pieces at a time have been added before).  Rows without a token are zeroed by
+// other workgroups of the same launch.  So the work is cut by places of the list, however often a token occurs, every row of the
+// table is written once, and a row's sum has one order: no atomics on values.
 #include "net_device.hpp"
 
 namespace kannet {
@@ -15,7 +16,7 @@ namespace {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxDigit = 10;
 constexpr int kMaxBlocks = 64;        // of a sort pass: every block reads all blocks' counts
-constexpr int kPiece = 32;
+constexpr int kPiece = 16;
 
 template <class T, class Y>
 __global__ __launch_bounds__(256) void embedding_rows_kernel(const int64_t *ids, const T *table, Y *y, int64_t T_, int64_t V, int n, int pieces, float scale)
@@ -131,16 +132,14 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass 
 
 // ---- sums -----------------------------------------------------------------------------------
 
-// Adds eight channels of `count` rows to t, one after the other, as many of them in flight as fit the registers: the rows `first`, first + 1, ...
-// of a table, or those that `places` names.
-template <int AHEAD, class Y>
-__device__ __forceinline__ void add_rows(const Y *rows, const uint32_t *places, uint32_t first, uint32_t count, int n, int c, float (&t)[8])
+// Adds eight channels of the rows first .. first + count - 1, `stride` floats apart, to t, one after the other, AHEAD of them in flight.
+template <int AHEAD>
+__device__ __forceinline__ void add_rows(const float *rows, int64_t stride, uint32_t first, uint32_t count, int n, int c, float (&t)[8])
 {
-    uint32_t i = 0;
-    for (; i + AHEAD <= count; i += AHEAD) {
-        Raw<Y> r[AHEAD];
+    for (uint32_t i = 0; i < count; i += AHEAD) {
+        Raw<float> r[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) r[k] = raw_at(rows + (int64_t)(places ? places[first + i + k] : first + i + k) * n, c, n);
+        for (int k = 0; k < AHEAD; ++k) r[k] = raw_at(rows + (int64_t)(first + i + k) * stride, c, i + k < count ? n : 0);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             float v[8];
@@ -150,41 +149,9 @@ __device__ __forceinline__ void add_rows(const Y *rows, const uint32_t *places, 
             for (int j = 0; j < 8; ++j) t[j] += v[j];
         }
     }
-    for (; i < count; ++i) {
-        float v[8];
-        load_at(rows + (int64_t)(places ? places[first + i] : first + i) * n, c, n, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] += v[j];
-    }
 }
 
-// Pieces of 32 consecutive entries that have one id: of the sorted list (`places` names rows of gy), or of the pieces themselves (`step` = 32
-// entries of the list each).  Narrow rows leave the workgroup several workers, which take a share of the 32 each.
-template <class Y>
-__global__ __launch_bounds__(256) void embedding_piece_kernel(const uint32_t *keys, const uint32_t *places, const Y *rows, float *sums, int64_t V, int n, int lanes,
-                                                              int step)
-{
-    __shared__ float lds[256 * 8];
-    const uint32_t p = blockIdx.x, width = kPiece * step;
-    const uint32_t id = keys[p * width];
-    if (id >= V || keys[(p + 1) * width - 1] != id) return;
-    const int workers = 256 / lanes < kPiece ? 256 / lanes : kPiece, each = kPiece / workers;
-    const int w = threadIdx.x / lanes, lane = threadIdx.x % lanes, c = (blockIdx.y * lanes + lane) * 8;
-    float t[8] = {};
-    if (w < workers) add_rows<8>(rows, places, p * kPiece + w * each, each, n, c, t);
-    if (workers > 1) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) lds[k * 256 + threadIdx.x] = t[k];
-        __syncthreads();
-        if (w > 0) return;
-        for (int o = 1; o < workers; ++o)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) t[k] += lds[k * 256 + o * lanes + lane];
-    }
-    store_at(sums + (int64_t)p * n, c, n, t);
-}
-
-constexpr int kRows = 32;       // table rows of a workgroup
+constexpr int kRows = 32;       // table rows of a workgroup that looks for rows without tokens
 
 // the number of keys below `row` among `count` of them, by the whole workgroup: 256 samples at a time
 __device__ __forceinline__ uint32_t keys_below(const uint32_t *keys, uint32_t count, int64_t row, uint32_t *lds)
@@ -205,51 +172,161 @@ __device__ __forceinline__ uint32_t keys_below(const uint32_t *keys, uint32_t co
     return from;
 }
 
+struct SumCall {
+    const uint32_t *keys, *places;
+    float *fragments;       // [pieces][2][n]: of the run a piece begins with (all of the piece, or as far as the run goes), and of the one it ends with
+    float *groups;          // [pieces / 16][n]: sixteen pieces of one id; null: too few entries for that
+    uint32_t T, pieces;     // keys and places are readable up to whole pieces
+    int64_t V;
+    int n, lanes;
+    unsigned piece_blocks;
+    float scale;
+};
+
+// The first piece_blocks workgroups have the pieces, 256 / lanes each; the others 32 table rows each, which they zero where no token names them.
 template <class Y, class G>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t *keys, const uint32_t *places, const Y *gy, const float *sums, const float *sums2,
-                                                            G *gtable, uint32_t T, int64_t V, int n, int lanes, float scale)
+__global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y *gy, G *gtable)
 {
-    __shared__ uint32_t start[kRows + 1], lds[4];
-    const int64_t first = (int64_t)blockIdx.x * kRows;
-    const uint32_t begin = keys_below(keys, T, first, lds), rest = keys_below(keys + begin, T - begin, first + kRows, lds);
-    if (threadIdx.x <= kRows) {
-        // the first sorted place whose id is not below this row
-        const int64_t row = first + threadIdx.x;
-        uint32_t lo = begin, hi = begin + rest;
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if ((int64_t)keys[mid] < row) lo = mid + 1;
-            else hi = mid;
-        }
-        start[threadIdx.x] = lo;
-    }
-    __syncthreads();
-    const int workers = 256 / lanes;
-    for (int r = threadIdx.x / lanes; r < kRows && first + r < V; r += workers) {
-        const uint32_t from = start[r], to = start[r + 1];
-        // the run in whole pieces and what lies before and behind them, and these again in pieces of pieces
-        uint32_t p0 = (from + kPiece - 1) / kPiece, p1 = to / kPiece;
-        if (p1 <= p0) p0 = p1 = 0;
-        uint32_t q0 = (p0 + kPiece - 1) / kPiece, q1 = p1 / kPiece;
-        if (!sums2 || q1 <= q0) q0 = q1 = 0;
-        for (int c = threadIdx.x % lanes * 8; c < n; c += lanes * 8) {
-            float t[8] = {};
-            if (p1 > 0) {
-                add_rows<4>(gy, places, from, p0 * kPiece - from, n, c, t);
-                if (q1 > 0) {
-                    add_rows<4>(sums, nullptr, p0, q0 * kPiece - p0, n, c, t);
-                    add_rows<4>(sums2, nullptr, q0, q1 - q0, n, c, t);
-                    add_rows<4>(sums, nullptr, q1 * kPiece, p1 - q1 * kPiece, n, c, t);
-                } else {
-                    add_rows<4>(sums, nullptr, p0, p1 - p0, n, c, t);
-                }
-                add_rows<4>(gy, places, p1 * kPiece, to - p1 * kPiece, n, c, t);
-            } else {
-                add_rows<4>(gy, places, from, to - from, n, c, t);
+    __shared__ uint32_t lds[4], here[kRows];
+    const int n = a.n, lanes = a.lanes, worker = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    if (blockIdx.x >= a.piece_blocks) {
+        const int64_t first = (int64_t)(blockIdx.x - a.piece_blocks) * kRows;
+        const uint32_t begin = keys_below(a.keys, a.T, first, lds), rest = keys_below(a.keys + begin, a.T - begin, first + kRows, lds);
+        if (threadIdx.x < kRows) {
+            uint32_t lo = begin, hi = begin + rest;
+            while (lo < hi) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                if ((int64_t)a.keys[mid] < first + threadIdx.x) lo = mid + 1;
+                else hi = mid;
             }
+            here[threadIdx.x] = lo < begin + rest && (int64_t)a.keys[lo] == first + threadIdx.x;
+        }
+        __syncthreads();
+        const float zeros[8] = {};
+        for (int r = worker; r < kRows && first + r < a.V; r += 256 / lanes)
+            if (!here[r])
+                for (int c = lane * 8; c < n; c += lanes * 8) store_at<true>(gtable + (first + r) * n, c, n, zeros);
+        return;
+    }
+    const uint32_t p = blockIdx.x * (256 / lanes) + worker;
+    if (p >= a.pieces) return;
+    uint32_t key[kPiece], place[kPiece];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) t[k] *= scale;
-            store_at<true>(gtable + (first + r) * n, c, n, t);
+    for (int i = 0; i < kPiece; i += 4) {
+        const u32x4 k = *(const u32x4 *)(a.keys + p * kPiece + i), q = *(const u32x4 *)(a.places + p * kPiece + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool in = p * kPiece + i + j < a.T;
+            key[i + j] = in ? k[j] : 0xFFFFFFFFu;
+            place[i + j] = q[j];
+        }
+    }
+    const uint32_t V = (uint32_t)a.V;
+    const bool from_before = p > 0 && a.keys[p * kPiece - 1] == key[0];
+    const bool goes_on = (p + 1) * kPiece < a.T && a.keys[(p + 1) * kPiece] == key[kPiece - 1];
+    for (int c = lane * 8; c < n; c += lanes * 8) {
+        float t[8] = {};
+        bool first_run = true;
+#pragma unroll
+        for (int b = 0; b < kPiece; b += 8) {
+            Raw<Y> r[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[j] = raw_at(gy + (int64_t)place[b + j] * n, c, key[b + j] < V ? n : 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v[8];
+                settle(r[j], c, n);
+                unpack(r[j], v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) t[k] += v[k];
+                const bool last = b + j == kPiece - 1;
+                if (last || key[b + j] != key[b + j + 1 < kPiece ? b + j + 1 : 0]) {
+                    if (key[b + j] < V) {
+                        const bool left = first_run && from_before, right = last && goes_on;
+                        if (left || right) {
+                            store_at(a.fragments + ((int64_t)p * 2 + (first_run ? 0 : 1)) * n, c, n, t);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) t[k] *= a.scale;
+                            store_at<true>(gtable + (int64_t)key[b + j] * n, c, n, t);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) t[k] = 0.0f;
+                    first_run = false;
+                }
+            }
+        }
+    }
+}
+
+// sixteen pieces of one id, a workgroup each
+__global__ __launch_bounds__(256) void embedding_group_kernel(SumCall a)
+{
+    const uint32_t q = blockIdx.x, width = kPiece * kPiece;
+    if (a.keys[q * width] >= (uint32_t)a.V || a.keys[(q + 1) * width - 1] != a.keys[q * width]) return;
+    for (int c = threadIdx.x * 8; c < a.n; c += 256 * 8) {
+        float t[8] = {};
+        add_rows<8>(a.fragments + (int64_t)q * kPiece * 2 * a.n, 2ll * a.n, 0, kPiece, a.n, c, t);
+        store_at(a.groups + (int64_t)q * a.n, c, a.n, t);
+    }
+}
+
+// A workgroup for each piece that a run starts in and leaves: the run's fragments, shared among the workgroup's workers.
+template <class G>
+__global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtable)
+{
+    __shared__ float lds[256 * 8];
+    __shared__ uint32_t votes[4];
+    const uint32_t p = blockIdx.x;
+    const uint32_t id = a.keys[p * kPiece + kPiece - 1];
+    if (id >= (uint32_t)a.V || (p + 1) * kPiece >= a.T || a.keys[(p + 1) * kPiece] != id) return;
+    const bool whole = a.keys[p * kPiece] == id;
+    if (whole && p > 0 && a.keys[p * kPiece - 1] == id) return;
+    // pieces behind this one that begin with the id
+    uint32_t more = 0;
+    for (;;) {
+        const uint64_t at = (uint64_t)(p + 1 + more + threadIdx.x) * kPiece;
+        const uint64_t yes = __ballot(at < a.T && a.keys[at < a.T ? at : 0] == id);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) votes[threadIdx.x >> 6] = (uint32_t)__popcll(yes);       // the list is sorted: those that do come first
+        __syncthreads();
+        const uint32_t all = votes[0] + votes[1] + votes[2] + votes[3];
+        more += all;
+        if (all < 256) break;
+    }
+    const int n = a.n, lanes = a.lanes, workers = 256 / lanes, w = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    // pieces p + 1 .. end - 1; the groups q0 .. q1 - 1 lie wholly among those that hold nothing but the id
+    const uint32_t begin = p + 1, end = begin + more;
+    const uint64_t full_end = (uint64_t)end * kPiece <= a.T && a.keys[(uint64_t)end * kPiece - 1] == id ? end : end - 1;
+    uint32_t q0 = (begin + kPiece - 1) / kPiece, q1 = (uint32_t)(full_end / kPiece);
+    if (!a.groups || q1 <= q0) q0 = q1 = 0;
+    const uint32_t cut0 = q1 > 0 ? q0 * kPiece : end, cut1 = q1 > 0 ? q1 * kPiece : end;
+    const auto part = [&](uint32_t from, uint32_t count, int which) { return from + (uint32_t)((uint64_t)count * which / workers); };
+    for (int c0 = 0; c0 < n; c0 += lanes * 8) {
+        const int c = c0 + lane * 8;
+        float t[8] = {};
+        if (w == 0) add_rows<1>(a.fragments + ((int64_t)p * 2 + (whole ? 0 : 1)) * n, 0, 0, 1, n, c, t);
+        const uint32_t b0 = part(begin, cut0 - begin, w), b1 = part(begin, cut0 - begin, w + 1);
+        add_rows<8>(a.fragments, 2ll * n, b0, b1 - b0, n, c, t);
+        const uint32_t g0 = part(q0, q1 - q0, w), g1 = part(q0, q1 - q0, w + 1);
+        add_rows<8>(a.groups, n, g0, g1 - g0, n, c, t);
+        const uint32_t e0 = part(cut1, end - cut1, w), e1 = part(cut1, end - cut1, w + 1);
+        add_rows<8>(a.fragments, 2ll * n, e0, e1 - e0, n, c, t);
+        if (workers > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) lds[k * 256 + threadIdx.x] = t[k];
+            __syncthreads();
+            if (w == 0)
+                for (int o = 1; o < workers; ++o)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) t[k] += lds[k * 256 + o * lanes + lane];
+        }
+        if (w == 0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] *= a.scale;
+            store_at(gtable + (int64_t)id * n, c, n, t);
         }
     }
 }
@@ -259,7 +336,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t *keys
 struct Layout {
     int passes, bits, blocks;
     uint32_t per_block;
-    size_t counts, keys[2], places[2], sums, sums2, bytes;
+    size_t counts, keys[2], places[2], fragments, groups, bytes;
     bool second;
 };
 
@@ -274,7 +351,7 @@ Layout layout_of(int64_t T, int64_t V, int n)
     per = per < 1 ? kSortThreads : div_up(per, (int64_t)kSortThreads) * kSortThreads;
     l.per_block = (uint32_t)per;
     l.blocks = (int)div_up(T, per);
-    l.second = T >= 4 * kPiece * kPiece;
+    l.second = T >= 16 * kPiece * kPiece;
     size_t at = 0;
     const auto take = [&at](size_t bytes) {
         const size_t here = at;
@@ -283,11 +360,11 @@ Layout layout_of(int64_t T, int64_t V, int n)
     };
     l.counts = take((size_t)l.blocks * ((size_t)4 << l.bits));
     for (int i = 0; i < 2; ++i) {
-        l.keys[i] = take((size_t)T * 4);
-        l.places[i] = take((size_t)T * 4);
+        l.keys[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
+        l.places[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
     }
-    l.sums = take((size_t)(T / kPiece) * n * 4);
-    l.sums2 = l.second ? take((size_t)(T / (kPiece * kPiece)) * n * 4) : at;
+    l.fragments = take((size_t)div_up(T, (int64_t)kPiece) * 2 * n * 4);
+    l.groups = l.second ? take((size_t)(T / (kPiece * kPiece)) * n * 4) : at;
     l.bytes = at;
     return l;
 }
@@ -318,24 +395,32 @@ template <class Y, class G>
 hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint32_t *keys, const uint32_t *places, const void *gy, float scale, void *gtable,
                        char *ws, hipStream_t st)
 {
-    const int lanes = lanes_of_row(n) < 256 ? lanes_of_row(n) : 256;
-    const unsigned wide = (unsigned)div_up(n, lanes * 8);
-    float *sums = (float *)(ws + l.sums), *sums2 = (float *)(ws + l.sums2);
-    hipError_t e = hipSuccess;
-    if (T >= kPiece) {
+    SumCall a = {};
+    a.keys = keys;
+    a.places = places;
+    a.fragments = (float *)(ws + l.fragments);
+    a.groups = l.second ? (float *)(ws + l.groups) : nullptr;
+    a.T = (uint32_t)T;
+    a.pieces = (uint32_t)div_up(T, (int64_t)kPiece);
+    a.V = V;
+    a.n = n;
+    a.lanes = lanes_of_row(n) < 256 ? lanes_of_row(n) : 256;
+    a.piece_blocks = div_up(a.pieces, 256u / (unsigned)a.lanes);
+    a.scale = scale;
+    {
         prof::Timed timed("embedding_pieces", st);
-        embedding_piece_kernel<Y><<<dim3((unsigned)(T / kPiece), wide), 256, 0, st>>>(keys, places, (const Y *)gy, sums, V, n, lanes, 1);
-        e = hipGetLastError();
+        embedding_piece_kernel<Y, G><<<a.piece_blocks + (unsigned)div_up(V, (int64_t)kRows), 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
     }
-    if (e == hipSuccess && l.second) {
-        prof::Timed timed("embedding_pieces", st);
-        embedding_piece_kernel<float><<<dim3((unsigned)(T / (kPiece * kPiece)), wide), 256, 0, st>>>(keys, nullptr, sums, sums2, V, n, lanes, kPiece);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || T <= kPiece) return e;
+    if (l.second) {
+        prof::Timed timed("embedding_groups", st);
+        embedding_group_kernel<<<(unsigned)(T / (kPiece * kPiece)), 256, 0, st>>>(a);
         e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    if (e != hipSuccess) return e;
-    prof::Timed timed("embedding_sum", st);
-    embedding_sum_kernel<Y, G><<<(unsigned)div_up(V, (int64_t)kRows), 256, 0, st>>>(keys, places, (const Y *)gy, sums, l.second ? sums2 : nullptr, (G *)gtable,
-                                                                                   (uint32_t)T, V, n, lanes, scale);
+    prof::Timed timed("embedding_join", st);
+    embedding_join_kernel<G><<<a.pieces - 1, 256, 0, st>>>(a, (G *)gtable);
     return hipGetLastError();
 }
 
