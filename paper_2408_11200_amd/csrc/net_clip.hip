@@ -62,14 +62,17 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
 }
 
 template <class T>
-__device__ __forceinline__ double chunk_squares(const T *p, int64_t count)
+__device__ __forceinline__ double chunk_squares(const T *p, int count)
 {
+    constexpr int N = 16 / sizeof(T);
     double t = 0.0;
-    for (int64_t i = threadIdx.x * 8; i < count; i += kThreads * 8) {
-        float v[8];
-        load_at(p, i, count, v);
+    for (int i = threadIdx.x * N; i < count; i += kThreads * N) {
+        float v[N];
+        Raw<T, N> r = raw_at<N>(p, i, count);
+        settle(r, i, count);
+        unpack(r, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += (double)v[k] * (double)v[k];
+        for (int k = 0; k < N; ++k) t += (double)v[k] * (double)v[k];
     }
     return t;
 }
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipCall a)
     for (; chunk < end; ++chunk) {
         while (chunk >= a.first[i + 1]) ++i;
         const int64_t at = (int64_t)(chunk - a.first[i]) * kChunk, left = a.count[i] - at;
-        const int64_t count = left < kChunk ? left : kChunk;
+        const int count = left < kChunk ? (int)left : kChunk;
         t += a.type[i] == KAN_F32 ? chunk_squares((const float *)a.data[i] + at, count) : chunk_squares((const bf16 *)a.data[i] + at, count);
     }
     t = block_sum<kThreads>(t, lds);
@@ -100,14 +103,17 @@ __device__ __forceinline__ float norm_of(const ClipCall &a, double *lds)
 }
 
 template <class T>
-__device__ __forceinline__ void scale_chunk(const T *p, T *to, int64_t count, float factor)
+__device__ __forceinline__ void scale_chunk(const T *p, T *to, int count, float factor)
 {
-    for (int64_t i = threadIdx.x * 8; i < count; i += kThreads * 8) {
-        float v[8];
-        load_at(p, i, count, v);
+    constexpr int N = 16 / sizeof(T);
+    for (int i = threadIdx.x * N; i < count; i += kThreads * N) {
+        float v[N];
+        Raw<T, N> r = raw_at<N>(p, i, count);
+        settle(r, i, count);
+        unpack(r, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= factor;
-        store_at(to, i, count, v);
+        for (int k = 0; k < N; ++k) v[k] *= factor;
+        store_at<N>(to, i, count, v);
     }
 }
 
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipCall a)
         while (chunk >= a.first[i + 1]) ++i;
         if (factor == 1.0f && a.out[i] == a.data[i]) continue;        // in place, and nothing to change
         const int64_t at = (int64_t)(chunk - a.first[i]) * kChunk, left = a.count[i] - at;
-        const int64_t count = left < kChunk ? left : kChunk;
+        const int count = left < kChunk ? (int)left : kChunk;
         if (a.type[i] == KAN_F32) scale_chunk((const float *)a.data[i] + at, (float *)a.out[i] + at, count, factor);
         else scale_chunk((const bf16 *)a.data[i] + at, (bf16 *)a.out[i] + at, count, factor);
     }

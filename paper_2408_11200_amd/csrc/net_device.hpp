@@ -23,9 +23,16 @@ constexpr I div_up(I a, I b) { return (a + b - 1) / b; }
 
 struct bf16 { uint16_t bits; };
 
+template <class T>
+inline constexpr bool is_float = false;
+template <>
+inline constexpr bool is_float<float> = true;
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));     // rows of odd length start at any element: the wide accesses of global memory need
-typedef u32x4 u32x4_a4 __attribute__((aligned(4)));     // no more than the element's alignment
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));     // rows of odd length start at any element: the wide accesses of global memory need
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));     // no more than the element's alignment
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -41,86 +48,88 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)       // rounde
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16 *p, float v) { p->bits = (uint16_t)two_bf16(v, v); }
 
-// Eight consecutive elements as they lie in memory: what a thread holds of a row it will need later.
-template <class T>
+// N consecutive elements of a row as they lie in memory, what a lane reads or writes with one access: four of either type, or eight of bf16.
+// A row's accesses have to lie side by side over the lanes: eight floats a lane in two accesses 32 bytes apart, each of which leaves every
+// second half line, copied 500 MB at 3.7 TB/s with streaming stores and 5.8 side by side.
+template <class T, int N>
 struct Raw;
 template <>
-struct Raw<float> { u32x4 a, b; };
+struct Raw<float, 4> {
+    typedef u32x4_a4 Wide;
+    u32x4 a;
+};
 template <>
-struct Raw<bf16> { u32x4 a; };
+struct Raw<bf16, 4> {
+    typedef u32x2_a2 Wide;
+    u32x2 a;
+};
+template <>
+struct Raw<bf16, 8> {
+    typedef u32x4_a2 Wide;
+    u32x4 a;
+};
 
-template <bool NT = false>
-__device__ __forceinline__ Raw<float> raw8(const float *p)
+template <class T, int N>
+__device__ __forceinline__ Raw<T, N> no_raw()
 {
-    const u32x4_a4 *q = (const u32x4_a4 *)p;
-    if constexpr (NT) return Raw<float>{__builtin_nontemporal_load(q), __builtin_nontemporal_load(q + 1)};
-    else return Raw<float>{q[0], q[1]};
-}
-
-template <bool NT = false>
-__device__ __forceinline__ Raw<bf16> raw8(const bf16 *p)
-{
-    const u32x4_a2 *q = (const u32x4_a2 *)p;
-    if constexpr (NT) return Raw<bf16>{__builtin_nontemporal_load(q)};
-    else return Raw<bf16>{q[0]};
-}
-
-__device__ __forceinline__ Raw<float> no_raw(const float *) { return Raw<float>{u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}}; }
-__device__ __forceinline__ Raw<bf16> no_raw(const bf16 *) { return Raw<bf16>{u32x4{0u, 0u, 0u, 0u}}; }
-
-// fewer than eight, one by one: only where a whole row is that short
-__device__ __forceinline__ Raw<float> raw_few(const float *p, int count)
-{
-    Raw<float> r = no_raw(p);
-    const uint32_t *q = (const uint32_t *)p;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (k < count) r.a[k] = q[k];
-        if (4 + k < count) r.b[k] = q[4 + k];
-    }
+    Raw<T, N> r;
+    r.a = 0u;
     return r;
 }
 
-__device__ __forceinline__ Raw<bf16> raw_few(const bf16 *p, int count)
+// fewer than N elements, one by one: only where a whole row is that short
+template <int N>
+__device__ __forceinline__ Raw<float, N> raw_few(const float *p, int count)
 {
-    Raw<bf16> r = no_raw(p);
+    Raw<float, N> r = no_raw<float, N>();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N; ++k)
+        if (k < count) r.a[k] = ((const uint32_t *)p)[k];
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ Raw<bf16, N> raw_few(const bf16 *p, int count)
+{
+    Raw<bf16, N> r = no_raw<bf16, N>();
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
         if (2 * k < count) r.a[k] = p[2 * k].bits;
         if (2 * k + 1 < count) r.a[k] |= (uint32_t)p[2 * k + 1].bits << 16;
     }
     return r;
 }
 
-// The elements c .. c + 7 of a row of n, c a multiple of 8.  Where the row ends among them, its last eight are read instead, with the same
+// The elements c .. c + N - 1 of a row of n, c a multiple of N.  Where the row ends among them, its last N are read instead, with the same
 // access as everywhere (element by element, a row's end costs as many waits as it has elements: 771 channels 60 us, 768 42 us), and settle()
 // brings them to their places, zeros behind them: once they are needed, so that a read ahead is not waited for.
-template <bool NT = false, class T, class I>
-__device__ __forceinline__ Raw<T> raw_at(const T *row, I c, I n)
+template <int N, bool NT = false, class T, class I>
+__device__ __forceinline__ Raw<T, N> raw_at(const T *row, I c, I n)
 {
     const I left = n - c;
-    if (left <= 0) return no_raw(row);
-    if (left < 8 && c == 0) return raw_few(row, (int)left);
-    return raw8<NT>(row + (left < 8 ? n - 8 : c));
+    if (left <= 0) return no_raw<T, N>();
+    if (left < N && c == 0) return raw_few<N>(row, (int)left);
+    Raw<T, N> r;
+    typedef const typename Raw<T, N>::Wide *From;       // (a template parameter of this type would lose its alignment)
+    const T *p = row + (left < N ? n - N : c);
+    if constexpr (NT) r.a = __builtin_nontemporal_load((From)p);
+    else r.a = *(From)p;
+    return r;
 }
 
-__device__ __forceinline__ void move_down(Raw<float> &r, int by)
+__device__ __forceinline__ void move_down(Raw<float, 4> &r, int by)
 {
-    if (by & 4) {
-        r.a = r.b;
-        r.b = u32x4{0u, 0u, 0u, 0u};
-    }
-    if (by & 2) {
-        r.a = u32x4{r.a.z, r.a.w, r.b.x, r.b.y};
-        r.b = u32x4{r.b.z, r.b.w, 0u, 0u};
-    }
-    if (by & 1) {
-        r.a = u32x4{r.a.y, r.a.z, r.a.w, r.b.x};
-        r.b = u32x4{r.b.y, r.b.z, r.b.w, 0u};
-    }
+    if (by & 2) r.a = u32x4{r.a.z, r.a.w, 0u, 0u};
+    if (by & 1) r.a = u32x4{r.a.y, r.a.z, r.a.w, 0u};
 }
 
-__device__ __forceinline__ void move_down(Raw<bf16> &r, int by)
+__device__ __forceinline__ void move_down(Raw<bf16, 4> &r, int by)
+{
+    if (by & 2) r.a = u32x2{r.a.y, 0u};
+    if (by & 1) r.a = u32x2{r.a.x >> 16 | r.a.y << 16, r.a.y >> 16};
+}
+
+__device__ __forceinline__ void move_down(Raw<bf16, 8> &r, int by)
 {
     if (by & 4) r.a = u32x4{r.a.z, r.a.w, 0u, 0u};
     if (by & 2) r.a = u32x4{r.a.y, r.a.z, r.a.w, 0u};
@@ -128,88 +137,124 @@ __device__ __forceinline__ void move_down(Raw<bf16> &r, int by)
         r.a = u32x4{r.a.x >> 16 | r.a.y << 16, r.a.y >> 16 | r.a.z << 16, r.a.z >> 16 | r.a.w << 16, r.a.w >> 16};
 }
 
-template <class T, class I>
-__device__ __forceinline__ void settle(Raw<T> &r, I c, I n)
+template <class T, int N, class I>
+__device__ __forceinline__ void settle(Raw<T, N> &r, I c, I n)
 {
     const I left = n - c;
-    if (left < 8 && left > 0 && c > 0) move_down(r, 8 - (int)left);
+    if (left < N && left > 0 && c > 0) move_down(r, N - (int)left);
 }
 
-__device__ __forceinline__ void unpack(const Raw<float> &r, float (&v)[8])
+template <int N>
+__device__ __forceinline__ void unpack(const Raw<float, N> &r, float *v)
 {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t lo = r.a[k], hi = r.b[k];      // a bit cast of the vector's element itself takes element 0 (hipcc 7.2)
-        v[k] = __builtin_bit_cast(float, lo);
-        v[4 + k] = __builtin_bit_cast(float, hi);
+    for (int k = 0; k < N; ++k) {
+        const uint32_t w = r.a[k];          // a bit cast of the vector's element itself takes element 0 (hipcc 7.2)
+        v[k] = __builtin_bit_cast(float, w);
     }
 }
 
-__device__ __forceinline__ void unpack(const Raw<bf16> &r, float (&v)[8])
+template <int N>
+__device__ __forceinline__ void unpack(const Raw<bf16, N> &r, float *v)
 {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 2; ++k) {
         const uint32_t w = r.a[k];
         v[2 * k] = __builtin_bit_cast(float, w << 16);
         v[2 * k + 1] = __builtin_bit_cast(float, w & 0xFFFF0000u);
     }
 }
 
-template <bool NT = false, class T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8])
+template <int N>
+__device__ __forceinline__ Raw<float, N> pack(const float *, const float *v)
 {
-    unpack(raw8<NT>(p), v);
-}
-
-template <bool NT = false>
-__device__ __forceinline__ void store8(float *p, const float (&v)[8])
-{
-    u32x4 a, b;
+    Raw<float, N> r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        a[k] = __builtin_bit_cast(uint32_t, v[k]);
-        b[k] = __builtin_bit_cast(uint32_t, v[4 + k]);
-    }
-    u32x4_a4 *q = (u32x4_a4 *)p;
-    if (NT) {
-        __builtin_nontemporal_store(a, q);
-        __builtin_nontemporal_store(b, q + 1);
-    } else {
-        q[0] = a;
-        q[1] = b;
-    }
+    for (int k = 0; k < N; ++k) r.a[k] = __builtin_bit_cast(uint32_t, v[k]);
+    return r;
 }
 
-template <bool NT = false>
-__device__ __forceinline__ void store8(bf16 *p, const float (&v)[8])
+template <int N>
+__device__ __forceinline__ Raw<bf16, N> pack(const bf16 *, const float *v)
 {
-    u32x4 a;
+    Raw<bf16, N> r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = two_bf16(v[2 * k], v[2 * k + 1]);
-    u32x4_a2 *q = (u32x4_a2 *)p;
-    if (NT) __builtin_nontemporal_store(a, q);
-    else *q = a;
+    for (int k = 0; k < N / 2; ++k) r.a[k] = two_bf16(v[2 * k], v[2 * k + 1]);
+    return r;
 }
 
-template <bool NT = false, class T, class I>
-__device__ __forceinline__ void load_at(const T *row, I c, I n, float (&v)[8])
-{
-    Raw<T> r = raw_at<NT>(row, c, n);
-    settle(r, c, n);
-    unpack(r, v);
-}
-
-template <bool NT = false, class T, class I>
-__device__ __forceinline__ void store_at(T *row, I c, I n, const float (&v)[8])
+template <int N, bool NT = false, class T, class I>
+__device__ __forceinline__ void store_at(T *row, I c, I n, const float *v)
 {
     const I left = n - c;
-    T *p = row + c;
-    if (left >= 8) {
-        store8<NT>(p, v);
+    if (left >= N) {
+        typedef typename Raw<T, N>::Wide *To;
+        const auto w = pack<N>(row, v).a;
+        if constexpr (NT) __builtin_nontemporal_store(w, (To)(row + c));
+        else *(To)(row + c) = w;
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < left) put(p + k, v[k]);
+        for (int k = 0; k < N; ++k)
+            if (k < left) put(row + c + k, v[k]);
+    }
+}
+
+// Eight channels a lane of a row of n, those of all lanes a block of 8 * lanes that starts at `base`.  PAIR false (bf16 throughout): eight
+// side by side, one access.  PAIR true (an fp32 array takes part): four from either half of the block, so that the accesses of both types lie side
+// by side over the lanes.
+template <bool PAIR>
+__device__ __forceinline__ int channel_of(int base, int lane, int lanes, int k)
+{
+    return PAIR ? base + (k < 4 ? 0 : 4 * lanes - 4) + 4 * lane + k : base + 8 * lane + k;
+}
+
+template <class T, bool PAIR>
+struct Eight {
+    Raw<T, PAIR ? 4 : 8> a;
+    Raw<T, PAIR ? 4 : 8> b;         // PAIR only
+};
+
+template <bool PAIR, bool NT = false, class T>
+__device__ __forceinline__ Eight<T, PAIR> eight_at(const T *row, int base, int lane, int lanes, int n)
+{
+    Eight<T, PAIR> e;
+    if constexpr (PAIR) {
+        e.a = raw_at<4, NT>(row, base + 4 * lane, n);
+        e.b = raw_at<4, NT>(row, base + 4 * lanes + 4 * lane, n);
+    } else {
+        e.a = raw_at<8, NT>(row, base + 8 * lane, n);
+    }
+    return e;
+}
+
+template <bool PAIR, class T>
+__device__ __forceinline__ void unpack_at(Eight<T, PAIR> e, int base, int lane, int lanes, int n, float (&v)[8])
+{
+    if constexpr (PAIR) {
+        settle(e.a, base + 4 * lane, n);
+        settle(e.b, base + 4 * lanes + 4 * lane, n);
+        unpack(e.a, v);
+        unpack(e.b, v + 4);
+    } else {
+        settle(e.a, base + 8 * lane, n);
+        unpack(e.a, v);
+    }
+}
+
+template <bool PAIR, class T>
+__device__ __forceinline__ void load_eight(const T *row, int base, int lane, int lanes, int n, float (&v)[8])
+{
+    unpack_at<PAIR>(eight_at<PAIR>(row, base, lane, lanes, n), base, lane, lanes, n, v);
+}
+
+template <bool PAIR, bool NT = false, class T>
+__device__ __forceinline__ void store_eight(T *row, int base, int lane, int lanes, int n, const float (&v)[8])
+{
+    if constexpr (PAIR) {
+        store_at<4, NT>(row, base + 4 * lane, n, v);
+        store_at<4, NT>(row, base + 4 * lanes + 4 * lane, n, v + 4);
+    } else {
+        store_at<8, NT>(row, base + 8 * lane, n, v);
     }
 }
 

@@ -23,18 +23,19 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(const int64_t *ids,
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = i / pieces;
     if (t >= T_) return;
-    const int c = (int)(i - t * pieces) * 8;
+    constexpr bool PAIR = is_float<T> || is_float<Y>;
+    const int lane = (int)(i - t * pieces);
     const int64_t id = ids[t];
     float v[8];
     if (id >= 0 && id < V) {
-        load_at(table + id * n, c, n, v);
+        load_eight<PAIR>(table + id * n, 0, lane, pieces, n, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= scale;
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 0.0f;
     }
-    store_at(y + t * n, c, n, v);
+    store_eight<PAIR>(y + t * n, 0, lane, pieces, n, v);
 }
 
 // ---- the sort -------------------------------------------------------------------------------
@@ -132,19 +133,18 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass 
 
 // ---- sums -----------------------------------------------------------------------------------
 
-// Adds eight channels of the rows first .. first + count - 1, `stride` floats apart, to t, one after the other, AHEAD of them in flight.
+// Adds a lane's eight channels of the rows first .. first + count - 1, `stride` floats apart, to t, one after the other, AHEAD of them in flight.
 template <int AHEAD>
-__device__ __forceinline__ void add_rows(const float *rows, int64_t stride, uint32_t first, uint32_t count, int n, int c, float (&t)[8])
+__device__ __forceinline__ void add_rows(const float *rows, int64_t stride, uint32_t first, uint32_t count, int n, int base, int lane, int lanes, float (&t)[8])
 {
     for (uint32_t i = 0; i < count; i += AHEAD) {
-        Raw<float> r[AHEAD];
+        Eight<float, true> r[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) r[k] = raw_at(rows + (int64_t)(first + i + k) * stride, c, i + k < count ? n : 0);
+        for (int k = 0; k < AHEAD; ++k) r[k] = eight_at<true>(rows + (int64_t)(first + i + k) * stride, base, lane, lanes, i + k < count ? n : 0);
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             float v[8];
-            settle(r[k], c, n);
-            unpack(r[k], v);
+            unpack_at<true>(r[k], base, lane, lanes, n, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) t[j] += v[j];
         }
@@ -184,7 +184,8 @@ struct SumCall {
 };
 
 // The first piece_blocks workgroups have the pieces, 256 / lanes each; the others 32 table rows each, which they zero where no token names them.
-template <class Y, class G>
+// WAVES: a row takes whole waves (64 lanes and more): ids and places of a piece are then in scalar registers.
+template <class Y, class G, bool WAVES>
 __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y *gy, G *gtable)
 {
     __shared__ uint32_t lds[4], here[kRows];
@@ -203,12 +204,14 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
         }
         __syncthreads();
         const float zeros[8] = {};
+        constexpr bool kPairZero = is_float<G>;
         for (int r = worker; r < kRows && first + r < a.V; r += 256 / lanes)
             if (!here[r])
-                for (int c = lane * 8; c < n; c += lanes * 8) store_at<true>(gtable + (first + r) * n, c, n, zeros);
+                for (int base = 0; base < n; base += lanes * 8) store_eight<kPairZero, true>(gtable + (first + r) * n, base, lane, lanes, n, zeros);
         return;
     }
-    const uint32_t p = blockIdx.x * (256 / lanes) + worker;
+    uint32_t p = blockIdx.x * (256 / lanes) + worker;
+    if (WAVES) p = __builtin_amdgcn_readfirstlane(p);
     if (p >= a.pieces) return;
     uint32_t key[kPiece], place[kPiece];
 #pragma unroll
@@ -222,21 +225,22 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
         }
     }
     const uint32_t V = (uint32_t)a.V;
+    // the fragments are fp32 whatever the rows are
+    constexpr bool PAIR = true;
     const bool from_before = p > 0 && a.keys[p * kPiece - 1] == key[0];
     const bool goes_on = (p + 1) * kPiece < a.T && a.keys[(p + 1) * kPiece] == key[kPiece - 1];
-    for (int c = lane * 8; c < n; c += lanes * 8) {
+    for (int base = 0; base < n; base += lanes * 8) {
         float t[8] = {};
         bool first_run = true;
 #pragma unroll
         for (int b = 0; b < kPiece; b += 8) {
-            Raw<Y> r[8];
+            Eight<Y, PAIR> r[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r[j] = raw_at(gy + (int64_t)place[b + j] * n, c, key[b + j] < V ? n : 0);
+            for (int j = 0; j < 8; ++j) r[j] = eight_at<PAIR>(gy + (int64_t)place[b + j] * n, base, lane, lanes, key[b + j] < V ? n : 0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float v[8];
-                settle(r[j], c, n);
-                unpack(r[j], v);
+                unpack_at<PAIR>(r[j], base, lane, lanes, n, v);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) t[k] += v[k];
                 const bool last = b + j == kPiece - 1;
@@ -244,11 +248,11 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
                     if (key[b + j] < V) {
                         const bool left = first_run && from_before, right = last && goes_on;
                         if (left || right) {
-                            store_at(a.fragments + ((int64_t)p * 2 + (first_run ? 0 : 1)) * n, c, n, t);
+                            store_eight<PAIR>(a.fragments + ((int64_t)p * 2 + (first_run ? 0 : 1)) * n, base, lane, lanes, n, t);
                         } else {
 #pragma unroll
                             for (int k = 0; k < 8; ++k) t[k] *= a.scale;
-                            store_at<true>(gtable + (int64_t)key[b + j] * n, c, n, t);
+                            store_eight<PAIR, true>(gtable + (int64_t)key[b + j] * n, base, lane, lanes, n, t);
                         }
                     }
 #pragma unroll
@@ -265,10 +269,10 @@ __global__ __launch_bounds__(256) void embedding_group_kernel(SumCall a)
 {
     const uint32_t q = blockIdx.x, width = kPiece * kPiece;
     if (a.keys[q * width] >= (uint32_t)a.V || a.keys[(q + 1) * width - 1] != a.keys[q * width]) return;
-    for (int c = threadIdx.x * 8; c < a.n; c += 256 * 8) {
+    for (int base = 0; base < a.n; base += 256 * 8) {
         float t[8] = {};
-        add_rows<8>(a.fragments + (int64_t)q * kPiece * 2 * a.n, 2ll * a.n, 0, kPiece, a.n, c, t);
-        store_at(a.groups + (int64_t)q * a.n, c, a.n, t);
+        add_rows<8>(a.fragments + (int64_t)q * kPiece * 2 * a.n, 2ll * a.n, 0, kPiece, a.n, base, threadIdx.x, 256, t);
+        store_eight<true>(a.groups + (int64_t)q * a.n, base, threadIdx.x, 256, a.n, t);
     }
 }
 
@@ -303,16 +307,15 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
     if (!a.groups || q1 <= q0) q0 = q1 = 0;
     const uint32_t cut0 = q1 > 0 ? q0 * kPiece : end, cut1 = q1 > 0 ? q1 * kPiece : end;
     const auto part = [&](uint32_t from, uint32_t count, int which) { return from + (uint32_t)((uint64_t)count * which / workers); };
-    for (int c0 = 0; c0 < n; c0 += lanes * 8) {
-        const int c = c0 + lane * 8;
+    for (int base = 0; base < n; base += lanes * 8) {
         float t[8] = {};
-        if (w == 0) add_rows<1>(a.fragments + ((int64_t)p * 2 + (whole ? 0 : 1)) * n, 0, 0, 1, n, c, t);
+        if (w == 0) add_rows<1>(a.fragments + ((int64_t)p * 2 + (whole ? 0 : 1)) * n, 0, 0, 1, n, base, lane, lanes, t);
         const uint32_t b0 = part(begin, cut0 - begin, w), b1 = part(begin, cut0 - begin, w + 1);
-        add_rows<8>(a.fragments, 2ll * n, b0, b1 - b0, n, c, t);
+        add_rows<8>(a.fragments, 2ll * n, b0, b1 - b0, n, base, lane, lanes, t);
         const uint32_t g0 = part(q0, q1 - q0, w), g1 = part(q0, q1 - q0, w + 1);
-        add_rows<8>(a.groups, n, g0, g1 - g0, n, c, t);
+        add_rows<8>(a.groups, n, g0, g1 - g0, n, base, lane, lanes, t);
         const uint32_t e0 = part(cut1, end - cut1, w), e1 = part(cut1, end - cut1, w + 1);
-        add_rows<8>(a.fragments, 2ll * n, e0, e1 - e0, n, c, t);
+        add_rows<8>(a.fragments, 2ll * n, e0, e1 - e0, n, base, lane, lanes, t);
         if (workers > 1) {
             __syncthreads();
 #pragma unroll
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
         if (w == 0) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) t[k] *= a.scale;
-            store_at(gtable + (int64_t)id * n, c, n, t);
+            store_eight<true>(gtable + (int64_t)id * n, base, lane, lanes, n, t);
         }
     }
 }
@@ -351,7 +354,7 @@ Layout layout_of(int64_t T, int64_t V, int n)
     per = per < 1 ? kSortThreads : div_up(per, (int64_t)kSortThreads) * kSortThreads;
     l.per_block = (uint32_t)per;
     l.blocks = (int)div_up(T, per);
-    l.second = T >= 16 * kPiece * kPiece;
+    l.second = T >= 128 * kPiece * kPiece;
     size_t at = 0;
     const auto take = [&at](size_t bytes) {
         const size_t here = at;
@@ -409,7 +412,9 @@ hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint3
     a.scale = scale;
     {
         prof::Timed timed("embedding_pieces", st);
-        embedding_piece_kernel<Y, G><<<a.piece_blocks + (unsigned)div_up(V, (int64_t)kRows), 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
+        const unsigned blocks = a.piece_blocks + (unsigned)div_up(V, (int64_t)kRows);
+        if (a.lanes >= 64) embedding_piece_kernel<Y, G, true><<<blocks, 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
+        else embedding_piece_kernel<Y, G, false><<<blocks, 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || T <= kPiece) return e;

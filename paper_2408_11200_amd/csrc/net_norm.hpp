@@ -32,14 +32,47 @@ constexpr int forward_threads() { return TPR > 64 ? TPR : 256; }
 template <int TPR>
 constexpr int backward_threads() { return TPR > 512 ? TPR : 512; }
 
-template <int P>
+// Parameters and their sums are fp32 whatever the rows are: where those have eight channels side by side a lane, two accesses
+template <bool PAIR>
+__device__ __forceinline__ void load_param_eight(const float *w, int base, int lane, int lanes, int n, float (&v)[8])
+{
+    if constexpr (PAIR) {
+        load_eight<true>(w, base, lane, lanes, n, v);
+    } else {
+        const int c = base + 8 * lane;
+        Raw<float, 4> a = raw_at<4>(w, c, n), b = raw_at<4>(w, c + 4, n);
+        settle(a, c, n);
+        settle(b, c + 4, n);
+        unpack(a, v);
+        unpack(b, v + 4);
+    }
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void store_param_eight(float *w, int base, int lane, int lanes, int n, const float (&v)[8])
+{
+    if constexpr (PAIR) {
+        store_eight<true>(w, base, lane, lanes, n, v);
+    } else {
+        store_at<4>(w, base + 8 * lane, n, v);
+        store_at<4>(w, base + 8 * lane + 4, n, v + 4);
+    }
+}
+
+template <int P, bool PAIR>
+__device__ __forceinline__ void store_param(float *w, int lane, int tpr, int n, const float (&v)[P][8])
+{
+#pragma unroll
+    for (int q = 0; q < P; ++q) store_param_eight<PAIR>(w, q * tpr * 8, lane, tpr, n, v[q]);
+}
+
+template <int P, bool PAIR>
 __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, int n, float none, float (&v)[P][8])
 {
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-        const int c = (q * tpr + lane) * 8;
         if (w) {
-            load_at(w, c, n, v[q]);
+            load_param_eight<PAIR>(w, q * tpr * 8, lane, tpr, n, v[q]);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[q][k] = none;
@@ -49,69 +82,77 @@ __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, in
 
 // Past the caches where it is written once and read by other launches: of 16384 x 4096 bf16 the backward pass took 151 us with such stores and
 // 171 without, of 16384 x 512 fp32 the forward pass 25 and 30.  (Such loads cost more than they gave: x and f are read by both passes.)
-template <int P, class T, bool NT = true>
+template <int P, bool PAIR, class T>
 __device__ __forceinline__ void store_row(void *base, int64_t row, int lane, int tpr, int n, const float (&v)[P][8])
 {
 #pragma unroll
-    for (int q = 0; q < P; ++q) {
-        const int c = (q * tpr + lane) * 8;
-        store_at<NT>((T *)base + row * n, c, n, v[q]);
-    }
+    for (int q = 0; q < P; ++q) store_eight<PAIR, true>((T *)base + row * n, q * tpr * 8, lane, tpr, n, v[q]);
 }
 
 // v becomes norm(v) (0 in channels past the row's end); mean and 1/sigma.  The variance is that of the centred values: the mean of the
-// squares less the squared mean would lose all digits where the mean is large.
-template <int TPR, int P, bool LAYER>
+// squares less the squared mean would lose all digits where the mean is large.  What the mean's own rounding left in the centred values
+// is their mean, from the same sums as the variance.
+template <int TPR, int P, bool PAIR, bool LAYER>
 __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int n, float inv_n, float eps, RowSum<TPR> &total, float &mean, float &r)
 {
     mean = 0.0f;
+    float s[2] = {0.0f, 0.0f};
     if constexpr (LAYER) {
-        float s = 0.0f;
 #pragma unroll
         for (int q = 0; q < P; ++q)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += v[q][k];
-        mean = total(s) * inv_n;
-#pragma unroll
-        for (int q = 0; q < P; ++q)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[q][k] = (q * TPR + lane) * 8 + k < n ? v[q][k] - mean : 0.0f;
+            for (int k = 0; k < 8; ++k) s[1] += v[q][k];
+        mean = total(s[1]) * inv_n;
+        s[1] = 0.0f;
     }
-    float s = 0.0f;
 #pragma unroll
     for (int q = 0; q < P; ++q)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += v[q][k] * v[q][k];
-    r = 1.0f / sqrtf(total(s) * inv_n + eps);
+        for (int k = 0; k < 8; ++k) {
+            if (LAYER) {
+                v[q][k] = channel_of<PAIR>(q * TPR * 8, lane, TPR, k) < n ? v[q][k] - mean : 0.0f;
+                s[1] += v[q][k];
+            }
+            s[0] += v[q][k] * v[q][k];
+        }
+    if constexpr (LAYER) {
+        total.sum(s);
+    } else {
+        s[0] = total(s[0]);
+    }
+    const float rest = s[1] * inv_n;
+    r = 1.0f / sqrtf((LAYER ? fmaxf(s[0] * inv_n - rest * rest, 0.0f) : s[0] * inv_n) + eps);
+    mean += rest;
 #pragma unroll
     for (int q = 0; q < P; ++q)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[q][k] *= r;
+        for (int k = 0; k < 8; ++k) v[q][k] = (!LAYER || channel_of<PAIR>(q * TPR * 8, lane, TPR, k) < n) ? (v[q][k] - rest) * r : 0.0f;
 }
 
 template <class X, class F, int TPR, int P, bool LAYER>
 __global__ __launch_bounds__(forward_threads<TPR>()) void norm_forward_kernel(NormCall a)
 {
     constexpr int kWorkers = forward_threads<TPR>() / TPR;
+    constexpr bool PAIR = is_float<X> || is_float<F>;
     __shared__ float slots[RowSum<TPR>::kSlots];
     RowSum<TPR> total{slots};
     const int lane = threadIdx.x % TPR, n = a.n;
     const int64_t step = (int64_t)gridDim.x * kWorkers;
     float w_post[P][8], b_post[P][8], gate[P][8], w_pre[P][8], b_pre[P][8];
-    load_param<P>(a.p.w_pre, lane, TPR, n, 1.0f, w_pre);
-    load_param<P>(a.p.b_pre, lane, TPR, n, 0.0f, b_pre);
-    load_param<P>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
-    load_param<P>(a.f ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
-    load_param<P>(a.f && !a.gate_rows ? a.p.gate : nullptr, lane, TPR, n, 1.0f, gate);
+    load_param<P, PAIR>(a.p.w_pre, lane, TPR, n, 1.0f, w_pre);
+    load_param<P, PAIR>(a.p.b_pre, lane, TPR, n, 0.0f, b_pre);
+    load_param<P, PAIR>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
+    load_param<P, PAIR>(a.f ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
+    load_param<P, PAIR>(a.f && !a.gate_rows ? a.p.gate : nullptr, lane, TPR, n, 1.0f, gate);
     int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
-    Raw<X> next_x[P];
-    Raw<F> next_f[P];
+    Eight<X, PAIR> next_x[P];
+    Eight<F, PAIR> next_f[P];
     const auto read_ahead = [&](int64_t r) {
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const int c = (q * TPR + lane) * 8, m = r < a.B ? n : 0;
-            next_x[q] = raw_at((const X *)a.x + r * n, c, m);
-            next_f[q] = raw_at((const F *)a.f + r * n, c, a.f ? m : 0);
+            const int m = r < a.B ? n : 0;
+            next_x[q] = eight_at<PAIR>((const X *)a.x + r * n, q * TPR * 8, lane, TPR, m);
+            next_f[q] = eight_at<PAIR>((const F *)a.f + r * n, q * TPR * 8, lane, TPR, a.f ? m : 0);
         }
     };
     read_ahead(row);
@@ -119,29 +160,26 @@ __global__ __launch_bounds__(forward_threads<TPR>()) void norm_forward_kernel(No
         float v[P][8], u[P][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const int c = (q * TPR + lane) * 8;
-            settle(next_x[q], c, n);
-            settle(next_f[q], c, n);
-            unpack(next_x[q], v[q]);
-            unpack(next_f[q], u[q]);
+            unpack_at<PAIR>(next_x[q], q * TPR * 8, lane, TPR, n, v[q]);
+            unpack_at<PAIR>(next_f[q], q * TPR * 8, lane, TPR, n, u[q]);
         }
         read_ahead(row + step);
         if (a.f) {
-            if (a.gate_rows && a.p.gate) load_param<P>(a.p.gate + row / a.gate_rows * n, lane, TPR, n, 1.0f, gate);
-            normalise<TPR, P, LAYER>(u, lane, n, a.inv_n, a.eps, total, st[0], st[1]);
+            if (a.gate_rows && a.p.gate) load_param<P, PAIR>(a.p.gate + row / a.gate_rows * n, lane, TPR, n, 1.0f, gate);
+            normalise<TPR, P, PAIR, LAYER>(u, lane, n, a.inv_n, a.eps, total, st[0], st[1]);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[q][k] = a.residual_scale * v[q][k] + gate[q][k] * (u[q][k] * w_post[q][k] + b_post[q][k]);
-            store_row<P, X>(a.x_out, row, lane, TPR, n, v);
+            store_row<P, PAIR, X>(a.x_out, row, lane, TPR, n, v);
         }
         if (a.h) {
-            normalise<TPR, P, LAYER>(v, lane, n, a.inv_n, a.eps, total, st[2], st[3]);
+            normalise<TPR, P, PAIR, LAYER>(v, lane, n, a.inv_n, a.eps, total, st[2], st[3]);
 #pragma unroll
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[q][k] = v[q][k] * w_pre[q][k] + b_pre[q][k];
-            store_row<P, F>(a.h, row, lane, TPR, n, v);
+            store_row<P, PAIR, F>(a.h, row, lane, TPR, n, v);
         }
         if (a.stats && lane == 0) {
 #pragma unroll
@@ -177,22 +215,25 @@ __device__ __forceinline__ void norm_back(float (&q)[P][8], const float (&vhat)[
 // A worker's rows of the backward pass as they lie in memory, read while the rows before are worked on
 template <class X, class F, int P>
 struct RowsAhead {
-    Raw<X> x[P], gx_out[P];
-    Raw<F> f[P], gh[P];
+    static constexpr bool PAIR = is_float<X> || is_float<F>;
+    Eight<X, PAIR> x[P], gx_out[P];
+    Eight<F, PAIR> f[P], gh[P];
     float st[4];
 };
 
 template <class X, class F, int TPR, int P>
 __device__ __forceinline__ void read_ahead(RowsAhead<X, F, P> &r, const NormCall &a, int64_t row, bool live, int lane)
 {
+    constexpr bool PAIR = RowsAhead<X, F, P>::PAIR;
+    const int n = live ? a.n : 0;
+    const int64_t at = row * a.n;
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-        const int c = (q * TPR + lane) * 8, n = live ? a.n : 0;
-        const int64_t at = row * a.n;
-        r.x[q] = raw_at((const X *)a.x + at, c, n);
-        r.f[q] = raw_at((const F *)a.f + at, c, a.f ? n : 0);
-        r.gx_out[q] = raw_at((const X *)a.gx_out + at, c, a.gx_out ? n : 0);
-        r.gh[q] = raw_at((const F *)a.gh + at, c, a.gh ? n : 0);
+        const int base = q * TPR * 8;
+        r.x[q] = eight_at<PAIR>((const X *)a.x + at, base, lane, TPR, n);
+        r.f[q] = eight_at<PAIR>((const F *)a.f + at, base, lane, TPR, a.f ? n : 0);
+        r.gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + at, base, lane, TPR, a.gx_out ? n : 0);
+        r.gh[q] = eight_at<PAIR>((const F *)a.gh + at, base, lane, TPR, a.gh ? n : 0);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) r.st[i] = live ? a.stats[row * 4 + i] : 0.0f;
@@ -208,6 +249,7 @@ template <class X, class F, int TPR, int P, bool LAYER, bool WHOLE, bool BIAS>
 __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(NormCall a)
 {
     constexpr int NT = backward_threads<TPR>(), kWorkers = NT / TPR;
+    constexpr bool PAIR = is_float<X> || is_float<F>;
     __shared__ float slots[RowSum<TPR>::kSlots * (TPR > 64 ? kWorkers : 1)];
     constexpr int kJoin = TPR < 64 ? NT / 64 : kWorkers;       // workers of one wave are joined by shuffles first
     __shared__ float joined[kWorkers > 1 ? kJoin * TPR * 8 : 1];
@@ -230,10 +272,10 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
 
     // gate * w_post and gate * b_post; gate and the other two by themselves where the gate changes on the way
     float w_pre[P][8], w_post[P][8], b_post[P][8], gate[P][8];
-    load_param<P>(a.p.w_pre, lane, TPR, n, 1.0f, w_pre);
-    load_param<P>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
-    load_param<P>(a.f && BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
-    load_param<P>(gate_row, lane, TPR, n, 1.0f, gate);
+    load_param<P, PAIR>(a.p.w_pre, lane, TPR, n, 1.0f, w_pre);
+    load_param<P, PAIR>(a.f ? a.p.w_post : nullptr, lane, TPR, n, 1.0f, w_post);
+    load_param<P, PAIR>(a.f && BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
+    load_param<P, PAIR>(gate_row, lane, TPR, n, 1.0f, gate);
     if (!WHOLE)
 #pragma unroll
         for (int q = 0; q < P; ++q)
@@ -276,17 +318,12 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
         // out of the registers the next row is read into
         const float mean_f = next.st[0], r_f = next.st[1], mean_x = next.st[2], r_x = next.st[3];
         float v[P][8], fhat[P][8], d[P][8], g[P][8];
-        Raw<X> gx_out[P];
+        Eight<X, PAIR> gx_out[P];
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            const int c = (q * TPR + lane) * 8;
-            settle(next.x[q], c, n);
-            settle(next.f[q], c, n);
-            settle(next.gh[q], c, n);
-            settle(next.gx_out[q], c, n);
-            unpack(next.x[q], v[q]);
-            unpack(next.f[q], fhat[q]);
-            unpack(next.gh[q], g[q]);
+            unpack_at<PAIR>(next.x[q], q * TPR * 8, lane, TPR, n, v[q]);
+            unpack_at<PAIR>(next.f[q], q * TPR * 8, lane, TPR, n, fhat[q]);
+            unpack_at<PAIR>(next.gh[q], q * TPR * 8, lane, TPR, n, g[q]);
             gx_out[q] = next.gx_out[q];
         }
         read_ahead<X, F, TPR, P>(next, a, row + 1, row + 1 < end, lane);
@@ -297,7 +334,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
+                    const bool in = !LAYER || channel_of<PAIR>(q * TPR * 8, lane, TPR, k) < n;
                     fhat[q][k] = in ? (fhat[q][k] - mean_f) * r_f : 0.0f;
                     const float u = fhat[q][k] * w_post[q][k] + b_post[q][k];
                     v[q][k] = a.residual_scale * v[q][k] + (WHOLE ? gate[q][k] * u : u);
@@ -309,7 +346,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
+                    const bool in = !LAYER || channel_of<PAIR>(q * TPR * 8, lane, TPR, k) < n;
                     v[q][k] = in ? (v[q][k] - mean_x) * r_x : 0.0f;
                     pre1[q][k] += g[q][k] * v[q][k];
                     if (BIAS) pre0[q][k] += g[q][k];
@@ -319,7 +356,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
         }
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-            unpack(gx_out[q], d[q]);
+            unpack_at<PAIR>(gx_out[q], q * TPR * 8, lane, TPR, n, d[q]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) d[q][k] += g[q][k];        // without gh: zeros
         }
@@ -329,7 +366,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) g[q][k] = scale * d[q][k];
-            store_row<P, X>(a.gx, row, lane, TPR, n, g);
+            store_row<P, PAIR, X>(a.gx, row, lane, TPR, n, g);
         }
         if (a.f) {
             fetch(1, w_post);
@@ -338,7 +375,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             for (int q = 0; q < P; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const bool in = !LAYER || (q * TPR + lane) * 8 + k < n;
+                    const bool in = !LAYER || channel_of<PAIR>(q * TPR * 8, lane, TPR, k) < n;
                     float gu = d[q][k];
                     if (WHOLE) {
                         gates[q][k] += gu * (fhat[q][k] * w_post[q][k] + b_post[q][k]);
@@ -350,25 +387,25 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 }
             if (a.gf) {
                 norm_back<TPR, P, LAYER>(d, fhat, r_f, a.inv_n, total);
-                if (live) store_row<P, F>(a.gf, row, lane, TPR, n, d);
+                if (live) store_row<P, PAIR, F>(a.gf, row, lane, TPR, n, d);
             }
             if (WHOLE && live && (row + 1 == end || (row + 1) % a.gate_rows == 0)) {
-                if (a.ggate) store_row<P, float, false>(a.ggate, group, lane, TPR, n, gates);
+                if (a.ggate) store_param<P, PAIR>(a.ggate + group * n, lane, TPR, n, gates);
                 ++group;
 #pragma unroll
                 for (int q = 0; q < P; ++q)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) gates[q][k] = 0.0f;
-                if (a.p.gate && row + 1 < end) load_param<P>(a.p.gate + group * n, lane, TPR, n, 1.0f, gate);
+                if (a.p.gate && row + 1 < end) load_param<P, PAIR>(a.p.gate + group * n, lane, TPR, n, 1.0f, gate);
             }
         }
     }
     if (!a.part) return;
     if (a.parts && a.f) {
         // a part of a group: its share of the gate's gradient, and the gate's factor of the others
-        load_param<P>(a.p.w_post, lane, TPR, n, 1.0f, w_post);
-        load_param<P>(BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
-        load_param<P>(gate_row, lane, TPR, n, 1.0f, gate);
+        load_param<P, PAIR>(a.p.w_post, lane, TPR, n, 1.0f, w_post);
+        load_param<P, PAIR>(BIAS ? a.p.b_post : nullptr, lane, TPR, n, 0.0f, b_post);
+        load_param<P, PAIR>(gate_row, lane, TPR, n, 1.0f, gate);
 #pragma unroll
         for (int q = 0; q < P; ++q)
 #pragma unroll
@@ -377,7 +414,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 post1[q][k] *= gate[q][k];
                 post0[q][k] *= gate[q][k];
             }
-        if (a.ggate && group * a.gate_rows < a.B) store_row<P, float, false>(a.gate_part, worker, lane, TPR, n, gates);
+        if (a.ggate && group * a.gate_rows < a.B) store_param<P, PAIR>(a.gate_part + worker * n, lane, TPR, n, gates);
     }
     const auto leave = [&](float (&v)[P][8], int which) {
         float *to = a.part + ((int64_t)blockIdx.x * 4 + which) * n;
@@ -399,10 +436,10 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 for (int w = 0; w < kJoin; ++w)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) t[k] += joined[(w * 8 + k) * TPR + lane];
-                store_at(to, lane * 8, n, t);
+                store_param_eight<PAIR>(to, 0, lane, TPR, n, t);
             }
         } else {
-            store_row<P, float, false>(to, 0, lane, TPR, n, v);
+            store_param<P, PAIR>(to, lane, TPR, n, v);
         }
     };
     if (a.gh) {
