@@ -274,21 +274,13 @@ __device__ __forceinline__ f32x2 both_halves(float v)
     return f32x2{v, __builtin_bit_cast(float, o)};
 }
 
-// the sum, or the largest value, over each group of W lanes, the same bits in all of them
+// the sum over each group of W lanes, the same bits in all of them
 template <int W>
 __device__ __forceinline__ float lane_sum(float v)
 {
     if constexpr (W > 2) v = lane_sum<W / 2>(v);
     const f32x2 t = both_halves<W>(v);
     return t.x + t.y;
-}
-
-template <int W>
-__device__ __forceinline__ float lane_max(float v)
-{
-    if constexpr (W > 2) v = lane_max<W / 2>(v);
-    const f32x2 t = both_halves<W>(v);
-    return fmaxf(t.x, t.y);
 }
 
 // Sums of N values over the TPR lanes that share a row: within a wave, or over the TPR / 64 waves of the workgroup through LDS, with one

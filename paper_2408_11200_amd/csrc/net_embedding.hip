@@ -45,6 +45,7 @@ struct SortPass {
     const uint32_t *key_in, *place_in;
     uint32_t *key_out, *place_out;
     uint32_t *counts;                   // [blocks][digits]
+    uint32_t *starts;                   // set to 0 by the first pass
     int64_t V;
     uint32_t T, per_block;
     int blocks, shift, bits;
@@ -67,6 +68,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(SortPass 
     for (uint32_t i = from + threadIdx.x; i < to; i += kSortThreads) atomicAdd(&count[key_at(a, i) >> a.shift & (digits - 1)], 1u);
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.counts[blockIdx.x * digits + d] = count[d];
+    if (a.ids && blockIdx.x == 0 && threadIdx.x == 0) *a.starts = 0;
 }
 
 __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass a)
@@ -176,6 +178,7 @@ struct SumCall {
     const uint32_t *keys, *places;
     float *fragments;       // [pieces][2][n]: of the run a piece begins with (all of the piece, or as far as the run goes), and of the one it ends with
     float *groups;          // [pieces / 16][n]: sixteen pieces of one id; null: too few entries for that
+    uint32_t *starts;       // [0]: how many runs leave the piece they start in; then those pieces, in any order
     uint32_t T, pieces;     // keys and places are readable up to whole pieces
     int64_t V;
     int n, lanes;
@@ -225,10 +228,10 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
         }
     }
     const uint32_t V = (uint32_t)a.V;
-    // the fragments are fp32 whatever the rows are
-    constexpr bool PAIR = true;
+    constexpr bool PAIR = is_float<Y> || is_float<G>;
     const bool from_before = p > 0 && a.keys[p * kPiece - 1] == key[0];
     const bool goes_on = (p + 1) * kPiece < a.T && a.keys[(p + 1) * kPiece] == key[kPiece - 1];
+    if (lane == 0 && goes_on && key[kPiece - 1] < V && !(from_before && key[0] == key[kPiece - 1])) a.starts[1 + atomicAdd(a.starts, 1u)] = p;
     for (int base = 0; base < n; base += lanes * 8) {
         float t[8] = {};
         bool first_run = true;
@@ -248,7 +251,13 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
                     if (key[b + j] < V) {
                         const bool left = first_run && from_before, right = last && goes_on;
                         if (left || right) {
-                            store_eight<PAIR>(a.fragments + ((int64_t)p * 2 + (first_run ? 0 : 1)) * n, base, lane, lanes, n, t);
+                            float *to = a.fragments + ((int64_t)p * 2 + (first_run ? 0 : 1)) * n;
+                            if constexpr (PAIR) {
+                                store_eight<true>(to, base, lane, lanes, n, t);
+                            } else {
+                                store_at<4>(to, base + 8 * lane, n, t);
+                                store_at<4>(to, base + 8 * lane + 4, n, t + 4);
+                            }
                         } else {
 #pragma unroll
                             for (int k = 0; k < 8; ++k) t[k] *= a.scale;
@@ -276,17 +285,13 @@ __global__ __launch_bounds__(256) void embedding_group_kernel(SumCall a)
     }
 }
 
-// A workgroup for each piece that a run starts in and leaves: the run's fragments, shared among the workgroup's workers.
 template <class G>
-__global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtable)
+__device__ __forceinline__ void join_run(const SumCall &a, G *gtable, uint32_t p)
 {
     __shared__ float lds[256 * 8];
     __shared__ uint32_t votes[4];
-    const uint32_t p = blockIdx.x;
     const uint32_t id = a.keys[p * kPiece + kPiece - 1];
-    if (id >= (uint32_t)a.V || (p + 1) * kPiece >= a.T || a.keys[(p + 1) * kPiece] != id) return;
     const bool whole = a.keys[p * kPiece] == id;
-    if (whole && p > 0 && a.keys[p * kPiece - 1] == id) return;
     // pieces behind this one that begin with the id
     uint32_t more = 0;
     for (;;) {
@@ -299,7 +304,8 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
         more += all;
         if (all < 256) break;
     }
-    const int n = a.n, lanes = a.lanes, workers = 256 / lanes, w = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    // rows wider than a wave's 512 channels are shared by workgroups of as many workers
+    const int n = a.n, lanes = a.lanes < 64 ? a.lanes : 64, workers = 256 / lanes, w = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     // pieces p + 1 .. end - 1; the groups q0 .. q1 - 1 lie wholly among those that hold nothing but the id
     const uint32_t begin = p + 1, end = begin + more;
     const uint64_t full_end = (uint64_t)end * kPiece <= a.T && a.keys[(uint64_t)end * kPiece - 1] == id ? end : end - 1;
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
     if (!a.groups || q1 <= q0) q0 = q1 = 0;
     const uint32_t cut0 = q1 > 0 ? q0 * kPiece : end, cut1 = q1 > 0 ? q1 * kPiece : end;
     const auto part = [&](uint32_t from, uint32_t count, int which) { return from + (uint32_t)((uint64_t)count * which / workers); };
-    for (int base = 0; base < n; base += lanes * 8) {
+    for (int base = blockIdx.y * lanes * 8; base < n; base += gridDim.y * lanes * 8) {
         float t[8] = {};
         if (w == 0) add_rows<1>(a.fragments + ((int64_t)p * 2 + (whole ? 0 : 1)) * n, 0, 0, 1, n, base, lane, lanes, t);
         const uint32_t b0 = part(begin, cut0 - begin, w), b1 = part(begin, cut0 - begin, w + 1);
@@ -334,12 +340,20 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
     }
 }
 
+// The runs that leave the piece they start in, a workgroup each: its workers share the run's fragments.
+template <class G>
+__global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtable)
+{
+    const uint32_t runs = a.starts[0];
+    for (uint32_t i = blockIdx.x; i < runs; i += gridDim.x) join_run(a, gtable, a.starts[1 + i]);
+}
+
 // ---- workspace ------------------------------------------------------------------------------
 
 struct Layout {
     int passes, bits, blocks;
     uint32_t per_block;
-    size_t counts, keys[2], places[2], fragments, groups, bytes;
+    size_t counts, starts, keys[2], places[2], fragments, groups, bytes;
     bool second;
 };
 
@@ -362,6 +376,7 @@ Layout layout_of(int64_t T, int64_t V, int n)
         return here;
     };
     l.counts = take((size_t)l.blocks * ((size_t)4 << l.bits));
+    l.starts = take(((size_t)div_up(T, (int64_t)kPiece) + 1) * 4);
     for (int i = 0; i < 2; ++i) {
         l.keys[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
         l.places[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
@@ -403,6 +418,7 @@ hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint3
     a.places = places;
     a.fragments = (float *)(ws + l.fragments);
     a.groups = l.second ? (float *)(ws + l.groups) : nullptr;
+    a.starts = (uint32_t *)(ws + l.starts);
     a.T = (uint32_t)T;
     a.pieces = (uint32_t)div_up(T, (int64_t)kPiece);
     a.V = V;
@@ -425,7 +441,7 @@ hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint3
         if (e != hipSuccess) return e;
     }
     prof::Timed timed("embedding_join", st);
-    embedding_join_kernel<G><<<a.pieces - 1, 256, 0, st>>>(a, (G *)gtable);
+    embedding_join_kernel<G><<<dim3(a.pieces < 1024 ? a.pieces : 1024, (unsigned)div_up(n, 512)), 256, 0, st>>>(a, (G *)gtable);
     return hipGetLastError();
 }
 
@@ -475,6 +491,7 @@ extern "C" int kan_embedding_backward(int64_t T, int64_t V, int32_t n, const int
         a.key_out = (uint32_t *)(at + l.keys[1 - from]);
         a.place_out = (uint32_t *)(at + l.places[1 - from]);
         a.counts = (uint32_t *)(at + l.counts);
+        a.starts = (uint32_t *)(at + l.starts);
         a.V = V;
         a.T = (uint32_t)T;
         a.per_block = l.per_block;

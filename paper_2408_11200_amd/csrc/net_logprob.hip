@@ -7,9 +7,9 @@
 // of what little the others add (one multiply-add with a rounded reference would be an instruction less, and lose them).
 // Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.
 //
-// The most likely tokens come out of the same read: a thread's largest logit with its place is the best of its pieces, so the top ones
-// of the row all lie with the `top` threads whose bests are the largest.  Those threads' pieces are read again (from L2), and what is
-// not below the last of these bests is sorted into a list that a wave holds one entry a lane.
+// The most likely tokens come out of the same read: a thread's largest logit is the best of its pieces, so the top ones of the row all lie with
+// the `top` threads whose bests are the largest (and those that tie with the last).  These threads' pieces are read again, from L2, and the
+// logits that reach the last of the bests, hardly more than `top`, are put in order by counting for each how many are above it.
 #include "net_device.hpp"
 
 namespace kannet {
@@ -18,6 +18,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kFar = -200.0f;          // 2^-200 is zero in 32 bits: what a term further down adds to the second sum
+
+struct Sums {
+    float m, s, t;          // largest logit (at least the lowest finite value), sum of 2^y, sum of 2^y y
+};
 
 struct LogprobCall {
     const void *logits;
@@ -31,10 +35,10 @@ struct LogprobCall {
     float *top_logp;
     const float *g_logp, *g_entropy;
     void *glogits;
-};
-
-struct Sums {
-    float m, s, t;          // largest logit (at least the lowest finite value), sum of 2^y, sum of 2^y y
+    int parts;              // of a row, in the forward pass
+    uint32_t part_pieces;   // pieces of 16 bytes of a part
+    Sums *part_sums;        // [R][parts]
+    uint64_t *part_keys;    // [R][parts][top]
 };
 
 __device__ __forceinline__ void rescale(Sums &a, float m, float scale)
@@ -87,40 +91,129 @@ __device__ __forceinline__ float logit_of(uint64_t key)
     return __builtin_bit_cast(float, (b >> 31) ? b & 0x7FFFFFFFu : ~b);
 }
 
-__device__ __forceinline__ uint64_t shuffle(uint64_t v, int lane)
+// of a lane that is the same for the whole wave
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane)
 {
-    return (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane, 64) << 32 | (uint32_t)__shfl((int)(uint32_t)v, lane, 64);
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+// of the lane before (lane 0 keeps its own)
+__device__ __forceinline__ uint64_t of_lane_before(uint64_t v)
+{
+    const int hi = (int)(v >> 32), lo = (int)(uint32_t)v;
+    return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, 0x138, 0xF, 0xF, false) << 32 |
+           (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, 0x138, 0xF, 0xF, false);
 }
 
 // A wave's list of keys, best first, one a lane: puts in every lane's `key` (0: none) that is above entry `top` - 1
 __device__ __forceinline__ void put_in(uint64_t &list, uint64_t key, int top, int lane)
 {
-    uint64_t last = shuffle(list, top - 1);
+    uint64_t last = of_lane(list, top - 1);
     uint64_t open = __ballot(key > last);
     while (open) {
-        const int from = __ffsll((unsigned long long)open) - 1;
-        const uint64_t k = shuffle(key, from);
+        const uint64_t k = of_lane(key, __ffsll((unsigned long long)open) - 1);
         open &= open - 1;
         if (k <= last) continue;
         const int at = __popcll(__ballot(list > k));
-        const uint64_t before = shuffle(list, lane > 0 ? lane - 1 : 0);
+        const uint64_t before = of_lane_before(list);
         list = lane < at ? list : lane == at ? k : before;
-        last = shuffle(list, top - 1);
+        last = of_lane(list, top - 1);
     }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, CTRL, 0xF, 0xF, true));
+}
+
+template <int D>
+__device__ __forceinline__ float swapped(float v, int lane)
+{
+    const f32x2 t = both_halves<2 * D>(v);
+    return (lane & D) ? t.x : t.y;
+}
+
+// of lane ^ X, X = 2^k or 2^k - 1
+template <int X>
+__device__ __forceinline__ float of_partner(float v, int lane)
+{
+    if constexpr (X == 1) return dpp<0xB1>(v);
+    else if constexpr (X == 2) return dpp<0x4E>(v);
+    else if constexpr (X == 3) return dpp<0x1B>(v);
+    else if constexpr (X == 4) return dpp<0x1B>(dpp<0x141>(v));
+    else if constexpr (X == 7) return dpp<0x141>(v);
+    else if constexpr (X == 8) return dpp<0x128>(v);
+    else if constexpr (X == 15) return dpp<0x140>(v);
+    else if constexpr (X == 16) return swapped<16>(v, lane);
+    else if constexpr (X == 31) return dpp<0x140>(swapped<16>(v, lane));
+    else if constexpr (X == 32) return swapped<32>(v, lane);
+    else return dpp<0x140>(swapped<16>(swapped<32>(v, lane), lane));
+}
+
+// the larger value to the lane of the pair whose bit D is clear
+template <int X, int D>
+__device__ __forceinline__ float ordered(float v, int lane)
+{
+    const float o = of_partner<X>(v, lane), hi = fmaxf(v, o), lo = fminf(v, o);
+    return (lane & D) ? lo : hi;
+}
+
+// a wave's values that rise and then fall (or the other way round) in falling order
+template <int D>
+__device__ __forceinline__ float merged(float v, int lane)
+{
+    v = ordered<D, D>(v, lane);
+    if constexpr (D > 1) v = merged<D / 2>(v, lane);
+    return v;
+}
+
+// a wave's values in falling order: sorted halves, the second one mirrored
+template <int S = 64>
+__device__ __forceinline__ float sorted(float v, int lane)
+{
+    if constexpr (S > 2) v = sorted<S / 2>(v, lane);
+    v = ordered<S - 1, S / 2>(v, lane);
+    if constexpr (S > 2) v = merged<S / 4>(v, lane);
+    return v;
+}
+
+// the `top`-th largest of the threads' values, the same in all threads
+template <int NT>
+__device__ __forceinline__ float value_of_rank(float v, int top, int lane, float *lds)
+{
+    v = sorted(v, lane);
+    if constexpr (NT > 64) {
+        lds[threadIdx.x] = v;
+        __syncthreads();
+        v = lds[lane];
+        // of two sorted lists, the larger ones of the first against the other one backwards are the first 64 of both
+        for (int w = 1; w < NT / 64; ++w) v = merged<32>(fmaxf(v, lds[w * 64 + 63 - lane]), lane);
+    }
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), top - 1));
+}
+
+// how many of `count` keys in LDS are above k
+__device__ __forceinline__ int above(const uint64_t *keys, uint32_t count, uint64_t k)
+{
+    int n = 0;
+#pragma unroll 8
+    for (uint32_t i = 0; i < count; ++i) n += keys[i] > k ? 1 : 0;
+    return n;
 }
 
 constexpr int kAhead = 4;
 
 // one piece: N logits
 template <int N>
-__device__ __forceinline__ void add_piece(const float (&v)[N], uint32_t at, float scale, Sums &s, float &most, uint32_t &most_at)
+__device__ __forceinline__ void add_piece(const float (&v)[N], float scale, Sums &s, float &most)
 {
     float m = v[0];
 #pragma unroll
     for (int k = 1; k < N; ++k) m = fmaxf(m, v[k]);
     if (m > most) {
         most = m;
-        most_at = at;
         if (m > s.m) rescale(s, m, scale);
     }
 #pragma unroll
@@ -131,149 +224,223 @@ __device__ __forceinline__ void add_piece(const float (&v)[N], uint32_t at, floa
     }
 }
 
+// What a row, or a part of one, leaves for the wave that writes the results: its sums, and the keys of its most likely tokens, one a lane.
+__device__ __forceinline__ void finish(const LogprobCall &a, int64_t row, Sums s, uint64_t found, int lane, float given, bool there)
+{
+    const bool empty = s.s == 0.0f, wrong = s.s != s.s || s.m == INFINITY;
+    const float log_sum = empty ? 0.0f : logf(s.s);
+    const auto logp_of = [&](float v) { return empty ? -INFINITY : wrong ? NAN : (v - s.m) * a.inv_temperature - log_sum; };
+    if (lane == 0) {
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / s.s);
+        if (a.stats) {
+            a.stats[row * 2] = empty ? -INFINITY : wrong ? NAN : s.m;
+            a.stats[row * 2 + 1] = empty ? 0.0f : s.s;
+        }
+        if (a.logp) a.logp[row] = there ? logp_of(given) : 0.0f;
+    }
+    if (lane < a.top) {
+        a.top_ids[row * a.top + lane] = (int64_t)(uint32_t)~(uint32_t)found;
+        a.top_logp[row * a.top + lane] = logp_of(logit_of(found));
+    }
+}
+
+// A row, or part blockIdx.x of it (a.parts > 1: few rows are cut, so that the chip is filled; logprob_join_kernel does the rest).
 template <class T, int NT>
 __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
 {
     constexpr int kWaves = NT / 64, N = 16 / sizeof(T);
     __shared__ Sums wave_sums[kWaves];
-    __shared__ uint64_t best[NT];                // top > 0: the threads' bests; then wave 0's
-    const int64_t row = blockIdx.x;
+    constexpr uint32_t kCandidates = 4 * NT;
+    __shared__ uint64_t best[kCandidates], chosen[KAN_TOP_MAX];
+    __shared__ uint32_t candidates, sources;
+    __shared__ uint16_t source[NT];
+    __shared__ float thread_most[NT];
+    const int64_t row = blockIdx.y * 65535ll + blockIdx.x / a.parts;
+    if (row >= a.R) return;
+    const uint32_t part = blockIdx.x % a.parts;
     const T *z = (const T *)a.logits + row * a.row_stride;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t V = (uint32_t)a.V, whole = V / N, pieces = (V + N - 1) / N;
+    const uint32_t begin = part * a.part_pieces, end = pieces - begin < a.part_pieces ? pieces : begin + a.part_pieces;
     const float scale = a.scale;
+    // the wave that writes the results has the given token's logit on the way from the start
+    int64_t id = -1;
+    if (wave == 0 && a.logp && a.parts == 1) id = a.ids[row];
+    const bool there = id >= 0 && id < a.V;
+    const float given = there ? widen(z[id]) : 0.0f;
 
     Sums s = {kLowest, 0.0f, 0.0f};
     float most = -INFINITY;
-    uint32_t most_at = tid, p = tid;
-    {
-        typedef typename Raw<T, N>::Wide Wide;
-        const auto read = [&](Raw<T, N> (&r)[kAhead], uint32_t from) {
+    Raw<T, N> next[kAhead];
+    const auto read = [&](uint32_t from) {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) r[u].a = *(const Wide *)(z + (int64_t)(from + u * NT) * N);
-        };
-        const uint32_t reach = (kAhead - 1) * NT;
-        Raw<T, N> next[kAhead];
-        bool more = (uint64_t)p + reach < whole;
-        if (more) read(next, p);
-        while (more) {
-            Raw<T, N> now[kAhead];
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t p = from + u * NT;
+            next[u] = raw_at<N>(z, (int64_t)p * N, p < end ? a.V : 0);
+        }
+    };
+    read(begin + tid);
+    for (uint32_t at = begin + tid; at < end; at += kAhead * NT) {
+        Raw<T, N> now[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) now[u] = next[u];
-            const uint32_t at = p;
-            p += kAhead * NT;
-            more = (uint64_t)p + reach < whole;
-            if (more) read(next, p);
+        for (int u = 0; u < kAhead; ++u) now[u] = next[u];
+        read(at + kAhead * NT);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t p = at + u * NT;
+            if (p < end) {
                 float v[N];
+                settle(now[u], (int64_t)p * N, a.V);
                 unpack(now[u], v);
-                add_piece<N>(v, at + u * NT, scale, s, most, most_at);
+                if (p >= whole)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[k] = p * N + k < V ? v[k] : -INFINITY;
+                add_piece<N>(v, scale, s, most);
             }
         }
     }
-    for (; p < pieces; p += NT) {
-        float v[N];
-        Raw<T, N> r = raw_at<N>(z, (int64_t)p * N, a.V);
-        settle(r, (int64_t)p * N, a.V);
-        unpack(r, v);
-        if (p >= whole)
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[k] = p * N + k < V ? v[k] : -INFINITY;
-        add_piece<N>(v, p, scale, s, most, most_at);
-    }
-    if (a.top) best[tid] = tid < pieces ? key_of(most, most_at) : 0;     // of pieces, not of logits
     s = join_all<NT>(s, scale, wave_sums);
-    if (wave != 0) return;
-    const bool empty = s.s == 0.0f, wrong = s.s != s.s || s.m == INFINITY;
-    const float log_sum = empty ? 0.0f : logf(s.s);
-    const float entropy = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / s.s);
-    const auto logp_of = [&](float v) { return empty ? -INFINITY : wrong ? NAN : (v - s.m) * a.inv_temperature - log_sum; };
-    if (lane == 0) {
-        if (a.entropy) a.entropy[row] = entropy;
-        if (a.stats) {
-            a.stats[row * 2] = empty ? -INFINITY : wrong ? NAN : s.m;
-            a.stats[row * 2 + 1] = empty ? 0.0f : s.s;
-        }
-        if (a.logp) {
-            const int64_t id = a.ids[row];
-            a.logp[row] = id >= 0 && id < a.V ? logp_of(widen(z[id])) : 0.0f;
-        }
-    }
-    if (!a.top) return;
 
-    // the last of the `top` best threads: below it nothing is looked at (a NaN has no place among the bests: then everything is)
-    const bool all = s.s != s.s;
-    uint64_t list = 0;
-    for (int i = 0; i < kWaves; ++i) put_in(list, best[i * 64 + lane], a.top, lane);
-    const uint64_t bound = all ? 0 : shuffle(list, a.top - 1);
-    const uint32_t sources = all ? NT : a.top, each = (pieces + NT - 1) / NT, count = sources * each;
     uint64_t found = 0;
-    if (lane < (uint32_t)a.top) best[lane] = list;
-    __builtin_amdgcn_wave_barrier();
-    for (uint32_t first = 0; first < count; first += 64) {
-        // piece number i % each of source i / each: the thread that has the source's best
-        const uint32_t i = first + lane, src = i / each;
-        uint32_t at = pieces;
-        if (src < sources) {
-            const uint64_t k = all ? 1 : best[src];
-            if (k) at = (all ? src : (uint32_t)~(uint32_t)k % NT) + i % each * NT;
-        }
-        float v[N];
-        Raw<T, N> r = raw_at<N>(z, (int64_t)at * N, at < pieces ? a.V : 0);
-        settle(r, (int64_t)at * N, at < pieces ? a.V : 0);
-        unpack(r, v);
+    if (a.top) {
+        // The threads whose largest logit is among the `top` largest of these have all logits that matter (a NaN hides in their maximum: then
+        // all threads have).
+        const bool all = s.s != s.s;
+        const float bound = all ? -INFINITY : value_of_rank<NT>(most, a.top, lane, thread_most);
+        if (tid == 0) sources = candidates = 0;
+        if (tid < KAN_TOP_MAX) chosen[tid] = 0;
+        __syncthreads();
+        if (begin + tid < end && (all || most >= bound)) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
+        __syncthreads();
+        const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
+        // piece number i % each of source i / each
+        const auto piece_keys = [&](uint32_t i, uint64_t (&key)[N]) {
+            const uint32_t at = i < count ? begin + source[i / each] + i % each * NT : end;
+            float v[N];
+            Raw<T, N> r = raw_at<N>(z, (int64_t)at * N, at < end ? a.V : 0);
+            settle(r, (int64_t)at * N, at < end ? a.V : 0);
+            unpack(r, v);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const uint32_t index = at * N + k;
-            uint64_t key = at < pieces && index < V ? key_of(v[k], index) : 0;
-            // a thread's best stands for its piece: compare by piece
-            const uint64_t by_piece = key ? (key & 0xFFFFFFFF00000000ull) | (uint32_t)~at : 0;
-            if (by_piece < bound) key = 0;
-            put_in(found, key, a.top, lane);
+            for (int k = 0; k < N; ++k) key[k] = at < end && at * N + k < V && !(v[k] < bound) ? key_of(v[k], at * N + k) : 0;
+        };
+        uint64_t key[N];
+        for (uint32_t i = tid; i < count; i += NT) {
+            piece_keys(i, key);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (key[k]) {
+                    const uint32_t slot = atomicAdd(&candidates, 1u);
+                    if (slot < kCandidates) best[slot] = key[k];
+                }
+        }
+        __syncthreads();
+        if (candidates <= kCandidates) {
+            const uint32_t n = candidates;
+            for (uint32_t i = tid; i < n; i += NT) {
+                const uint64_t k = best[i];
+                const int at = above(best, n, k);
+                if (at < a.top) chosen[at] = k;
+            }
+            __syncthreads();
+            if (wave == 0 && lane < (uint32_t)a.top) found = chosen[lane];
+        } else if (wave == 0) {
+            // more than there is room for (many equal logits, rows with NaN): one by one into a sorted list
+            for (uint32_t first = 0; first < count; first += 64) {
+                piece_keys(first + lane, key);
+#pragma unroll
+                for (int k = 0; k < N; ++k) put_in(found, key[k], a.top, lane);
+            }
         }
     }
-    if (lane < (uint32_t)a.top) {
-        const float v = logit_of(found);
-        a.top_ids[row * a.top + lane] = (int64_t)(uint32_t)~(uint32_t)found;
-        a.top_logp[row * a.top + lane] = logp_of(v);
+    if (wave != 0) return;
+    if (a.parts == 1) {
+        finish(a, row, s, found, lane, given, there);
+        return;
     }
+    const int64_t slot = row * a.parts + part;
+    if (lane == 0) a.part_sums[slot] = s;
+    if (lane < (uint32_t)a.top) a.part_keys[slot * a.top + lane] = found;
 }
 
-constexpr int kBackPieces = 4;      // of 16 bytes a thread
-
+// a workgroup for each row that was cut, at most 64 parts
 template <class T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobCall a)
+{
+    __shared__ uint64_t key[256], chosen[KAN_TOP_MAX];
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, keys = a.parts * a.top;
+    uint64_t found = 0;
+    if (keys > 0 && keys <= 256) {
+        const uint64_t k = tid < keys ? a.part_keys[row * keys + tid] : 0;
+        key[tid] = k;
+        if (tid < KAN_TOP_MAX) chosen[tid] = 0;
+        __syncthreads();
+        const int at = above(key, keys, k);
+        if (k && at < a.top) chosen[at] = k;
+        __syncthreads();
+        if (lane < a.top) found = chosen[lane];
+    }
+    if (tid >= 64) return;
+    int64_t id = -1;
+    if (a.logp) id = a.ids[row];
+    const bool there = id >= 0 && id < a.V;
+    const float given = there ? widen(((const T *)a.logits + row * a.row_stride)[id]) : 0.0f;
+    Sums s = {kLowest, 0.0f, 0.0f};
+    if (lane < a.parts) s = a.part_sums[row * a.parts + lane];
+    s = join_all<64>(s, a.scale, nullptr);
+    if (keys > 256)
+        for (int i = 0; i < keys; i += 64) put_in(found, i + lane < keys ? a.part_keys[row * keys + i + lane] : 0, a.top, lane);
+    finish(a, row, s, found, lane, given, there);
+}
+
+constexpr int kBackPieces = 4;      // of 16 bytes a thread, next to one another in a row or (ROWS) in four rows
+
+template <class T, bool ROWS>
 __global__ __launch_bounds__(256) void logprob_back_kernel(LogprobCall a)
 {
     constexpr int N = 16 / sizeof(T);
-    const int64_t row = blockIdx.y, V = a.V, first = ((int64_t)blockIdx.x * 256 * kBackPieces + threadIdx.x) * N;
-    const T *z = (const T *)a.logits + row * a.row_stride;
+    const int64_t V = a.V;
+    int64_t row[kBackPieces], c[kBackPieces];
     Raw<T, N> r[kBackPieces];
 #pragma unroll
-    for (int u = 0; u < kBackPieces; ++u) r[u] = raw_at<N>(z, first + u * 256 * N, V);
-    const float m = a.stats[row * 2], sum = a.stats[row * 2 + 1];
-    const int64_t id = a.g_logp ? a.ids[row] : -1;
-    const bool given = id >= 0 && id < V;
-    const float g = given ? a.g_logp[row] : 0.0f, ge = a.g_entropy ? a.g_entropy[row] : 0.0f;
-    // -p (g + ge (log p + entropy)) / temperature = 2^y (c0 + c1 y)
-    const float shift = a.g_entropy ? a.entropy[row] - logf(sum) : 0.0f, inv = -a.inv_temperature / sum;
-    const float c0 = inv * (g + ge * shift), c1 = inv * ge * kLn2, hit = g * a.inv_temperature;
-    const bool empty = m == -INFINITY;
+    for (int u = 0; u < kBackPieces; ++u) {
+        row[u] = ROWS ? (int64_t)blockIdx.y * kBackPieces + u : blockIdx.y;
+        c[u] = ROWS ? ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * N : (((int64_t)blockIdx.x * kBackPieces + u) * blockDim.x + threadIdx.x) * N;
+        if (ROWS && row[u] >= a.R) row[u] = a.R - 1, c[u] = V;
+        r[u] = raw_at<N>((const T *)a.logits + row[u] * a.row_stride, c[u], V);
+    }
+    float m = 0.0f, c0 = 0.0f, c1 = 0.0f, hit = 0.0f;
+    int64_t id = -1;
+    bool empty = false;
 #pragma unroll
     for (int u = 0; u < kBackPieces; ++u) {
-        const int64_t c = first + u * 256 * N;
+        if (ROWS || u == 0) {
+            // -p (g + ge (log p + entropy)) / temperature = 2^y (c0 + c1 y)
+            const int64_t at = row[u];
+            m = a.stats[at * 2];
+            const float sum = a.stats[at * 2 + 1];
+            id = a.g_logp ? a.ids[at] : -1;
+            const bool given = id >= 0 && id < V;
+            const float g = given ? a.g_logp[at] : 0.0f, ge = a.g_entropy ? a.g_entropy[at] : 0.0f;
+            const float shift = a.g_entropy ? a.entropy[at] - logf(sum) : 0.0f, inv = -a.inv_temperature / sum;
+            c0 = inv * (g + ge * shift);
+            c1 = inv * ge * kLn2;
+            hit = g * a.inv_temperature;
+            empty = m == -INFINITY;
+            if (!given || empty) id = -1;
+        }
         float v[N];
-        settle(r[u], c, V);
+        settle(r[u], c[u], V);
         unpack(r[u], v);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float y = (v[k] - m) * a.scale;
             v[k] = empty ? 0.0f : __builtin_amdgcn_exp2f(y) * __builtin_fmaf(c1, fmaxf(y, kFar), c0);
         }
-        if (given && !empty && id >= c && id < c + N)
+        if (id >= c[u] && id < c[u] + N)
 #pragma unroll
-            for (int k = 0; k < N; ++k) v[k] += c + k == id ? hit : 0.0f;
-        store_at<N, true>((T *)a.glogits + row * V, c, V, v);
+            for (int k = 0; k < N; ++k) v[k] += c[u] + k == id ? hit : 0.0f;
+        store_at<N, true>((T *)a.glogits + row[u] * V, c[u], V, v);
     }
 }
 
@@ -284,24 +451,49 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, float temperat
     return KAN_OK;
 }
 
-template <class T>
-hipError_t launch_forward(const LogprobCall &a, hipStream_t st)
+// How a row is cut: few rows of a large vocabulary are shared among workgroups, four a CU, of 4096 logits at least.  16 x 32768 bf16 with five
+// alternatives in one piece a row 14.8 us, in eight 8.0 (a launch more); 1 x 131072 22.6 and 9.2.
+int parts_of(int64_t R, int64_t V)
 {
-    prof::Timed timed("token_logprob", st);
-    const unsigned rows = (unsigned)a.R;
-    if (a.V <= 4096) logprob_kernel<T, 64><<<rows, 64, 0, st>>>(a);
-    else if (a.V <= 16384 || a.R >= 1024) logprob_kernel<T, 256><<<rows, 256, 0, st>>>(a);
-    else logprob_kernel<T, 1024><<<rows, 1024, 0, st>>>(a);
+    if (R <= 0 || R > 512 || V < 8192) return 1;
+    int64_t parts = 1024 / R;
+    if (parts > V / 4096) parts = V / 4096;
+    return (int)(parts > 64 ? 64 : parts);
+}
+
+template <class T>
+hipError_t launch_forward(LogprobCall &a, hipStream_t st)
+{
+    constexpr uint32_t N = 16 / sizeof(T);
+    const uint32_t pieces = (uint32_t)div_up(a.V, (int64_t)N);
+    a.part_pieces = div_up(pieces, (uint32_t)a.parts);
+    a.parts = (int)div_up(pieces, a.part_pieces);
+    const dim3 grid((unsigned)(a.R < 65535 ? a.R : 65535) * a.parts, (unsigned)div_up(a.R, (int64_t)65535));
+    {
+        prof::Timed timed("token_logprob", st);
+        if (a.V <= 4096) logprob_kernel<T, 64><<<grid, 64, 0, st>>>(a);
+        else logprob_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 1) return e;
+    prof::Timed timed("token_logprob_join", st);
+    logprob_join_kernel<T><<<(unsigned)a.R, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t launch_backward(const LogprobCall &all, hipStream_t st)
 {
+    constexpr int N = 16 / sizeof(T);
     prof::Timed timed("token_logprob_backward", st);
-    for (int64_t first = 0; first < all.R; first += 65535) {
+    // Rows of up to two workgroups' width: four rows a thread, a piece of each.
+    const int64_t pieces = div_up(all.V, (int64_t)N);
+    const bool by_rows = pieces <= 512;
+    const int threads = pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256;
+    const int64_t most = by_rows ? 65535ll * kBackPieces : 65535;
+    for (int64_t first = 0; first < all.R; first += most) {
         LogprobCall a = all;
-        const int64_t rows = all.R - first < 65535 ? all.R - first : 65535;
+        a.R = all.R - first < most ? all.R - first : most;
         a.logits = (const T *)all.logits + first * all.row_stride;
         a.glogits = (T *)all.glogits + first * all.V;
         a.stats = all.stats + first * 2;
@@ -313,7 +505,10 @@ hipError_t launch_backward(const LogprobCall &all, hipStream_t st)
             a.g_entropy += first;
             a.entropy += first;
         }
-        logprob_back_kernel<T><<<dim3((unsigned)div_up(all.V, (int64_t)(256 * kBackPieces * 16 / sizeof(T))), (unsigned)rows), 256, 0, st>>>(a);
+        if (by_rows)
+            logprob_back_kernel<T, true><<<dim3((unsigned)div_up(pieces, (int64_t)threads), (unsigned)div_up(a.R, (int64_t)kBackPieces)), threads, 0, st>>>(a);
+        else
+            logprob_back_kernel<T, false><<<dim3((unsigned)div_up(pieces, (int64_t)(256 * kBackPieces)), (unsigned)a.R), 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -325,7 +520,13 @@ hipError_t launch_backward(const LogprobCall &all, hipStream_t st)
 
 using namespace kannet;
 
-extern "C" size_t kan_token_logprob_workspace_bytes(int64_t, int64_t, int32_t) { return 0; }
+// nothing where rows are not cut
+extern "C" size_t kan_token_logprob_workspace_bytes(int64_t R, int64_t V, int32_t top)
+{
+    if (V <= 0 || top < 0 || top > KAN_TOP_MAX) return 0;
+    const int parts = parts_of(R, V);
+    return parts > 1 ? align_up((size_t)R * parts * sizeof(Sums)) + align_up((size_t)R * parts * top * sizeof(uint64_t)) : 0;
+}
 
 extern "C" int kan_token_logprob_forward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, const int64_t *ids,
                                          float temperature, int32_t top, float *logp, float *entropy, float *stats, int64_t *top_ids,
@@ -355,6 +556,9 @@ extern "C" int kan_token_logprob_forward(int64_t R, int64_t V, const void *logit
     a.stats = stats;
     a.top_ids = top_ids;
     a.top_logp = top_logp;
+    a.parts = parts_of(R, V);
+    a.part_sums = (Sums *)ws;
+    a.part_keys = (uint64_t *)((char *)ws + align_up((size_t)R * a.parts * sizeof(Sums)));
     return status_of(type == KAN_F32 ? launch_forward<float>(a, (hipStream_t)stream) : launch_forward<bf16>(a, (hipStream_t)stream));
 }
 
