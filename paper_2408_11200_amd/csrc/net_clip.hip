@@ -1,9 +1,11 @@
 // The norm of all gradients of a network, and the gradients scaled to it (kan_net.h).
 //
 // Bound by HBM: the norm needs every element before the first one can be scaled, so the data are read twice and written once.  A launch takes
-// up to kMost tensors from its arguments (no table is copied to the device); its workgroups have consecutive chunks of the list, add squares
-// in 64 bits (a float's square fits exactly, so neither range nor digits are lost) and leave one sum each.  Every workgroup of the
-// scaling launch adds all of these sums in the same order: no launch in between, and one factor for all.
+// up to kMost tensors from its arguments (no table is copied to the device) and goes through the list in chunks of 8192 elements, its
+// workgroups side by side: squares are added in 64 bits (a float's square fits exactly, so neither range nor digits are lost), one sum a
+// workgroup.  Every workgroup of the scaling launch adds all of these sums in the same order: no launch in between, and one factor for
+// all.  It goes from the list's end to its start, where the first pass has been last: what the caches still hold is not read again, and
+// what they cannot hold is read past them.  A network that fits eight chunks is one workgroup's work, in one launch.
 #include "net_device.hpp"
 
 namespace kannet {
@@ -13,6 +15,8 @@ constexpr int kMost = 96;                // tensors of a launch
 constexpr int kThreads = 256;
 constexpr int kChunk = 8192;             // elements of a chunk
 constexpr int kSums = 1024;              // of all launches, but one for each launch at least
+constexpr int kSmall = 8;                // chunks that one workgroup takes
+constexpr double kCached = 192e6;        // bytes of the list's end that are read through the caches
 
 struct ClipCall {
     const void *data[kMost];
@@ -24,17 +28,10 @@ struct ClipCall {
     float *norm;
     float max_norm;
     int n, sums_before, sums_all;
+    uint32_t stream_until;               // chunks before this one are read past the caches
     bool writes_norm;
 };
 static_assert(sizeof(ClipCall) <= 4096, "kernel arguments");
-
-// chunks of a workgroup
-__device__ __forceinline__ void share(const ClipCall &a, uint32_t &chunk, uint32_t &end)
-{
-    const uint64_t all = a.first[a.n];
-    chunk = (uint32_t)(all * blockIdx.x / gridDim.x);
-    end = (uint32_t)(all * (blockIdx.x + 1) / gridDim.x);
-}
 
 // the tensor that has a chunk
 __device__ __forceinline__ int tensor_of(const ClipCall &a, uint32_t chunk)
@@ -61,35 +58,93 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return t;
 }
 
-template <class T>
+// the elements of a chunk that a thread has, one of NT that share it: `f` gets N values and their place
+template <int NT, bool STREAM, class T, class F>
+__device__ __forceinline__ void each_piece(const T *p, int count, F f)
+{
+    constexpr int N = 16 / sizeof(T), AHEAD = kChunk / (N * NT) < 8 ? kChunk / (N * NT) : 8;
+    for (int i = threadIdx.x % NT * N; i < count; i += NT * N * AHEAD) {
+        Raw<T, N> r[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) r[u] = raw_at<N, STREAM>(p, i + u * NT * N, count);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            float v[N];
+            settle(r[u], i + u * NT * N, count);
+            unpack(r[u], v);
+            f(v, i + u * NT * N);
+        }
+    }
+}
+
+template <int NT, bool STREAM, class T>
 __device__ __forceinline__ double chunk_squares(const T *p, int count)
 {
-    constexpr int N = 16 / sizeof(T);
     double t = 0.0;
-    for (int i = threadIdx.x * N; i < count; i += kThreads * N) {
-        float v[N];
-        Raw<T, N> r = raw_at<N>(p, i, count);
-        settle(r, i, count);
-        unpack(r, v);
+    each_piece<NT, STREAM>(p, count, [&](const float(&v)[16 / sizeof(T)], int) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) t += (double)v[k] * (double)v[k];
-    }
+        for (int k = 0; k < 16 / (int)sizeof(T); ++k) t += (double)v[k] * (double)v[k];
+    });
     return t;
 }
+
+template <int NT, class T>
+__device__ __forceinline__ void scale_chunk(const T *p, T *to, int count, float factor)
+{
+    each_piece<NT, false>(p, count, [&](float(&v)[16 / sizeof(T)], int i) {
+#pragma unroll
+        for (int k = 0; k < 16 / (int)sizeof(T); ++k) v[k] *= factor;
+        store_at<16 / sizeof(T), true>(to, i, count, v);
+    });
+}
+
+// chunk c of the list, or a quarter of it: its tensor, and where in it
+struct Place {
+    int i, count;
+    int64_t at;
+};
+
+__device__ __forceinline__ Place place_of(const ClipCall &a, uint32_t c)
+{
+    Place p;
+    p.i = tensor_of(a, c);
+    p.at = (int64_t)(c - a.first[p.i]) * kChunk;
+    const int64_t left = a.count[p.i] - p.at;
+    p.count = left < kChunk ? (int)left : kChunk;
+    return p;
+}
+
+__device__ __forceinline__ Place quarter_of(const ClipCall &a, uint32_t q)
+{
+    Place p = place_of(a, q / 4);
+    const int from = (int)(q % 4) * (kChunk / 4);
+    p.at += from;
+    p.count = p.count - from < kChunk / 4 ? p.count - from : kChunk / 4;
+    return p;
+}
+
+template <int NT, bool STREAM>
+__device__ __forceinline__ double squares_at(const ClipCall &a, const Place &p)
+{
+    return a.type[p.i] == KAN_F32 ? chunk_squares<NT, STREAM>((const float *)a.data[p.i] + p.at, p.count)
+                                  : chunk_squares<NT, STREAM>((const bf16 *)a.data[p.i] + p.at, p.count);
+}
+
+template <int NT>
+__device__ __forceinline__ void scale_at(const ClipCall &a, const Place &p, float factor)
+{
+    if (factor == 1.0f && a.out[p.i] == a.data[p.i]) return;        // in place, and nothing to change
+    if (a.type[p.i] == KAN_F32) scale_chunk<NT>((const float *)a.data[p.i] + p.at, (float *)a.out[p.i] + p.at, p.count, factor);
+    else scale_chunk<NT>((const bf16 *)a.data[p.i] + p.at, (bf16 *)a.out[p.i] + p.at, p.count, factor);
+}
+
+__device__ __forceinline__ float factor_of(float norm, float max_norm) { return norm < INFINITY && norm > max_norm ? max_norm / norm : 1.0f; }
 
 __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipCall a)
 {
     __shared__ double lds[kThreads / 64];
-    uint32_t chunk, end;
-    share(a, chunk, end);
     double t = 0.0;
-    int i = chunk < end ? tensor_of(a, chunk) : 0;
-    for (; chunk < end; ++chunk) {
-        while (chunk >= a.first[i + 1]) ++i;
-        const int64_t at = (int64_t)(chunk - a.first[i]) * kChunk, left = a.count[i] - at;
-        const int count = left < kChunk ? (int)left : kChunk;
-        t += a.type[i] == KAN_F32 ? chunk_squares((const float *)a.data[i] + at, count) : chunk_squares((const bf16 *)a.data[i] + at, count);
-    }
+    for (uint32_t c = blockIdx.x; c < a.first[a.n]; c += gridDim.x) t += c < a.stream_until ? squares_at<kThreads, true>(a, place_of(a, c)) : squares_at<kThreads, false>(a, place_of(a, c));
     t = block_sum<kThreads>(t, lds);
     if (threadIdx.x == 0) a.sums[a.sums_before + blockIdx.x] = t;
 }
@@ -102,39 +157,14 @@ __device__ __forceinline__ float norm_of(const ClipCall &a, double *lds)
     return (float)sqrt(block_sum<kThreads>(t, lds));
 }
 
-template <class T>
-__device__ __forceinline__ void scale_chunk(const T *p, T *to, int count, float factor)
-{
-    constexpr int N = 16 / sizeof(T);
-    for (int i = threadIdx.x * N; i < count; i += kThreads * N) {
-        float v[N];
-        Raw<T, N> r = raw_at<N>(p, i, count);
-        settle(r, i, count);
-        unpack(r, v);
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] *= factor;
-        store_at<N>(to, i, count, v);
-    }
-}
-
 __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipCall a)
 {
     __shared__ double lds[kThreads / 64];
     const float norm = norm_of(a, lds);
     if (a.writes_norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
-    const bool finite = norm < INFINITY;
-    const float factor = finite && norm > a.max_norm ? a.max_norm / norm : 1.0f;
-    uint32_t chunk, end;
-    share(a, chunk, end);
-    int i = chunk < end ? tensor_of(a, chunk) : 0;
-    for (; chunk < end; ++chunk) {
-        while (chunk >= a.first[i + 1]) ++i;
-        if (factor == 1.0f && a.out[i] == a.data[i]) continue;        // in place, and nothing to change
-        const int64_t at = (int64_t)(chunk - a.first[i]) * kChunk, left = a.count[i] - at;
-        const int count = left < kChunk ? (int)left : kChunk;
-        if (a.type[i] == KAN_F32) scale_chunk((const float *)a.data[i] + at, (float *)a.out[i] + at, count, factor);
-        else scale_chunk((const bf16 *)a.data[i] + at, (bf16 *)a.out[i] + at, count, factor);
-    }
+    const float factor = factor_of(norm, a.max_norm);
+    const uint32_t all = a.first[a.n];
+    for (uint32_t c = blockIdx.x; c < all; c += gridDim.x) scale_at<kThreads>(a, place_of(a, all - 1 - c), factor);
 }
 
 __global__ __launch_bounds__(kThreads) void clip_norm_kernel(ClipCall a)
@@ -142,6 +172,42 @@ __global__ __launch_bounds__(kThreads) void clip_norm_kernel(ClipCall a)
     __shared__ double lds[kThreads / 64];
     const float norm = norm_of(a, lds);
     if (threadIdx.x == 0) *a.norm = norm;
+}
+
+// A wave for each quarter of a chunk, element by element: what counts here is the way to the first value and little code, not bandwidth.
+template <class T, class F>
+__device__ __forceinline__ void each_element(const T *p, int count, F f)
+{
+    for (int i = threadIdx.x & 63; i < count; i += 64 * 8) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * 64 < count ? widen(p[i + u * 64]) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u * 64 < count) f(v[u], i + u * 64);
+    }
+}
+
+__global__ __launch_bounds__(1024) void clip_small_kernel(ClipCall a, bool clip)
+{
+    __shared__ double lds[16];
+    double t = 0.0;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarters = 4 * a.first[a.n];
+    for (uint32_t q = wave; q < quarters; q += 16) {
+        const Place p = quarter_of(a, q);
+        const auto square = [&](float v, int) { t += (double)v * (double)v; };
+        if (a.type[p.i] == KAN_F32) each_element((const float *)a.data[p.i] + p.at, p.count, square);
+        else each_element((const bf16 *)a.data[p.i] + p.at, p.count, square);
+    }
+    const float norm = (float)sqrt(block_sum<1024>(t, lds));
+    if (threadIdx.x == 0) *a.norm = norm;
+    if (!clip) return;
+    const float factor = factor_of(norm, a.max_norm);
+    for (uint32_t q = wave; q < quarters; q += 16) {
+        const Place p = quarter_of(a, q);
+        if (a.type[p.i] == KAN_F32) each_element((const float *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((float *)a.out[p.i] + p.at + i, v * factor); });
+        else each_element((const bf16 *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((bf16 *)a.out[p.i] + p.at + i, v * factor); });
+    }
 }
 
 int launches_of(int n) { return n > 0 ? div_up(n, kMost) : 1; }
@@ -167,25 +233,43 @@ int run(int32_t n, const kan_tensor_ref *list, float max_norm, bool clip, float 
     if (!norm || misplaced(norm, KAN_F32)) return KAN_ERR_INVALID_ARG;
     if (bad_workspace(ws, ws_bytes, kan_clip_workspace_bytes(n))) return KAN_ERR_WORKSPACE;
     const int launches = launches_of(n), most = kSums / launches > 1 ? kSums / launches : 1;
+    double bytes = 0.0;
+    for (int i = 0; i < n; ++i) bytes += (double)list[i].count * (double)size_of(list[i].type);
     int sums_all = 0;
     for (int phase = 0; phase < 2; ++phase) {
         int before = 0;
-        for (int l = 0; l < launches; ++l) {
+        double at = 0.0;
+        // the second pass takes the launches from the last one on, too
+        for (int k = 0; k < launches; ++k) {
+            const int l = phase == 0 ? k : launches - 1 - k;
             ClipCall a = {};
-            uint64_t chunks = 0;
+            uint64_t chunks = 0, stream_until = 0;
             for (int i = l * kMost; i < n && i < (l + 1) * kMost; ++i) {
                 if (list[i].count == 0) continue;
                 a.data[a.n] = list[i].data;
                 a.out[a.n] = list[i].out;
                 a.count[a.n] = list[i].count;
                 a.type[a.n] = (uint8_t)list[i].type;
-                chunks += (uint64_t)div_up(list[i].count, (int64_t)kChunk);
+                const uint64_t here = (uint64_t)div_up(list[i].count, (int64_t)kChunk);
+                const double chunk_bytes = (double)kChunk * (double)size_of(list[i].type);
+                // whole chunks of this tensor that end before the list's last kCached bytes
+                const double before_cached = (bytes - kCached - at) / chunk_bytes;
+                if (before_cached > 0.0) stream_until = chunks + (before_cached < (double)here ? (uint64_t)before_cached : here);
+                at += (double)list[i].count * (double)size_of(list[i].type);
+                chunks += here;
+                if (chunks > 0xFFFFFFFFull) return KAN_ERR_UNSUPPORTED;
                 a.first[++a.n] = (uint32_t)chunks;
             }
-            const int blocks = chunks < 1 ? 1 : chunks < (uint64_t)most ? (int)chunks : most;
+            a.stream_until = (uint32_t)stream_until;
             a.sums = (double *)ws;
             a.norm = norm;
             a.max_norm = max_norm;
+            if (launches == 1 && chunks <= kSmall) {
+                prof::Timed timed("gradient_clip", st);
+                clip_small_kernel<<<1, 1024, 0, st>>>(a, clip);
+                return status_of(hipGetLastError());
+            }
+            const int blocks = chunks < 1 ? 1 : chunks < (uint64_t)most ? (int)chunks : most;
             a.sums_before = before;
             a.sums_all = sums_all;
             a.writes_norm = l == 0;
@@ -194,7 +278,7 @@ int run(int32_t n, const kan_tensor_ref *list, float max_norm, bool clip, float 
                 prof::Timed timed("gradient_squares", st);
                 clip_squares_kernel<<<blocks, kThreads, 0, st>>>(a);
             } else if (clip) {
-                const int wide = chunks < 1 ? 1 : chunks < 4096 ? (int)chunks : 4096;
+                const int wide = chunks < 1 ? 1 : chunks < 2048 ? (int)chunks : 2048;
                 prof::Timed timed("gradient_scale", st);
                 clip_scale_kernel<<<wide, kThreads, 0, st>>>(a);
             } else if (l == 0) {
