@@ -2,7 +2,8 @@
 
 The compute lives in the HIP library built from `csrc/` (C ABI declared in
 `include/kan.h`); `binding` is the thin ctypes front end with the same entry
-point names.  Importing this package does not load the library; the first call
+point names, and `net` that of the operators around the layers
+(`include/kan_net.h`).  Importing this package does not load the library; the first call
 into `binding` does, and fails loudly when it has not been built.
 """
-__all__ = ["binding", "autograd", "workloads", "roofline"]
+__all__ = ["binding", "net", "autograd", "workloads", "roofline"]

@@ -109,11 +109,11 @@ struct BlockNorm : torch::autograd::Function<BlockNorm> {
         const Tensor gx_out = f.defined() ? whole(grads[0]) : Tensor(), gh = c.want_h ? whole(grads[f.defined() ? 1 : 0]) : Tensor();
         if (!gx_out.defined() && !gh.defined()) return g;
         bool any = false;
-        // edges: x, f, then the parameters, whether or not they are there
-        if (ctx->needs_input_grad(0)) g[0] = at::empty(saved[0].sizes(), x.options()), any = true;
-        if (f.defined() && ctx->needs_input_grad(1)) g[1] = at::empty(saved[1].sizes(), f.options()), any = true;
-        for (int i = 0; i < 5; ++i)
-            if (p[i].defined() && ctx->needs_input_grad((size_t)i + 2)) g[i + 2] = at::empty(p[i].sizes(), p[i].options()), any = true;
+        size_t edge = 0;        // of the tensors that are there
+        for (int i = 0; i < 7; ++i) {
+            if (!saved[i].defined()) continue;
+            if (ctx->needs_input_grad(edge++)) g[i] = at::empty(saved[i].sizes(), saved[i].options()), any = true;
+        }
         if (!any) return g;
         const kan_block_norm_params q = params_of(p);
         const kan_block_norm_grads w = {f32(g[2]), f32(g[3]), f32(g[4]), f32(g[5]), f32(g[6])};

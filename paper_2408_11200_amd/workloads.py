@@ -204,3 +204,15 @@ def regression_task(which, seed=1200, B=4096):
         i = np.arange(16)
         t = np.exp(np.sin((4.0 * i / 15.0 + 1.0) * np.pi * x).sum(1) / 15.0)
     return _f32(x), _f32(t[:, None])
+
+
+def token_task(vocab=64, n=1 << 16, seed=1300, noise=0.1):
+    """Pairs of tokens and the token behind them: most often a fixed function of the two, else any token.  (ids[n][2], target[n], the least loss
+    a model can reach.)"""
+    rng = np.random.default_rng(seed)
+    a, b = rng.permutation(vocab), rng.permutation(vocab)
+    follow = (a[:, None] + b[None, :]) % vocab
+    ids = rng.integers(0, vocab, size=(n, 2))
+    target = np.where(rng.random(n) < noise, rng.integers(0, vocab, n), follow[ids[:, 0], ids[:, 1]])
+    hit, other = 1.0 - noise + noise / vocab, noise / vocab
+    return ids, target, float(-(hit * np.log(hit) + (vocab - 1) * other * np.log(other)))

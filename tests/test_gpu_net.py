@@ -183,6 +183,27 @@ def test_block_norm_through_autograd():
         assert a is t["x"] and b.dtype == F32
 
 
+@pytest.mark.parametrize("have", [(), ("gate",), ("w_pre",), ("b_post", "w_pre"), ("w_post", "b_post", "gate")])
+@pytest.mark.parametrize("branch", [True, False])
+@pytest.mark.parametrize("frozen", [None, "x", "f", "gate"])
+def test_block_norm_through_autograd_with_some_of_its_tensors(have, branch, frozen):
+    """Missing and frozen tensors: each of the others gets its own gradient."""
+    spec, t, p = norm_case(40, 72, "layer", 10, 13, have=have)
+    leaves = dict(x=t["x"], **(dict(f=t["f"]) if branch else {}), **p)
+    leaves = {k: v.clone().requires_grad_(k != frozen) for k, v in leaves.items()}
+    x_out, h = autograd.block_norm(spec, **leaves)
+    stats = torch.empty((40, 4), device="cuda")
+    f = t["f"] if branch else None
+    net.kan_block_norm_forward(spec, t["x"], f, p, stats=stats)
+    ref = net.kan_block_norm_backward(spec, t["x"], f, p, stats, t["gx_out"] if branch else None, t["gh"])
+    live = [k for k, v in leaves.items() if v.requires_grad and (branch or k in ("x", "w_pre", "b_pre"))]
+    outs, gouts = ([x_out, h], [t["gx_out"], t["gh"]]) if branch else ([h], [t["gh"]])
+    if not live:
+        return
+    for k, v in zip(live, torch.autograd.grad(outs, [leaves[k] for k in live], gouts)):
+        assert v.shape == leaves[k].shape and torch.equal(v.view(-1), ref["g" + k].view(-1)), k
+
+
 def test_block_norm_gradient_is_the_difference():
     """Along a random direction: (loss(v + e d) - loss(v - e d)) / 2 e, the loss summed in 64 bits.  32-bit outputs of size 1 are off by some 64 u
     each; over e = 2^-7 and the square root of 7000 of them that is 64 u 84 / 2^-6 = 0.02; the third derivative adds e^2 times the gradient's size."""
