@@ -452,7 +452,7 @@ Layout layout_of(int64_t T, int64_t V, int n)
         return here;
     };
     l.counts = take((size_t)l.blocks * ((size_t)4 << l.bits));
-    l.starts = take(((size_t)div_up(T, (int64_t)kPiece) + 1) * 4);
+    l.starts = take(T > 0 ? ((size_t)div_up(T, (int64_t)kPiece) + 1) * 4 : 0);
     for (int i = 0; i < 2; ++i) {
         l.keys[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
         l.places[i] = take((size_t)div_up(T, (int64_t)kPiece) * kPiece * 4);
