@@ -146,65 +146,62 @@ __global__ __launch_bounds__(kSortThreads) void embedding_place_kernel(SortPass 
     }
 }
 
-// The whole sort of up to 4096 entries in one workgroup, four a thread, which lie in LDS between the passes: two launches a pass cost more than
-// one CU's work up to there (two passes over 4096 entries 13.1 and 17.4 us, over 8192 21.2 and 17.4).
-constexpr int kSmallEntries = 4;
-constexpr int64_t kSmallSort = (int64_t)kSmallEntries * kSortThreads;
+// The whole sort of up to 16384 tokens in one launch: a workgroup for each range of 2^bits ids goes through all tokens, a wave through consecutive
+// ones; it keeps those of its range, in their order, in LDS, counts those below, and places what it kept.  The tokens come from L2, so that the
+// launches saved (two a digit, some 9 us) are worth it while the ranges' workgroups are hardly more than the CUs.  By digits and so, us: 16384 tokens
+// of 50001 ids 18.2 and 14.0, 4096 of 8000 17.4 and 6.5; one digit, 256 ids, 16384 tokens 8.7 and 13.2.
+constexpr int kRangeRounds = 16;                                  // of 64 tokens a wave
+constexpr int64_t kRangeTokens = (int64_t)kRangeRounds * kSortThreads;
+constexpr int64_t kRanges = 512;
 
-__global__ __launch_bounds__(kSortThreads) void embedding_small_sort_kernel(SortPass a, int passes)
+__global__ __launch_bounds__(kSortThreads) void embedding_range_sort_kernel(SortPass a)
 {
     __shared__ uint32_t cursor[kSortWaves][1 << kMaxDigit];
-    __shared__ uint32_t wave_total[kSortWaves], keys[kSmallSort], places[kSmallSort];
-    const uint32_t digits = 1u << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_wave = (a.T + kSortThreads - 1) / kSortThreads * 64;
-    if (threadIdx.x == 0) *a.starts = 0;
-    uint32_t key[kSmallEntries], place[kSmallEntries];
+    __shared__ uint32_t kept[kSortWaves][kRangeRounds * 64];         // id in the range, and which of the wave's tokens it is
+    __shared__ uint32_t wave_total[kSortWaves], wave_below[kSortWaves];
+    constexpr uint32_t kNone = 0xFFFFFFFFu;
+    const uint32_t digits = 1u << a.bits, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, start = blockIdx.x << a.bits;
+    const uint32_t per_wave = (a.T + kSortThreads - 1) / kSortThreads * 64, from = wave * per_wave;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.starts = 0;
+    uint32_t key[kRangeRounds];
 #pragma unroll
-    for (int j = 0; j < kSmallEntries; ++j) {
-        place[j] = wave * per_wave + j * 64 + lane;
-        key[j] = (uint32_t)j * 64 < per_wave && place[j] < a.T ? key_at(a, place[j]) : 0u;
+    for (int u = 0; u < kRangeRounds; ++u) {
+        const uint32_t i = from + u * 64 + lane;
+        key[u] = (uint32_t)u * 64 < per_wave && i < a.T ? key_at(a, i) : kNone;
     }
-    for (int pass = 0; pass < passes; ++pass) {
-        const int shift = pass * a.bits;
-        for (uint32_t d = threadIdx.x; d < kSortWaves * (1u << kMaxDigit); d += kSortThreads) (&cursor[0][0])[d] = 0;
-        __syncthreads();
+    for (uint32_t d = threadIdx.x; d < kSortWaves * digits; d += kSortThreads) cursor[d >> a.bits][d & (digits - 1)] = 0;
+    uint32_t below = 0, count = 0;
 #pragma unroll
-        for (int j = 0; j < kSmallEntries; ++j)
-            if ((uint32_t)j * 64 < per_wave && wave * per_wave + j * 64 + lane < a.T) atomicAdd(&cursor[wave][key[j] >> shift & (digits - 1)], 1u);
-        __syncthreads();
-        uint32_t all = 0;
-        if (threadIdx.x < digits)
-            for (int w = 0; w < kSortWaves; ++w) all += cursor[w][threadIdx.x];
-        uint32_t base = smaller_digits(all, wave_total);
-        if (threadIdx.x < digits)
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = cursor[w][threadIdx.x];
-                cursor[w][threadIdx.x] = base;
-                base += c;
-            }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kSmallEntries; ++j)
-            if ((uint32_t)j * 64 < per_wave) {
-                const bool in = wave * per_wave + j * 64 + lane < a.T;
-                const uint32_t at = take_place(cursor[wave], key[j] >> shift & (digits - 1), a.bits, in);
-                if (in) {
-                    keys[at] = key[j];
-                    places[at] = place[j];
-                }
-            }
-        __syncthreads();
-        const bool last = pass == passes - 1;
-#pragma unroll
-        for (int j = 0; j < kSmallEntries; ++j) {
-            const uint32_t i = wave * per_wave + j * 64 + lane;
-            if ((uint32_t)j * 64 < per_wave && i < a.T) {
-                key[j] = keys[i];
-                place[j] = places[i];
-                if (last) {
-                    a.key_out[i] = key[j];
-                    a.place_out[i] = place[j];
-                }
-            }
+    for (int u = 0; u < kRangeRounds; ++u) {
+        below += (uint32_t)__popcll(__ballot(key[u] < start));
+        const bool in = key[u] - start < digits;
+        const uint64_t those = __ballot(in);
+        if (in) kept[wave][count + (uint32_t)__popcll(those & ((1ull << lane) - 1))] = (key[u] - start) << 16 | (uint32_t)(u * 64 + lane);
+        count += (uint32_t)__popcll(those);
+    }
+    if (lane == 0) wave_below[wave] = below;
+    __syncthreads();
+    for (uint32_t e = lane; e < count; e += 64) atomicAdd(&cursor[wave][kept[wave][e] >> 16], 1u);
+    __syncthreads();
+    uint32_t all = 0;
+    if (threadIdx.x < digits)
+        for (int w = 0; w < kSortWaves; ++w) all += cursor[w][threadIdx.x];
+    uint32_t base = smaller_digits(all, wave_total);
+    for (int w = 0; w < kSortWaves; ++w) base += wave_below[w];
+    if (threadIdx.x < digits)
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = cursor[w][threadIdx.x];
+            cursor[w][threadIdx.x] = base;
+            base += c;
+        }
+    __syncthreads();
+    for (uint32_t first = 0; first < count; first += 64) {
+        const bool in = first + lane < count;
+        const uint32_t k = in ? kept[wave][first + lane] : 0u;
+        const uint32_t at = take_place(cursor[wave], k >> 16, a.bits, in);
+        if (in) {
+            a.key_out[at] = start + (k >> 16);
+            a.place_out[at] = from + (k & 0xFFFFu);
         }
     }
 }
@@ -229,7 +226,7 @@ __device__ __forceinline__ void add_rows(const float *rows, int64_t stride, uint
     }
 }
 
-constexpr int kRows = 32;       // table rows of a workgroup that looks for rows without tokens
+constexpr int kRows = 256;      // most table rows of a workgroup that looks for rows without tokens
 
 // the number of keys below `row` among `count` of them, by the whole workgroup: 256 samples at a time
 __device__ __forceinline__ uint32_t keys_below(const uint32_t *keys, uint32_t count, int64_t row, uint32_t *lds)
@@ -259,10 +256,12 @@ struct SumCall {
     int64_t V;
     int n, lanes;
     unsigned piece_blocks;
+    int zero_rows;
     float scale;
 };
 
-// The first piece_blocks workgroups have the pieces, 256 / lanes each; the others 32 table rows each, which they zero where no token names them.
+// The first piece_blocks workgroups have the pieces, 256 / lanes each; the others zero_rows table rows each (32 KB, 32 rows at least), which they zero
+// where no token names them.
 // WAVES: a row takes whole waves (64 lanes and more): ids and places of a piece are then in scalar registers.
 template <class Y, class G, bool WAVES>
 __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y *gy, G *gtable)
@@ -270,9 +269,10 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
     __shared__ uint32_t lds[4], here[kRows];
     const int n = a.n, lanes = a.lanes, worker = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     if (blockIdx.x >= a.piece_blocks) {
-        const int64_t first = (int64_t)(blockIdx.x - a.piece_blocks) * kRows;
-        const uint32_t begin = keys_below(a.keys, a.T, first, lds), rest = keys_below(a.keys + begin, a.T - begin, first + kRows, lds);
-        if (threadIdx.x < kRows) {
+        const int rows = a.zero_rows;
+        const int64_t first = (int64_t)(blockIdx.x - a.piece_blocks) * rows;
+        const uint32_t begin = keys_below(a.keys, a.T, first, lds), rest = keys_below(a.keys + begin, a.T - begin, first + rows, lds);
+        if ((int)threadIdx.x < rows) {
             uint32_t lo = begin, hi = begin + rest;
             while (lo < hi) {
                 const uint32_t mid = lo + (hi - lo) / 2;
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256) void embedding_piece_kernel(SumCall a, const Y
         __syncthreads();
         const float zeros[8] = {};
         constexpr bool kPairZero = is_float<G>;
-        for (int r = worker; r < kRows && first + r < a.V; r += 256 / lanes)
+        for (int r = worker; r < rows && first + r < a.V; r += 256 / lanes)
             if (!here[r])
                 for (int base = 0; base < n; base += lanes * 8) store_eight<kPairZero, true>(gtable + (first + r) * n, base, lane, lanes, n, zeros);
         return;
@@ -427,6 +427,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtabl
 // ---- workspace ------------------------------------------------------------------------------
 
 struct Layout {
+    int ranges, range_bits;     // of ids, where one launch sorts; 0: by digits
     int passes, bits, blocks;
     uint32_t per_block;
     size_t counts, starts, keys[2], places[2], fragments, groups, bytes;
@@ -444,6 +445,10 @@ Layout layout_of(int64_t T, int64_t V, int n)
     per = per < 1 ? kSortThreads : div_up(per, (int64_t)kSortThreads) * kSortThreads;
     l.per_block = (uint32_t)per;
     l.blocks = (int)div_up(T, per);
+    // about 64 ranges, of 16 .. 1024 ids
+    l.range_bits = bits - 6 < 4 ? 4 : bits - 6 > kMaxDigit ? kMaxDigit : bits - 6;
+    const int64_t ranges = (V >> l.range_bits) + 1;
+    l.ranges = T <= (l.passes > 1 ? kRangeTokens : kRangeTokens / 2) && ranges <= kRanges ? (int)ranges : 0;
     l.second = T >= 128 * kPiece * kPiece;
     size_t at = 0;
     const auto take = [&at](size_t bytes) {
@@ -501,10 +506,12 @@ hipError_t launch_sums(const Layout &l, int64_t T, int64_t V, int n, const uint3
     a.n = n;
     a.lanes = lanes_of_row(n) < 256 ? lanes_of_row(n) : 256;
     a.piece_blocks = div_up(a.pieces, 256u / (unsigned)a.lanes);
+    const int64_t zero_rows = 32768 / ((int64_t)n * (int64_t)sizeof(G));
+    a.zero_rows = zero_rows < 32 ? 32 : zero_rows > kRows ? kRows : (int)zero_rows;
     a.scale = scale;
     {
         prof::Timed timed("embedding_pieces", st);
-        const unsigned blocks = a.piece_blocks + (unsigned)div_up(V, (int64_t)kRows);
+        const unsigned blocks = a.piece_blocks + (unsigned)div_up(V, (int64_t)a.zero_rows);
         if (a.lanes >= 64) embedding_piece_kernel<Y, G, true><<<blocks, 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
         else embedding_piece_kernel<Y, G, false><<<blocks, 256, 0, st>>>(a, (const Y *)gy, (G *)gtable);
     }
@@ -559,8 +566,20 @@ extern "C" int kan_embedding_backward(int64_t T, int64_t V, int32_t n, const int
     hipStream_t st = (hipStream_t)stream;
     char *at = (char *)ws;
     int from = 0;
-    for (int pass = 0; pass < l.passes && T > 0; ++pass) {
-        const bool small = T <= kSmallSort;
+    if (T > 0 && l.ranges) {
+        SortPass a = {};
+        a.ids = ids;
+        a.key_out = (uint32_t *)(at + l.keys[0]);
+        a.place_out = (uint32_t *)(at + l.places[0]);
+        a.starts = (uint32_t *)(at + l.starts);
+        a.V = V;
+        a.T = (uint32_t)T;
+        a.bits = l.range_bits;
+        prof::Timed timed("embedding_sort", st);
+        embedding_range_sort_kernel<<<l.ranges, kSortThreads, 0, st>>>(a);
+        if (hipGetLastError() != hipSuccess) return KAN_ERR_HIP;
+    }
+    for (int pass = 0; pass < l.passes && T > 0 && !l.ranges; ++pass) {
         SortPass a = {};
         a.ids = pass == 0 ? ids : nullptr;
         a.key_in = (const uint32_t *)(at + l.keys[from]);
@@ -576,12 +595,6 @@ extern "C" int kan_embedding_backward(int64_t T, int64_t V, int32_t n, const int
         a.shift = pass * l.bits;
         a.bits = l.bits;
         from = 1 - from;
-        if (small) {
-            prof::Timed timed("embedding_sort", st);
-            embedding_small_sort_kernel<<<1, kSortThreads, 0, st>>>(a, l.passes);
-            if (hipGetLastError() != hipSuccess) return KAN_ERR_HIP;
-            break;
-        }
         {
             prof::Timed timed("embedding_sort", st);
             embedding_count_kernel<<<l.blocks, kSortThreads, 0, st>>>(a);
