@@ -6,7 +6,7 @@ import ctypes
 import torch
 
 from . import binding
-from .binding import KAN_OK, KanError, _f32, _on_stream, _ptr, _stream, _workspace
+from .binding import KAN_OK, KanError, _on_stream, _ptr, _stream, _workspace
 
 EXPORTS = ["kan_block_norm_forward", "kan_block_norm_workspace_bytes", "kan_block_norm_backward", "kan_embedding_forward",
            "kan_embedding_workspace_bytes", "kan_embedding_backward", "kan_token_logprob_forward", "kan_token_logprob_workspace_bytes",
@@ -38,6 +38,7 @@ class KanTensorRef(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32)]
 
 
+F32 = torch.float32
 _lib = None
 
 
@@ -74,8 +75,15 @@ def _done(rc, where):
 
 
 def _of(t, dtype):
-    assert t is None or t.dtype == dtype, "tensors of the operator's type only"
-    return _ptr(t)
+    """The address of a tensor of the operator's type (None: no tensor)."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.is_cuda and t.is_contiguous(), "device-resident contiguous tensors of the operator's type only"
+    return t.data_ptr()
+
+
+def _of32(t):
+    return _of(t, F32)
 
 
 def _type(dtype):
@@ -89,42 +97,51 @@ def _new(shape, dtype, device, stream):
 
 # ---- norms at a block boundary --------------------------------------------------------------
 
+_descs = {}
+
+
 def block_norm_desc(spec, stream_dtype=torch.float32, branch_dtype=None):
     """KanBlockNormDesc from anything with n, norm, eps, residual_scale, gate_rows, branch."""
-    branch = TYPE_NAMES[spec.branch] if branch_dtype is None else _type(branch_dtype)
-    return KanBlockNormDesc(spec.n, NORMS[spec.norm], spec.eps, spec.residual_scale, spec.gate_rows, _type(stream_dtype), branch)
+    key = (spec.n, spec.norm, spec.eps, spec.residual_scale, spec.gate_rows, stream_dtype, branch_dtype or spec.branch)
+    d = _descs.get(key)
+    if d is None:
+        if len(_descs) >= 1024:
+            _descs.clear()
+        branch = TYPE_NAMES[spec.branch] if branch_dtype is None else _type(branch_dtype)
+        d = _descs[key] = KanBlockNormDesc(spec.n, NORMS[spec.norm], spec.eps, spec.residual_scale, spec.gate_rows, _type(stream_dtype), branch)
+    return d
 
 
-def _norm_shapes(spec, B):
-    groups = -(-B // spec.gate_rows) if spec.gate_rows > 0 else 1
-    return {n: ((groups, spec.n) if n == "gate" else (spec.n,)) for n in PARAMS}
-
-
-def _norm_rows(spec, x, f, p):
-    assert x.shape[-1] == spec.n and (f is None or f.shape == x.shape), "rows of n channels"
-    B = x.numel() // spec.n
-    for n, shape in _norm_shapes(spec, B).items():
-        t = p.get(n)
-        assert t is None or t.numel() == shape[0] * (shape[1] if len(shape) > 1 else 1), n
-    return B
-
-
-def _norm_dtype(spec, f):
-    return f.dtype if f is not None else (torch.float32 if spec.branch == "f32" else torch.bfloat16)
+def _norm_call(spec, x, f, p):
+    """(rows, type of the branch, addresses of the parameters) of a call whose shapes have been checked."""
+    n = spec.n
+    assert x.shape[-1] == n and (f is None or f.shape == x.shape), "rows of n channels"
+    B = x.numel() // n
+    at = []
+    for name in PARAMS:
+        t = p.get(name)
+        if t is None:
+            at.append(None)
+            continue
+        assert t.numel() == (n * -(-B // spec.gate_rows) if name == "gate" and spec.gate_rows > 0 else n), name
+        at.append(_of(t, F32))
+    return B, f.dtype if f is not None else F32 if spec.branch == "f32" else torch.bfloat16, at
 
 
 def kan_block_norm_forward(spec, x, f, p, x_out=None, h=None, stats=None, want_h=True, stream=None):
     """(x_out, h); p maps w_post, b_post, gate, w_pre, b_pre to tensors (missing ones: ones and zeros).  f None: x_out is x."""
     lib = load()
-    B, branch = _norm_rows(spec, x, f, p), _norm_dtype(spec, f)
-    d = block_norm_desc(spec, x.dtype, branch)
-    if f is not None and x_out is None:
+    B, branch, at = _norm_call(spec, x, f, p)
+    if f is None:
+        x_out = None
+    elif x_out is None:
         x_out = _new(x.shape, x.dtype, x.device, stream)
     if want_h and h is None:
         h = _new(x.shape, branch, x.device, stream)
-    q = KanBlockNormParams(*[_f32(p.get(n)) for n in PARAMS])
-    _done(lib.kan_block_norm_forward(ctypes.byref(d), B, _of(x, x.dtype), _of(f, branch), ctypes.byref(q), _of(x_out, x.dtype) if f is not None else None,
-                                     _of(h, branch), _f32(stats), _stream(stream)), "kan_block_norm_forward")
+    dtype = x.dtype
+    assert (x_out is None or x_out.numel() == x.numel()) and (h is None or h.numel() == x.numel()) and (stats is None or stats.numel() == 4 * B), "outputs of the rows"
+    _done(lib.kan_block_norm_forward(ctypes.byref(block_norm_desc(spec, dtype, branch)), B, _of(x, dtype), _of(f, branch), ctypes.byref(KanBlockNormParams(*at)),
+                                     _of(x_out, dtype), _of(h, branch), _of(stats, F32), _stream(stream)), "kan_block_norm_forward")
     return (x if f is None else x_out), h
 
 
@@ -135,23 +152,31 @@ def kan_block_norm_workspace_bytes(spec, B):
 def kan_block_norm_backward(spec, x, f, p, stats, gx_out, gh, want=None, out=None, ws=None, stream=None):
     """All (or the wanted) gradients, named gx, gf, gw_post, ...; default: of x, of f and of every parameter in p."""
     lib = load()
-    B, branch = _norm_rows(spec, x, f, p), _norm_dtype(spec, f)
-    d = block_norm_desc(spec, x.dtype, branch)
-    names = ("w_pre", "b_pre") if f is None else PARAMS
+    B, branch, at = _norm_call(spec, x, f, p)
+    dtype = x.dtype
+    d = block_norm_desc(spec, dtype, branch)
     if want is None:
-        want = ["gx"] + ([] if f is None else ["gf"]) + ["g" + n for n in names if p.get(n) is not None]
-    out, shapes = dict(out or {}), _norm_shapes(spec, B)
+        want = ("gx",) if f is None else ("gx", "gf")
+        want += tuple(["g" + n for n in (PARAMS[3:] if f is None else PARAMS) if p.get(n) is not None])
+    out = dict(out or ())
     for name in want:
         if name not in out:
-            out[name] = _new(x.shape, x.dtype if name == "gx" else branch, x.device, stream) if name in ("gx", "gf") else _new(
-                shapes[name[1:]], torch.float32, x.device, stream)
-    if ws is None and any(out.get("g" + n) is not None for n in PARAMS):
+            if name in ("gx", "gf"):
+                out[name] = _new(x.shape, dtype if name == "gx" else branch, x.device, stream)
+            else:
+                rows = -(-B // spec.gate_rows) if spec.gate_rows > 0 else 1
+                out[name] = _new((rows, spec.n) if name == "ggate" else (spec.n,), F32, x.device, stream)
+    grads = [out.get("g" + n) for n in PARAMS]
+    for name, t in zip(PARAMS, grads):
+        assert t is None or t.numel() == (spec.n * -(-B // spec.gate_rows) if name == "gate" and spec.gate_rows > 0 else spec.n), "g" + name
+    gx, gf = out.get("gx"), out.get("gf")
+    assert all([t is None or t.numel() == x.numel() for t in (gx, gf, gx_out, gh)]) and stats.numel() == 4 * B, "gradients of the rows"
+    if ws is None and any([t is not None for t in grads]):
         ws = _workspace(lib.kan_block_norm_workspace_bytes(ctypes.byref(d), B), x.device, stream)
-    q = KanBlockNormParams(*[_f32(p.get(n)) for n in PARAMS])
-    g = KanBlockNormGrads(*[_f32(out.get("g" + n)) for n in PARAMS])
-    _done(lib.kan_block_norm_backward(ctypes.byref(d), B, _of(x, x.dtype), _of(f, branch), ctypes.byref(q), _f32(stats), _of(gx_out, x.dtype),
-                                      _of(gh, branch), _of(out.get("gx"), x.dtype), _of(out.get("gf"), branch), ctypes.byref(g), _ptr(ws),
-                                      0 if ws is None else ws.numel(), _stream(stream)), "kan_block_norm_backward")
+    _done(lib.kan_block_norm_backward(ctypes.byref(d), B, _of(x, dtype), _of(f, branch), ctypes.byref(KanBlockNormParams(*at)), _of(stats, F32),
+                                      _of(gx_out, dtype), _of(gh, branch), _of(gx, dtype), _of(gf, branch),
+                                      ctypes.byref(KanBlockNormGrads(*[_of(t, F32) for t in grads])), _ptr(ws), 0 if ws is None else ws.numel(),
+                                      _stream(stream)), "kan_block_norm_backward")
     return out
 
 
@@ -218,9 +243,9 @@ def kan_token_logprob_forward(logits, ids, temperature=1.0, top=0, out=None, ws=
     if ws is None:
         need = lib.kan_token_logprob_workspace_bytes(R, V, top)
         ws = _workspace(need, dev, stream) if need else None
-    _done(lib.kan_token_logprob_forward(R, V, at, _type(logits.dtype), stride, _of(ids, torch.int64), temperature, top, _f32(out["logp"]),
-                                        _f32(out["entropy"]), _f32(out["stats"]), _of(out["top_ids"], torch.int64) if top > 0 else None,
-                                        _f32(out["top_logp"]) if top > 0 else None, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
+    _done(lib.kan_token_logprob_forward(R, V, at, _type(logits.dtype), stride, _of(ids, torch.int64), temperature, top, _of32(out["logp"]),
+                                        _of32(out["entropy"]), _of32(out["stats"]), _of(out["top_ids"], torch.int64) if top > 0 else None,
+                                        _of32(out["top_logp"]) if top > 0 else None, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
           "kan_token_logprob_forward")
     return out
 
@@ -232,8 +257,8 @@ def kan_token_logprob_backward(logits, ids, fwd, g_logp=None, g_entropy=None, te
     if glogits is None:
         glogits = _new((R, V), logits.dtype, logits.device, stream)
     assert glogits.numel() == R * V, "rows of V gradients"
-    _done(load().kan_token_logprob_backward(R, V, at, _type(logits.dtype), stride, _of(ids, torch.int64), temperature, _f32(fwd["stats"]),
-                                            _f32(fwd["entropy"]), _f32(g_logp), _f32(g_entropy), _of(glogits, logits.dtype), _stream(stream)),
+    _done(load().kan_token_logprob_backward(R, V, at, _type(logits.dtype), stride, _of(ids, torch.int64), temperature, _of32(fwd["stats"]),
+                                            _of32(fwd["entropy"]), _of32(g_logp), _of32(g_entropy), _of(glogits, logits.dtype), _stream(stream)),
           "kan_token_logprob_backward")
     return glogits
 
@@ -256,7 +281,7 @@ def kan_gradient_norm(tensors, norm=None, ws=None, stream=None):
     lib, refs = load(), _tensor_list(tensors, tensors)
     norm = _new((), torch.float32, tensors[0].device, stream) if norm is None else norm
     ws = _workspace(lib.kan_clip_workspace_bytes(len(tensors)), norm.device, stream) if ws is None else ws
-    _done(lib.kan_gradient_norm(len(tensors), refs, _f32(norm), _ptr(ws), ws.numel(), _stream(stream)), "kan_gradient_norm")
+    _done(lib.kan_gradient_norm(len(tensors), refs, _of32(norm), _ptr(ws), ws.numel(), _stream(stream)), "kan_gradient_norm")
     return norm
 
 
@@ -265,5 +290,5 @@ def kan_clip_gradients(tensors, max_norm, out=None, norm=None, ws=None, stream=N
     lib, refs = load(), _tensor_list(tensors, tensors if out is None else out)
     norm = _new((), torch.float32, tensors[0].device, stream) if norm is None else norm
     ws = _workspace(lib.kan_clip_workspace_bytes(len(tensors)), norm.device, stream) if ws is None else ws
-    _done(lib.kan_clip_gradients(len(tensors), refs, max_norm, _f32(norm), _ptr(ws), ws.numel(), _stream(stream)), "kan_clip_gradients")
+    _done(lib.kan_clip_gradients(len(tensors), refs, max_norm, _of32(norm), _ptr(ws), ws.numel(), _stream(stream)), "kan_clip_gradients")
     return norm
