@@ -232,7 +232,7 @@ __device__ __forceinline__ void read_ahead(RowsAhead<X, F, P> &r, const NormCall
         const int base = q * TPR * 8;
         r.x[q] = eight_at<PAIR>((const X *)a.x + at, base, lane, TPR, n);
         r.f[q] = eight_at<PAIR>((const F *)a.f + at, base, lane, TPR, a.f ? n : 0);
-        r.gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + at, base, lane, TPR, a.gx_out ? n : 0);
+        if (TPR < 1024) r.gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + at, base, lane, TPR, a.gx_out ? n : 0);
         r.gh[q] = eight_at<PAIR>((const F *)a.gh + at, base, lane, TPR, a.gh ? n : 0);
     }
 #pragma unroll
@@ -324,7 +324,9 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             unpack_at<PAIR>(next.x[q], q * TPR * 8, lane, TPR, n, v[q]);
             unpack_at<PAIR>(next.f[q], q * TPR * 8, lane, TPR, n, fhat[q]);
             unpack_at<PAIR>(next.gh[q], q * TPR * 8, lane, TPR, n, g[q]);
-            gx_out[q] = next.gx_out[q];
+            // with 128 registers a lane it is read now; it is needed behind the first sum
+            if (TPR < 1024) gx_out[q] = next.gx_out[q];
+            else gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + row * n, q * TPR * 8, lane, TPR, a.gx_out && live ? n : 0);
         }
         read_ahead<X, F, TPR, P>(next, a, row + 1, row + 1 < end, lane);
         if (a.f) {
