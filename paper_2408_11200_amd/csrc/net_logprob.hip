@@ -452,11 +452,12 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, float temperat
     return KAN_OK;
 }
 
-// How a row is cut: few rows of a large vocabulary are shared among workgroups, four a CU, of 4096 logits at least.  16 x 32768 bf16 with five
-// alternatives in one piece a row 14.8 us, in eight 8.0 (a launch more); 1 x 131072 22.6 and 9.2.
+// How a row is cut: few rows of a large vocabulary are shared among workgroups, four a CU, of 4096 logits at least, and joined by a launch more.
+// Whole and cut, bf16, us: 1 x 131072 with five alternatives 29.1 and 11.9, without 25.6 and 7.9; 64 x 131072 with twenty 35.0 and 20.7;
+// 16 x 32768 11.8 and 10.9, 128 x 32768 12.0 and 14.0; 1 x 16384 8.6 and 10.0; 400 x 100000 fp32 49.7 and 42.1.
 int parts_of(int64_t R, int64_t V)
 {
-    if (R <= 0 || R > 512 || V < 8192) return 1;
+    if (R <= 0 || R > 512 || V < (R <= 32 ? 32768 : 65536)) return 1;
     int64_t parts = 1024 / R;
     if (parts > V / 4096) parts = V / 4096;
     return (int)(parts > 64 ? 64 : parts);

@@ -2,6 +2,7 @@
 // record (a server's calls) the node is passed by and nothing is kept.
 #include "kan_torch.hpp"
 #include "kan_net.h"
+#include <c10/core/DeviceGuard.h>
 
 namespace {
 
@@ -47,6 +48,9 @@ void together(std::initializer_list<const Tensor *> tensors)
     for (const Tensor *t : tensors)
         if (t->defined() && t->device() != first.device()) refuse("tensors on one device only");
 }
+
+// backward(create_graph=True) would take these gradients for constants
+void first_derivatives_only(const char *what) { TORCH_CHECK(!at::GradMode::is_enabled(), what, ": gradients of gradients are not available"); }
 
 // ---- block norm -----------------------------------------------------------------------------
 
@@ -99,6 +103,7 @@ struct BlockNorm : torch::autograd::Function<BlockNorm> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        first_derivatives_only("block_norm");
         const NormCall c = unpack<NormCall>(ctx->saved_data["call"]);
         const variable_list saved = ctx->get_saved_variables();
         const Tensor x = whole(saved[0]), f = whole(saved[1]);
@@ -138,6 +143,7 @@ variable_list block_norm(const Tensor &x, const Maybe &f, const Maybe &w_post, c
     same(n > 0 && x.dim() >= 1 && x.size(-1) == n, "x: rows of n channels");
     same(!branch.defined() || branch.sizes() == x.sizes(), "f: the shape of x");
     together({&x, &branch, &p[0], &p[1], &p[2], &p[3], &p[4]});
+    const c10::DeviceGuard on(x.device());
     same(branch.defined() || want_h, "no branch and no norm behind it: nothing to compute");
     const int64_t B = x.numel() / n, groups = gate_rows > 0 ? (B + gate_rows - 1) / gate_rows : 1;
     for (int i = 0; i < 5; ++i) same(!p[i].defined() || p[i].numel() == (i == 2 ? groups * n : n), kNames[i]);
@@ -178,6 +184,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        first_derivatives_only("embedding");
         variable_list g(4);
         if (!ctx->needs_input_grad(1)) return g;
         const Tensor ids = whole(ctx->get_saved_variables()[0]), gy = whole(grads[0]);
@@ -197,6 +204,7 @@ Tensor embedding(const Tensor &ids, const Tensor &table, double scale, at::Scala
 {
     same(table.dim() == 2 && table.size(0) > 0 && table.size(1) > 0 && table.size(1) < (1ll << 31), "table: rows of n channels");
     together({&table, &ids});
+    const c10::DeviceGuard on(table.device());
     return recorded({&table}) ? Embedding::apply(ids, table, scale, out) : embedding_rows(ids, table, scale, out);
 }
 
@@ -264,6 +272,7 @@ struct TokenLogprob : torch::autograd::Function<TokenLogprob> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
+        first_derivatives_only("token_logprob");
         variable_list g(3);
         const Tensor g_logp = whole(grads[0]), g_entropy = whole(grads[1]);
         if (!ctx->needs_input_grad(0) || (!g_logp.defined() && !g_entropy.defined())) return g;
@@ -285,6 +294,7 @@ variable_list token_logprob(const Tensor &logits, const Tensor &ids, double temp
     same(ids.sizes() == logits.sizes().slice(0, logits.dim() - 1), "ids: one for each row of logits");
     same(top >= 0 && top <= logits.size(-1) && top <= KAN_TOP_MAX, "top: at most 64 and at most the vocabulary");
     together({&logits, &ids});
+    const c10::DeviceGuard on(logits.device());
     const LogprobCall c = {temperature, top};
     if (recorded({&logits})) return TokenLogprob::apply(logits, ids, c);
     const LogprobRows r = logprob_forward(logits, ids, c, false);
@@ -309,6 +319,7 @@ Tensor clip_gradients(const std::vector<Tensor> &grads, double max_norm, const s
         same(g.device() == grads[0].device(), "gradients on one device");
         list[i] = {g.data_ptr(), o.data_ptr(), g.numel(), type_of(g.scalar_type())};
     }
+    const c10::DeviceGuard on(grads[0].device());
     const Tensor norm = at::empty({}, grads[0].options().dtype(at::kFloat));
     const Tensor ws = bytes_like(norm, kan_clip_workspace_bytes((int32_t)list.size()));
     check(kan_clip_gradients((int32_t)list.size(), list.data(), (float)max_norm, f32(norm), ws.data_ptr(), (size_t)ws.numel(), stream()),

@@ -491,6 +491,22 @@ def test_clip_through_autograd_module():
         autograd.clip_gradients(tensors[:2], 1.0, out=tensors[:1])
 
 
+def test_second_derivatives_are_refused():
+    """not silently taken for zero"""
+    z, ids, a, b = logit_case(4, 30, 1)
+    z = z.clone().requires_grad_(True)
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        torch.autograd.grad(autograd.token_logprob(z, ids)[0].sum(), z, create_graph=True)
+    spec, t, p = norm_case(4, 30, "rms", 0, 1)
+    x = t["x"].clone().requires_grad_(True)
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        torch.autograd.grad(autograd.block_norm(spec, x, t["f"], **p)[1].sum(), x, create_graph=True)
+    ids, table, _ = embed_case(5, 6, 7, 1)
+    table.requires_grad_(True)
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        torch.autograd.grad(autograd.embedding(ids, table).sum(), table, create_graph=True)
+
+
 # ---- streams and graphs ---------------------------------------------------------------------
 
 def test_operators_on_another_stream():
