@@ -7,9 +7,10 @@
 // of what little the others add (one multiply-add with a rounded reference would be an instruction less, and lose them).
 // Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.
 //
-// The most likely tokens come out of the same read: a thread's largest logit is the best of its pieces, so the top ones of the row all lie with
-// the `top` threads whose bests are the largest (and those that tie with the last).  These threads' pieces are read again, from L2, and the
-// logits that reach the last of the bests, hardly more than `top`, are put in order by counting for each how many are above it.
+// The most likely tokens come out of the same read.  The `top`-th largest of the threads' largest logits is a bound that `top` logits reach: after
+// the first round of pieces, still in registers, those that reach its bound are kept, and of every later piece those that reach it; behind
+// the row the bound of all of it leaves hardly more than `top` of them, put in order by counting for each how many are above it.  (Reading
+// the pieces of the threads that have the bound once more, at the end, cost a quarter of the row: they lie in as many lines.)
 #include "net_device.hpp"
 
 namespace kannet {
@@ -205,9 +206,9 @@ __device__ __forceinline__ int above(const uint64_t *keys, uint32_t count, uint6
 
 constexpr int kAhead = 4;
 
-// one piece: N logits
+// one piece: N logits; the largest of them
 template <int N>
-__device__ __forceinline__ void add_piece(const float (&v)[N], float scale, Sums &s, float &most)
+__device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Sums &s, float &most)
 {
     float m = v[0];
 #pragma unroll
@@ -222,6 +223,7 @@ __device__ __forceinline__ void add_piece(const float (&v)[N], float scale, Sums
         s.s += e;
         s.t += e * fmaxf(y, kFar);
     }
+    return m;
 }
 
 // What a row, or a part of one, leaves for the wave that writes the results: its sums, and the keys of its most likely tokens, one a lane.
@@ -252,8 +254,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
     constexpr int kWaves = NT / 64, N = 16 / sizeof(T);
     __shared__ Sums wave_sums[kWaves];
     constexpr uint32_t kCandidates = 4 * NT;
-    __shared__ uint64_t best[kCandidates], chosen[KAN_TOP_MAX];
-    __shared__ uint32_t candidates, sources;
+    __shared__ uint64_t best[kCandidates], shortlist[NT], chosen[KAN_TOP_MAX];
+    __shared__ uint32_t candidates, kept, sources;
     __shared__ uint16_t source[NT];
     __shared__ float thread_most[NT];
     const int64_t row = blockIdx.y * 65535ll + blockIdx.x / a.parts;
@@ -280,8 +282,28 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
             next[u] = raw_at<N, STREAM>(z, (int64_t)p * N, p < end ? a.V : 0);
         }
     };
+    const auto logits_of = [&](Raw<T, N> r, uint32_t p, float (&v)[N]) {
+        settle(r, (int64_t)p * N, a.V);
+        unpack(r, v);
+        if (p >= whole)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = p * N + k < V ? v[k] : -INFINITY;
+    };
+    // the candidates: all logits that are not below the `top`-th largest of the threads' largest ones in the first round
+    float bound = NAN;
+    const auto collect = [&](const float (&v)[N], uint32_t p) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (v[k] >= bound && p * N + k < V) {
+                const uint32_t slot = atomicAdd(&candidates, 1u);
+                if (slot < kCandidates) best[slot] = key_of(v[k], p * N + k);
+            }
+    };
+    if (tid == 0) sources = candidates = kept = 0;
+    if (tid < KAN_TOP_MAX) chosen[tid] = 0;
     read(begin + tid);
-    for (uint32_t at = begin + tid; at < end; at += kAhead * NT) {
+    for (uint32_t first = begin; first < end; first += kAhead * NT) {
+        const uint32_t at = first + tid;
         Raw<T, N> now[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) now[u] = next[u];
@@ -291,12 +313,21 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
             const uint32_t p = at + u * NT;
             if (p < end) {
                 float v[N];
-                settle(now[u], (int64_t)p * N, a.V);
-                unpack(now[u], v);
-                if (p >= whole)
+                logits_of(now[u], p, v);
+                if (add_piece<N>(v, scale, s, most) >= bound) collect(v, p);
+            }
+        }
+        if (a.top && first == begin) {
+            bound = value_of_rank<NT>(most, a.top, lane, thread_most);
+            if (NT == 64) __syncthreads();          // the counters above
 #pragma unroll
-                    for (int k = 0; k < N; ++k) v[k] = p * N + k < V ? v[k] : -INFINITY;
-                add_piece<N>(v, scale, s, most);
+            for (int u = 0; u < kAhead; ++u) {
+                const uint32_t p = at + u * NT;
+                if (p < end) {
+                    float v[N];
+                    logits_of(now[u], p, v);
+                    collect(v, p);
+                }
             }
         }
     }
@@ -304,52 +335,45 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
 
     uint64_t found = 0;
     if (a.top) {
-        // The threads whose largest logit is among the `top` largest of these have all logits that matter (a NaN hides in their maximum: then
-        // all threads have).
-        const bool all = s.s != s.s;
-        const float bound = all ? -INFINITY : value_of_rank<NT>(most, a.top, lane, thread_most);
-        if (tid == 0) sources = candidates = 0;
-        if (tid < KAN_TOP_MAX) chosen[tid] = 0;
+        const bool all = s.s != s.s;                // a NaN hides in the maxima
+        const bool rounds = end - begin > kAhead * NT;
+        if (rounds && !all) bound = value_of_rank<NT>(most, a.top, lane, thread_most);
         __syncthreads();
-        if (begin + tid < end && (all || most >= bound)) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
-        __syncthreads();
-        const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
-        // piece number i % each of source i / each
-        const auto piece_keys = [&](uint32_t i, uint64_t (&key)[N]) {
-            const uint32_t at = i < count ? begin + source[i / each] + i % each * NT : end;
-            float v[N];
-            Raw<T, N> r = raw_at<N>(z, (int64_t)at * N, at < end ? a.V : 0);
-            settle(r, (int64_t)at * N, at < end ? a.V : 0);
-            unpack(r, v);
-#pragma unroll
-            for (int k = 0; k < N; ++k) key[k] = at < end && at * N + k < V && !(v[k] < bound) ? key_of(v[k], at * N + k) : 0;
-        };
-        uint64_t key[N];
-        for (uint32_t i = tid; i < count; i += NT) {
-            piece_keys(i, key);
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (key[k]) {
-                    const uint32_t slot = atomicAdd(&candidates, 1u);
-                    if (slot < kCandidates) best[slot] = key[k];
-                }
-        }
-        __syncthreads();
-        if (candidates <= kCandidates) {
-            const uint32_t n = candidates;
+        uint32_t n = candidates;
+        if (!all && n <= kCandidates) {
+            // of these, the ones that reach the bound of the whole row
             for (uint32_t i = tid; i < n; i += NT) {
                 const uint64_t k = best[i];
-                const int at = above(best, n, k);
-                if (at < a.top) chosen[at] = k;
+                if (logit_of(k) >= bound) {
+                    const uint32_t slot = atomicAdd(&kept, 1u);
+                    if (slot < NT) shortlist[slot] = k;
+                }
+            }
+            __syncthreads();
+            const bool shorter = kept <= NT;
+            const uint64_t *list = shorter ? shortlist : best;
+            n = shorter ? kept : n;
+            for (uint32_t i = tid; i < n; i += NT) {
+                const uint64_t k = list[i];
+                const int place = above(list, n, k);
+                if (place < a.top) chosen[place] = k;
             }
             __syncthreads();
             if (wave == 0 && lane < (uint32_t)a.top) found = chosen[lane];
-        } else if (wave == 0) {
-            // more than there is room for (many equal logits, rows with NaN): one by one into a sorted list
-            for (uint32_t first = 0; first < count; first += 64) {
-                piece_keys(first + lane, key);
+        } else {
+            // More than there is room for (rising logits, many equal ones, rows with NaN): the pieces of the threads whose largest logit reaches
+            // the bound are read again, one after the other into a sorted list.
+            if (begin + tid < end && (all || most >= bound)) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
+            __syncthreads();
+            if (wave == 0) {
+                const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
+                for (uint32_t first = 0; first < count; first += 64) {
+                    const uint32_t i = first + lane, p = i < count ? begin + source[i / each] + i % each * NT : end;
+                    float v[N];
+                    logits_of(raw_at<N>(z, (int64_t)p * N, p < end ? a.V : 0), p, v);
 #pragma unroll
-                for (int k = 0; k < N; ++k) put_in(found, key[k], a.top, lane);
+                    for (int k = 0; k < N; ++k) put_in(found, p < end && p * N + k < V && (all || v[k] >= bound) ? key_of(v[k], p * N + k) : 0, a.top, lane);
+                }
             }
         }
     }
