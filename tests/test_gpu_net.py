@@ -362,6 +362,14 @@ def test_logprob_values(how, V, dtype):
     check_logprob(*logit_case(9, V, V, dtype, how=how), top=20)
 
 
+@pytest.mark.parametrize("how", ["normal", "ties", "rising", "falling", "equal", "special"])
+@pytest.mark.parametrize("top", [1, 20, 64])
+@pytest.mark.parametrize("dtype,V", [(F32, 9001), (BF16, 20011)])
+def test_logprob_many_rows(how, top, dtype, V):
+    """enough rows that none is cut: several rounds over each, more candidates than there is room for"""
+    check_logprob(*logit_case(600, V, V, dtype, how=how), top=top)
+
+
 @pytest.mark.parametrize("temperature", [0.05, 0.7, 30.0])
 def test_logprob_temperature(temperature):
     check_logprob(*logit_case(20, 333, 2), temperature=temperature, top=3)
