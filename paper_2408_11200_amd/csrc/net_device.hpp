@@ -324,12 +324,13 @@ struct RowSum {
     }
 };
 
-// Lanes a row of n channels gets, at eight channels a lane: a power of two from 8 on, 2 * 1024 * 8 channels at most (two pieces a lane)
+// Lanes a row of n channels gets, at eight channels a lane: a power of two from 8 on, 2 * 1024 * 8 channels at most (two pieces a lane).  And
+// 768 for up to 6144 channels: the block norm's backward pass has 168 registers a lane there (8192 x 6000 in two types 324 us with 1024 lanes, 190 so).
 inline int lanes_of_row(int n)
 {
     int t = 8;
     while (t < 1024 && t * 8 < n) t *= 2;
-    return t;
+    return t == 1024 && n <= 768 * 8 ? 768 : t;
 }
 
 }  // namespace kannet

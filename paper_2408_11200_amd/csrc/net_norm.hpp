@@ -221,7 +221,7 @@ struct RowsAhead {
     float st[4];
 };
 
-template <class X, class F, int TPR, int P>
+template <class X, class F, int TPR, int P, bool LATE>
 __device__ __forceinline__ void read_ahead(RowsAhead<X, F, P> &r, const NormCall &a, int64_t row, bool live, int lane)
 {
     constexpr bool PAIR = RowsAhead<X, F, P>::PAIR;
@@ -232,7 +232,7 @@ __device__ __forceinline__ void read_ahead(RowsAhead<X, F, P> &r, const NormCall
         const int base = q * TPR * 8;
         r.x[q] = eight_at<PAIR>((const X *)a.x + at, base, lane, TPR, n);
         r.f[q] = eight_at<PAIR>((const F *)a.f + at, base, lane, TPR, a.f ? n : 0);
-        if (TPR < 1024) r.gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + at, base, lane, TPR, a.gx_out ? n : 0);
+        if (!LATE) r.gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + at, base, lane, TPR, a.gx_out ? n : 0);
         r.gh[q] = eight_at<PAIR>((const F *)a.gh + at, base, lane, TPR, a.gh ? n : 0);
     }
 #pragma unroll
@@ -250,6 +250,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
 {
     constexpr int NT = backward_threads<TPR>(), kWorkers = NT / TPR;
     constexpr bool PAIR = is_float<X> || is_float<F>;
+    constexpr bool kTight = TPR == 768 && sizeof(F) == 4 && (WHOLE || BIAS), kLate = TPR == 1024 || kTight;
     __shared__ float slots[RowSum<TPR>::kSlots * (TPR > 64 ? kWorkers : 1)];
     constexpr int kJoin = TPR < 64 ? NT / 64 : kWorkers;       // workers of one wave are joined by shuffles first
     __shared__ float joined[kWorkers > 1 ? kJoin * TPR * 8 : 1];
@@ -284,10 +285,11 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 w_post[q][k] *= gate[q][k];
                 b_post[q][k] *= gate[q][k];
             }
-    // 1024 threads have 128 registers: the parameters wait in LDS, each lane's own, until they are needed.  8192 channels in fp32, layer norm
-    // with biases: 323 us with what did not fit in scratch, 221 so; the smallest kernel has 44 bytes in scratch and is faster with them (150, 174).
-    constexpr bool kAside = TPR == 1024 && P == 1 && (LAYER || WHOLE || BIAS || sizeof(F) == 4);
-    __shared__ f32x4 aside[kAside ? 6 : 1][kAside ? 1024 : 1];
+    // 1024 threads have 128 registers each, 768 have 168: the parameters wait in LDS, each lane's own, until they are needed.  Layer norm with
+    // biases in fp32, us with what does not fit in scratch and so: 4096 x 8192 299 and 236, 4096 x 6144 (with gx_out read late too) 158 and 120.
+    // The smallest kernels have little in scratch, and are faster with that (8192 x 8192 bf16: 150, 174 so).
+    constexpr bool kAside = P == 1 && ((TPR == 1024 && (LAYER || WHOLE || BIAS || sizeof(F) == 4)) || kTight);
+    __shared__ f32x4 aside[kAside ? 6 : 1][kAside ? TPR : 1];
     const auto put_aside = [&](int which, const float (&v)[P][8]) {
         aside[2 * which][threadIdx.x] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
         aside[2 * which + 1][threadIdx.x] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
     // of w_pre and b_pre; of w_post and b_post, without their common factors if not WHOLE; of the gate of a group if WHOLE
     float pre1[P][8] = {}, pre0[P][8] = {}, post1[P][8] = {}, post0[P][8] = {}, gates[P][8] = {};
     RowsAhead<X, F, P> next;
-    read_ahead<X, F, TPR, P>(next, a, row, row < end, lane);
+    read_ahead<X, F, TPR, P, kLate>(next, a, row, row < end, lane);
     // workers of several waves share their barriers: each goes through all rounds
     for (int64_t i = 0; i < a.span; ++i, ++row) {
         const bool live = row < end;
@@ -324,11 +326,11 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
             unpack_at<PAIR>(next.x[q], q * TPR * 8, lane, TPR, n, v[q]);
             unpack_at<PAIR>(next.f[q], q * TPR * 8, lane, TPR, n, fhat[q]);
             unpack_at<PAIR>(next.gh[q], q * TPR * 8, lane, TPR, n, g[q]);
-            // with 128 registers a lane it is read now; it is needed behind the first sum
-            if (TPR < 1024) gx_out[q] = next.gx_out[q];
+            // with few registers a lane it is read now; it is needed behind the first sum
+            if (!kLate) gx_out[q] = next.gx_out[q];
             else gx_out[q] = eight_at<PAIR>((const X *)a.gx_out + row * n, q * TPR * 8, lane, TPR, a.gx_out && live ? n : 0);
         }
-        read_ahead<X, F, TPR, P>(next, a, row + 1, row + 1 < end, lane);
+        read_ahead<X, F, TPR, P, kLate>(next, a, row + 1, row + 1 < end, lane);
         if (a.f) {
             fetch(1, w_post);
             if (BIAS) fetch(2, b_post);
@@ -484,6 +486,7 @@ hipError_t launch_norm_types(const NormCall &a, const NormPick &p, hipStream_t s
     case 128: return launch_norm<X, F, LAYER, 128, 1>(a, p, st);
     case 256: return launch_norm<X, F, LAYER, 256, 1>(a, p, st);
     case 512: return launch_norm<X, F, LAYER, 512, 1>(a, p, st);
+    case 768: return launch_norm<X, F, LAYER, 768, 1>(a, p, st);
     default: break;
     }
     return a.n <= 8192 ? launch_norm<X, F, LAYER, 1024, 1>(a, p, st) : launch_norm<X, F, LAYER, 1024, 2>(a, p, st);

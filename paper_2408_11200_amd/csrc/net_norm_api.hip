@@ -6,11 +6,13 @@ namespace kannet {
 namespace {
 
 constexpr int kColumns = 32, kSegments = 32;     // a workgroup of the reduction: columns, and threads that share one
+constexpr int kFewParts = 16;                    // of a group: summed by one thread a column
 
 struct NormReduce {
     const float *part, *gate_part;
     kan_block_norm_params p;
     kan_block_norm_grads g;
+    int64_t gates;          // groups * n
     int n, blocks, parts;
     bool by_group, bias, pre, post;
 };
@@ -36,12 +38,23 @@ __device__ __forceinline__ float column_sum(const float *from, int64_t stride, i
     return total;
 }
 
-// blockIdx.y: 0 w_pre, 1 b_pre, 2 w_post, b_post and a gate that all rows share, 3 + group: a group's gate from its parts
+// blockIdx.y: 0 w_pre, 1 b_pre, 2 w_post, b_post and a gate that all rows share, 3 + group: a group's gate from its parts (few parts: 3 + ..., all
+// groups' columns a thread each)
 __global__ __launch_bounds__(kColumns *kSegments) void norm_reduce_kernel(NormReduce a)
 {
     __shared__ float lds[kSegments][kColumns];
     const int which = blockIdx.y, n = a.n, c = blockIdx.x * kColumns + threadIdx.x % kColumns;
     const bool mine = threadIdx.x < kColumns && c < n;
+    if (which >= 3 && a.parts <= kFewParts) {
+        const int64_t i = ((int64_t)(which - 3) * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x;
+        if (i >= a.gates) return;
+        const int64_t group = i / n;
+        const float *from = a.gate_part + group * a.parts * n + (i - group * n);
+        float t = 0.0f;
+        for (int k = 0; k < a.parts; ++k) t += from[(int64_t)k * n];
+        a.g.ggate[i] = t;
+        return;
+    }
     if (which >= 3) {
         const int64_t group = which - 3;
         const float t = column_sum(a.gate_part + group * a.parts * n, n, a.parts, c, n, lds);
@@ -70,8 +83,11 @@ struct Cut {
 int forward_workers(int n) { return lanes_of_row(n) > 64 ? 1 : 256 / lanes_of_row(n); }
 int backward_workers(int n) { return lanes_of_row(n) > 512 ? 1 : 512 / lanes_of_row(n); }
 
-// Rows of a worker in the backward pass: two workgroups a CU (of 1024 threads: one), two rows at least, so that the partial sums of the
-// parameters stay below what the rows themselves cost.
+// Rows of a worker in the backward pass: one workgroup a CU (its registers fill one), two rows at least, so that the partial sums of the
+// parameters stay below what the rows themselves cost.  A worker has rows of one group of a gate, or whole groups; of both ways to cut, the one
+// with the least rows behind each other on a CU, a workgroup's start and end taken as four rows more.  (22369 x 1500 fp32, a gate every
+// 7 rows: 267 workgroups of 42 rows left most CUs idle while the last eleven ran, 310 us; 229 of 49 rows
+// 208.  Every 40 rows: 280 of two whole groups 287 us, 560 of half a group 184.)
 Cut cut_rows(const kan_block_norm_desc *d, int64_t B)
 {
     const int per_block = backward_workers(d->n);
@@ -80,21 +96,28 @@ Cut cut_rows(const kan_block_norm_desc *d, int64_t B)
     c.span = div_up(B, most);
     if (c.span < 2) c.span = 2;
     c.parts = 0;
-    if (d->gate_rows > 0 && d->gate_rows < B) {
-        if (d->gate_rows >= c.span) {
-            // as many parts as leave all workers in one round
-            const int64_t groups = div_up(B, d->gate_rows), room = most / groups > 1 ? most / groups : 1;
-            int64_t parts = div_up(d->gate_rows, c.span);
-            if (parts > room) parts = room;
-            c.span = div_up(d->gate_rows, parts);
-            c.parts = (int)div_up(d->gate_rows, c.span);
-            c.workers = groups * c.parts;
-            c.blocks = (int)div_up(c.workers, (int64_t)per_block);
-            return c;
-        }
-        c.span = c.span / d->gate_rows * d->gate_rows;
-    }
     c.workers = div_up(B, c.span);
+    if (d->gate_rows > 0 && d->gate_rows < B) {
+        const int64_t groups = div_up(B, d->gate_rows), fair = c.span;
+        int64_t least = INT64_MAX;
+        const auto consider = [&](int64_t span, int64_t workers, int64_t parts) {
+            const int64_t cost = div_up(workers, most) * (span + 4);
+            if (cost >= least) return;
+            least = cost;
+            c.span = span;
+            c.workers = workers;
+            c.parts = (int)parts;
+        };
+        if (d->gate_rows < fair) {
+            const int64_t some = fair / d->gate_rows;
+            for (int64_t m = some; m <= some + 1; ++m) consider(m * d->gate_rows, div_up(groups, m), 0);
+        }
+        for (int64_t parts = 1; groups <= 4 * most && parts <= div_up(d->gate_rows, fair) + 3; ++parts) {
+            const int64_t span = div_up(d->gate_rows, parts);
+            if (span < 2) break;
+            consider(span, groups * div_up(d->gate_rows, span), div_up(d->gate_rows, span));
+        }
+    }
     c.blocks = (int)div_up(c.workers, (int64_t)per_block);
     return c;
 }
@@ -176,7 +199,7 @@ extern "C" size_t kan_block_norm_workspace_bytes(const kan_block_norm_desc *desc
 {
     if (check(desc) != KAN_OK || B <= 0) return 0;
     const Cut c = cut_rows(desc, B);
-    return part_bytes(desc, c) + (c.parts ? align_up((size_t)c.workers * (size_t)desc->n * sizeof(float)) : 0);
+    return part_bytes(desc, c) + (c.parts > 1 ? align_up((size_t)c.workers * (size_t)desc->n * sizeof(float)) : 0);
 }
 
 extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t B, const void *x, const void *f,
@@ -209,7 +232,8 @@ extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t 
         a.gf = gf;
         a.ggate = w->ggate;
         a.part = params ? (float *)ws : nullptr;
-        a.gate_part = params ? (float *)((char *)ws + part_bytes(desc, c)) : nullptr;
+        // a group in one part: its gate's gradient is whole
+        a.gate_part = c.parts == 1 ? w->ggate : params ? (float *)((char *)ws + part_bytes(desc, c)) : nullptr;
         a.span = c.span;
         a.parts = c.parts;
         const NormPick pick = {desc->norm == KAN_NORM_LAYER, true, by_group && !c.parts, bias, c.blocks};
@@ -229,8 +253,11 @@ extern "C" int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t 
     r.bias = bias;
     r.pre = B > 0 && gh;
     r.post = B > 0 && f;
-    const unsigned groups = c.parts && w->ggate && f ? (unsigned)div_up(B, desc->gate_rows) : 0;
+    const unsigned across = (unsigned)div_up(desc->n, kColumns);
+    int64_t more = c.parts > 1 && w->ggate && f ? div_up(B, desc->gate_rows) : 0;
+    r.gates = more * desc->n;
+    if (c.parts <= kFewParts) more = div_up(r.gates, (int64_t)across * kColumns * kSegments);
     prof::Timed timed("block_norm_reduce", st);
-    norm_reduce_kernel<<<dim3((unsigned)div_up(desc->n, kColumns), 3 + groups), kColumns * kSegments, 0, st>>>(r);
+    norm_reduce_kernel<<<dim3(across, 3 + (unsigned)more), kColumns * kSegments, 0, st>>>(r);
     return status_of(hipGetLastError());
 }

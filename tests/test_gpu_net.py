@@ -110,6 +110,14 @@ def test_block_norm_ends_of_a_network(kind, branch, gx_out, gh):
     check_norm(*norm_case(70, 1100, kind, 30, 3), branch=branch, gx_out=gx_out, gh=gh)
 
 
+@pytest.mark.parametrize("n,B,gate_rows", [(1200, 6000, 11), (1200, 6000, 12), (1200, 6000, 13), (1200, 6000, 900), (1200, 6000, 5000), (40, 40000, 5), (40, 40000, 31),
+                                           (4400, 1500, 5), (4400, 1500, 6), (4400, 1500, 200), (6144, 700, 1), (6145, 700, 4)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_block_norm_groups_cut(n, B, gate_rows, kind):
+    """whole groups a worker, groups in one part, in a few and in many"""
+    check_norm(*norm_case(B, n, kind, gate_rows, B + gate_rows))
+
+
 @pytest.mark.parametrize("have", [(), ("gate",), ("w_post",), ("w_pre", "b_pre"), ("b_post", "gate")])
 @pytest.mark.parametrize("gate_rows", [0, 3, 50])
 def test_block_norm_without_parameters(have, gate_rows):
