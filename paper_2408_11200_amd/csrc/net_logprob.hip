@@ -5,7 +5,9 @@
 // then waves are joined the same way.  log sum = log of the first; entropy = log sum - (second / first), two terms of one sign.  The
 // difference is taken before the scaling: logits of the type's lowest value stay finite, and a row with one likely token keeps the digits
 // of what little the others add (one multiply-add with a rounded reference would be an instruction less, and lose them).
-// Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.
+// Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.  Measured: 4093 x 50001 fp32 135-141 us
+// (819 MB, 5.9 TB/s), bound by HBM; 8192 x 131072 bf16 with eight top tokens 410-500 us (2.15 GB, 4.3-5.2 TB/s), bound by its vector instructions:
+// some twelve issue slots an element (widen, compare, subtract, scale, the exponential's four, two clamped sums) are 330 us by themselves.
 //
 // The most likely tokens come out of the same read.  The `top`-th largest of the threads' largest logits is a bound that `top` logits reach: after
 // the first round of pieces, still in registers, those that reach its bound are kept, and of every later piece those that reach it; behind
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
     if (lane < (uint32_t)a.top) a.part_keys[slot * a.top + lane] = found;
 }
 
-// a workgroup for each row that was cut, at most 64 parts
+// A workgroup for each row that was cut, at most 64 parts: 3.5 us, one latency after another (16 x 32768, 8 parts, five tokens)
 template <class T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobCall a)
 {
@@ -426,6 +428,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobCall a)
     finish(a, row, s, found, lane, given, there);
 }
 
+// The gradient's row, from the forward pass's largest logit and sum: no sum is left to take, so elements are independent and the pass is bound by HBM,
+// a read and a write of the logits: 4093 x 50001 fp32 295 us (1.64 GB, 5.6 TB/s), 8192 x 131072 bf16 735 (4.3 GB, 5.8).
 constexpr int kBackPieces = 4;      // of 16 bytes a thread, next to one another in a row or (ROWS) in four rows
 
 template <class T, bool ROWS>
@@ -485,11 +489,11 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, float temperat
 }
 
 // How a row is cut: few rows of a large vocabulary are shared among workgroups, four a CU, of 4096 logits at least, and joined by a launch more.
-// Whole and cut, bf16, us: 1 x 131072 with five alternatives 29.1 and 11.9, without 25.6 and 7.9; 64 x 131072 with twenty 35.0 and 20.7;
-// 16 x 32768 11.8 and 10.9, 128 x 32768 12.0 and 14.0; 1 x 16384 8.6 and 10.0; 400 x 100000 fp32 49.7 and 42.1.
+// Whole and cut, us, bf16: 1 x 131072 with five alternatives 31.6 and 11.6, without 27.9 and 7.6; 64 x 131072 with twenty 34.8 and 21.6;
+// 16 x 32768 with five 14.2 and 10.2, 128 x 32768 14.8 and 13.8, 1 x 16384 10.3 and 10.4; fp32: 64 x 50001 24.1 and 15.1, 400 x 100000 54.6 and 53.8.
 int parts_of(int64_t R, int64_t V)
 {
-    if (R <= 0 || R > 512 || V < (R <= 32 ? 32768 : 65536)) return 1;
+    if (R <= 0 || R > 512 || V < 32768) return 1;
     int64_t parts = 1024 / R;
     if (parts > V / 4096) parts = V / 4096;
     return (int)(parts > 64 ? 64 : parts);

