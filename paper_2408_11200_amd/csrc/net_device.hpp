@@ -283,15 +283,23 @@ __device__ __forceinline__ float lane_sum(float v)
     return t.x + t.y;
 }
 
-// Sums of N values over the TPR lanes that share a row: within a wave, or over the TPR / 64 waves of the workgroup through LDS, with one
-// barrier a call (two sets of slots taken in turn: a wave that writes a set again has passed the barrier of the call in between, and
-// with it every wave's reads of that set).
+// Sums of N values over the lanes that share a row, TPR at most: within a wave, or over the waves through LDS, with one barrier a call (two
+// sets of slots taken in turn: a wave that writes a set again has passed the barrier of the call in between, and with it every wave's
+// reads of that set).  Slots of waves that are not there hold zeros from clear() on.
 template <int TPR>
 struct RowSum {
-    static constexpr int kWaves = TPR / 64, kMost = 2;
+    static constexpr int kWaves = TPR > 512 ? 16 : TPR > 64 ? TPR / 64 : 1, kMost = 2;
     static constexpr int kSlots = TPR > 64 ? 2 * kMost * kWaves : 1;
     float *slots;       // [2][kWaves][kMost]
-    int turn = 0;
+    int turn = 0, wave = 0;
+    __device__ __forceinline__ void clear(int lane)
+    {
+        if constexpr (TPR > 64) {
+            wave = lane >> 6;
+            if (lane < kSlots) slots[lane] = 0.0f;
+            __syncthreads();
+        }
+    }
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N])
     {
@@ -305,15 +313,11 @@ struct RowSum {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = lane_sum<64>(v[i]);
-                if ((threadIdx.x & 63) == 0) s[(threadIdx.x % TPR >> 6) * kMost + i] = v[i];
+                if ((threadIdx.x & 63) == 0) s[wave * kMost + i] = v[i];
             }
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[i] = s[i];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) v[i] += s[w * kMost + i];
-            }
+            for (int i = 0; i < N; ++i) v[i] = lane_sum<kWaves>(s[(threadIdx.x & (kWaves - 1)) * kMost + i]);
         }
     }
     __device__ __forceinline__ float operator()(float v)

@@ -160,6 +160,7 @@ NormCall call_of(const kan_block_norm_desc *d, int64_t B, const void *x, const v
     a.B = B;
     a.gate_rows = grouped(d, B) ? d->gate_rows : 0;
     a.n = d->n;
+    a.lanes = div_up(d->n, 512) * 64;
     a.eps = d->eps;
     a.residual_scale = d->residual_scale;
     a.inv_n = 1.0f / (float)d->n;
@@ -190,8 +191,7 @@ extern "C" int kan_block_norm_forward(const kan_block_norm_desc *desc, int64_t B
     a.h = h;
     a.stats = stats;
     const int64_t blocks = div_up(B, (int64_t)forward_workers(desc->n));
-    const int64_t most = lanes_of_row(desc->n) >= 512 ? 1024 : 2048;
-    const NormPick pick = {desc->norm == KAN_NORM_LAYER, false, false, false, (int)(blocks < most ? blocks : most)};
+    const NormPick pick = {desc->norm == KAN_NORM_LAYER, false, false, false, (int)(blocks < 65536 ? blocks : 65536)};
     return status_of(launch(desc, a, pick, (hipStream_t)stream));
 }
 
