@@ -4,7 +4,7 @@
 // needs the whole row (mean, mean square, the two projections of the backward pass) is a sum over those lanes.  Workers are the groups of
 // TPR lanes; rows of up to 512 channels lie within a wave, so that their sums are DPP moves and need no barrier.  Forward and backward, us and
 // TB/s of what a pass has to move: 16384 x 512 fp32 layer norm 23.7 (5.7) and 38.8 (5.2); 8190 x 771 bf16 stream and fp32 branch, a gate each 117
-// rows, 21.3 (3.6) and 33 (3.4); 16384 x 4096 bf16 RMS norm 104 (5.2) and 152 (5.3); 4096 x 6144 fp32 90 (4.5) and 120 (5.0).
+// rows, 20.5 (3.7) and 32 (3.6); 16384 x 4096 bf16 RMS norm 104 (5.2) and 152 (5.3); 5461 x 6144 fp32 layer norm 115 (4.7) and 157 (5.1).
 #pragma once
 #include <atomic>
 #include "net_device.hpp"
@@ -299,9 +299,9 @@ __global__ __launch_bounds__(backward_threads<TPR>()) void norm_backward_kernel(
                 b_post[q][k] *= gate[q][k];
             }
     // 1024 threads have 128 registers each, 768 have 168: the parameters wait in LDS, each lane's own, until they are needed.  Layer norm with
-    // biases in fp32, us with what does not fit in scratch and so: 4096 x 8192 299 and 236, 4096 x 6144 (with gx_out read late too) 158 and 120.
-    // The smallest kernels have little in scratch, and are faster with that (8192 x 8192 bf16: 150, 174 so).
-    constexpr bool kAside = P == 1 && ((TPR == 1024 && (LAYER || WHOLE || BIAS || sizeof(F) == 4)) || kTight);
+    // biases in fp32, us with what does not fit in scratch and so: 4096 x 8192 234 and 174, 5461 x 6144 with a gate each row 405 and 233.  RMS norm
+    // without biases 164 and 155, but of a bf16 stream 110 and 115: there they stay.
+    constexpr bool kAside = P == 1 && ((TPR == 1024 && (LAYER || WHOLE || BIAS || sizeof(X) == 4)) || kTight);
     __shared__ f32x4 aside[kAside ? 6 : 1][kAside ? TPR : 1];
     const auto put_aside = [&](int which, const float (&v)[P][8]) {
         aside[2 * which][threadIdx.x] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
