@@ -283,6 +283,15 @@ __device__ __forceinline__ float lane_sum(float v)
     return t.x + t.y;
 }
 
+// the largest of each group of W lanes
+template <int W>
+__device__ __forceinline__ float lane_max(float v)
+{
+    if constexpr (W > 2) v = lane_max<W / 2>(v);
+    const f32x2 t = both_halves<W>(v);
+    return fmaxf(t.x, t.y);
+}
+
 // Sums of N values over the lanes that share a row, TPR at most: within a wave, or over the waves through LDS, with one barrier a call (two
 // sets of slots taken in turn: a wave that writes a set again has passed the barrier of the call in between, and with it every wave's
 // reads of that set).  Slots of waves that are not there hold zeros from clear() on.

@@ -60,15 +60,15 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float scale)
     return Sums{m, a.s + b.s, a.t + b.t};
 }
 
-// over a workgroup
+// over a workgroup: everyone's sums brought to the largest logit first, then plain sums (joined two by two over the lanes, each time with two
+// exponentials and three exchanges, 16384 rows of 256 took 13.2 us, 11.3 so)
 template <int NT>
 __device__ __forceinline__ Sums join_all(Sums s, float scale, Sums *lds)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const Sums o = {__shfl_xor(s.m, d, 64), __shfl_xor(s.s, d, 64), __shfl_xor(s.t, d, 64)};
-        s = join(s, o, scale);
-    }
+    const float m = lane_max<64>(s.m);
+    rescale(s, m, scale);
+    s.s = lane_sum<64>(s.s);
+    s.t = lane_sum<64>(s.t);
     if (NT == 64) return s;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
