@@ -101,7 +101,8 @@ int kan_embedding_backward(int64_t T, int64_t V, int32_t n, const int64_t *ids, 
    top <= KAN_TOP_MAX and top <= V.  Masked tokens are logits of -infinity (p = 0, no part of the entropy) or of the type's lowest
    value.  A row that is -infinity throughout has logp = -infinity (0 for an id outside), entropy 0, and for alternatives the tokens
    0 .. top-1 at -infinity.  A NaN or a +infinity in a row makes its logp, entropy and top_logp NaN (an id outside still gives 0);
-   for top_ids a NaN counts as larger than +infinity.  stats[R][2] (largest logit of the row; sum of exp(z - its z)) is for the backward pass.
+   for top_ids a NaN counts as larger than +infinity.  stats[R][2] (largest logit of the row; sum of exp(z - its z) over the other tokens) is for
+   the backward pass.  logp, entropy and the gradients keep their digits, not only their places, in rows of one likely token.
    logp, entropy, stats and the pair of top_* may be NULL; ids is read for logp only.  1e-30 <= temperature <= 1e30. */
 #define KAN_TOP_MAX 64
 int kan_token_logprob_forward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, const int64_t *ids,

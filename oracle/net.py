@@ -114,16 +114,18 @@ def token_logprob(logits, ids, temperature=1.0, top=0):
     m = np.where(empty | wrong, 0.0, np.where(wrong[:, None], 0.0, z).max(1))
     y = (np.where(wrong[:, None], 0.0, z) - m[:, None]) / temperature
     e = np.exp(y)
-    s = np.where(empty, 1.0, e.sum(1))
-    p = e / s[:, None]
-    lse = np.log(s)
-    lp = y - lse[:, None]
+    others = e.copy()
+    others[np.arange(R), y.argmax(1)] = 0.0
+    rest = np.where(empty, 0.0, others.sum(1))          # the sum but for the largest logit's 1, which it would be rounded against
+    p = e / (1.0 + rest)[:, None]
+    lp = y - np.log1p(rest)[:, None]
+    other_p = np.where((np.arange(V) == y.argmax(1)[:, None]) & ~empty[:, None], (rest / (1.0 + rest))[:, None], 1.0 - p)
     with np.errstate(invalid="ignore"):
         entropy = -np.where(p > 0, p * lp, 0.0).sum(1)
     entropy = np.where(wrong, np.nan, entropy)
     lp = np.where(wrong[:, None], np.nan, lp)
-    p = np.where(wrong[:, None], np.nan, p)
-    out = dict(entropy=entropy, p=p, lp=lp, empty=empty)
+    p, other_p = np.where(wrong[:, None], np.nan, p), np.where(wrong[:, None], np.nan, other_p)
+    out = dict(entropy=entropy, p=p, other_p=other_p, lp=lp, empty=empty)
     if ids is not None:
         ids = np.asarray(ids)
         there = (ids >= 0) & (ids < V)
@@ -146,12 +148,10 @@ def token_logprob_backward(fwd, ids, g_logp, g_entropy, temperature=1.0):
     if g_logp is not None:
         there = fwd["there"]
         a = np.where(there, np.asarray(g_logp, np.float64), 0.0)[:, None]
-        g -= a * p
-        scale += np.abs(a * p)
         hit = np.zeros_like(p)
         hit[np.arange(R)[there], np.asarray(ids)[there]] = 1.0
-        g += a * hit
-        scale += np.abs(a * hit)
+        g += np.where(hit > 0, a * fwd["other_p"], -a * p)
+        scale += np.abs(a * p) + np.abs(a * hit)
     if g_entropy is not None:
         b = np.asarray(g_entropy, np.float64)[:, None]
         with np.errstate(invalid="ignore"):

@@ -3,8 +3,12 @@
 // Forward reads a row of logits once.  Every thread keeps, over its pieces of 16 bytes, the largest logit, the sum of the exponentials
 // 2^y relative to it, y = (logit - largest) * log2(e) / temperature, and the sum of 2^y * y, rescaled when a larger one turns up; threads,
 // then waves are joined the same way.  log sum = log of the first; entropy = log sum - (second / first), two terms of one sign.  The
-// difference is taken before the scaling: logits of the type's lowest value stay finite, and a row with one likely token keeps the digits
-// of what little the others add (one multiply-add with a rounded reference would be an instruction less, and lose them).
+// difference is taken before the scaling: logits of the type's lowest value stay finite, and no digits go to a rounded reference.
+//
+// In a row with one likely token the largest logit's own 1 would round off what the others add, and with it the log probability and 1 - p of
+// that token.  Such a row (a sum below 5/4) gets the sum without that 1 for a little more reading: only the thread that has the largest logit
+// has added to it, so its pieces, one in 64 or 256, are summed once more without it and added to the other threads' sums.  From
+// there on a row is known by that rest.
 // Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.  Measured: 4093 x 50001 fp32 135-141 us
 // (819 MB, 5.9 TB/s), bound by HBM; 8192 x 131072 bf16 with eight top tokens 410-500 us (2.15 GB, 4.3-5.2 TB/s), bound by its vector instructions:
 // some twelve issue slots an element (widen, compare, subtract, scale, the exponential's four, two clamped sums) are 330 us by themselves.
@@ -26,6 +30,20 @@ struct Sums {
     float m, s, t;          // largest logit (at least the lowest finite value), sum of 2^y, sum of 2^y y
 };
 
+struct Part {
+    float m, rest, t;       // the same, but the sum less 2^0 = 1 of the largest logit; -1: nothing but -infinity
+};
+
+// Sums below this: the rest is summed without the largest logit.  What is left above it is the difference to 1, off by five times the sum's error.
+constexpr float kClear = 1.25f;
+
+// log(1 + x), by W. Kahan's correction of log for the rounding of 1 + x
+__device__ __forceinline__ float log_1p(float x)
+{
+    const float u = 1.0f + x;
+    return u == 1.0f ? x : logf(u) * (x * __builtin_amdgcn_rcpf(u - 1.0f));
+}
+
 struct LogprobCall {
     const void *logits;
     int64_t row_stride, V, R;
@@ -40,7 +58,7 @@ struct LogprobCall {
     void *glogits;
     int parts;              // of a row, in the forward pass
     uint32_t part_pieces;   // pieces of 16 bytes of a part
-    Sums *part_sums;        // [R][parts]
+    Part *part_sums;        // [R][parts]
     uint64_t *part_keys;    // [R][parts][top]
 };
 
@@ -229,16 +247,16 @@ __device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Sum
 }
 
 // What a row, or a part of one, leaves for the wave that writes the results: its sums, and the keys of its most likely tokens, one a lane.
-__device__ __forceinline__ void finish(const LogprobCall &a, int64_t row, Sums s, uint64_t found, int lane, float given, bool there)
+__device__ __forceinline__ void finish(const LogprobCall &a, int64_t row, Part s, uint64_t found, int lane, float given, bool there)
 {
-    const bool empty = s.s == 0.0f, wrong = s.s != s.s || s.m == INFINITY;
-    const float log_sum = empty ? 0.0f : logf(s.s);
+    const bool empty = s.rest == -1.0f, wrong = s.rest != s.rest || s.m == INFINITY;
+    const float log_sum = empty ? 0.0f : log_1p(s.rest);
     const auto logp_of = [&](float v) { return empty ? -INFINITY : wrong ? NAN : (v - s.m) * a.inv_temperature - log_sum; };
     if (lane == 0) {
-        if (a.entropy) a.entropy[row] = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / s.s);
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / (1.0f + s.rest));
         if (a.stats) {
             a.stats[row * 2] = empty ? -INFINITY : wrong ? NAN : s.m;
-            a.stats[row * 2 + 1] = empty ? 0.0f : s.s;
+            a.stats[row * 2 + 1] = empty ? 0.0f : s.rest;
         }
         if (a.logp) a.logp[row] = there ? logp_of(given) : 0.0f;
     }
@@ -255,6 +273,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
 {
     constexpr int kWaves = NT / 64, N = 16 / sizeof(T);
     __shared__ Sums wave_sums[kWaves];
+    __shared__ float wave_rest[kWaves];
+    __shared__ uint32_t holder;
     constexpr uint32_t kCandidates = 4 * NT;
     __shared__ uint64_t best[kCandidates], shortlist[NT], chosen[KAN_TOP_MAX];
     __shared__ uint32_t candidates, kept, sources;
@@ -335,7 +355,28 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
             }
         }
     }
+    const Sums mine = s;
     s = join_all<NT>(s, scale, wave_sums);
+    float rest = s.s - 1.0f;
+    if (s.s >= 1.0f && s.s < kClear) {              // the same in all threads; exactly one has the largest logit, and has it once
+        if (most == s.m) holder = tid;
+        __syncthreads();
+        const uint32_t h = holder;
+        rest = tid == h ? 0.0f : mine.s * __builtin_amdgcn_exp2f(fmaxf((mine.m - s.m) * scale, kFar));
+        for (uint32_t p = begin + h + tid * NT; p < end; p += NT * NT) {
+            float v[N];
+            logits_of(raw_at<N>(z, (int64_t)p * N, a.V), p, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) rest += v[k] == s.m ? 0.0f : __builtin_amdgcn_exp2f((v[k] - s.m) * scale);
+        }
+        rest = lane_sum<64>(rest);
+        if (NT > 64) {
+            if (lane == 0) wave_rest[wave] = rest;
+            __syncthreads();
+            rest = wave_rest[0];
+            for (int w = 1; w < kWaves; ++w) rest += wave_rest[w];
+        }
+    }
 
     uint64_t found = 0;
     if (a.top) {
@@ -389,11 +430,11 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
     }
     if (wave != 0) return;
     if (a.parts == 1) {
-        finish(a, row, s, found, lane, given, there);
+        finish(a, row, Part{s.m, rest, s.t}, found, lane, given, there);
         return;
     }
     const int64_t slot = row * a.parts + part;
-    if (lane == 0) a.part_sums[slot] = s;
+    if (lane == 0) a.part_sums[slot] = Part{s.m, rest, s.t};
     if (lane < (uint32_t)a.top) a.part_keys[slot * a.top + lane] = found;
 }
 
@@ -420,9 +461,16 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobCall a)
     if (a.logp) id = a.ids[row];
     const bool there = id >= 0 && id < a.V;
     const float given = there ? widen(((const T *)a.logits + row * a.row_stride)[id]) : 0.0f;
-    Sums s = {kLowest, 0.0f, 0.0f};
+    // the parts' sums behind the row's largest logit; the first part that has it brings its rest
+    Part s = {kLowest, -1.0f, 0.0f};
     if (lane < a.parts) s = a.part_sums[row * a.parts + lane];
-    s = join_all<64>(s, a.scale, nullptr);
+    Sums all = {s.m, 1.0f + s.rest, s.t};
+    s.m = lane_max<64>(all.m);
+    const uint64_t holders = __ballot(all.m == s.m && s.rest != -1.0f);
+    const bool holds = holders && lane == __ffsll((unsigned long long)holders) - 1;
+    rescale(all, s.m, a.scale);
+    s.rest = holders ? lane_sum<64>(holds ? s.rest : all.s) : -1.0f;
+    s.t = lane_sum<64>(all.t);
     if (keys > 256)
         for (int i = 0; i < keys; i += 64) put_in(found, i + lane < keys ? a.part_keys[row * keys + i + lane] : 0, a.top, lane);
     finish(a, row, s, found, lane, given, there);
@@ -446,21 +494,23 @@ __global__ __launch_bounds__(256) void logprob_back_kernel(LogprobCall a)
         if (ROWS && row[u] >= a.R) row[u] = a.R - 1, c[u] = V;
         r[u] = raw_at<N>((const T *)a.logits + row[u] * a.row_stride, c[u], V);
     }
-    float m = 0.0f, c0 = 0.0f, c1 = 0.0f, hit = 0.0f;
+    float m = 0.0f, c0 = 0.0f, c1 = 0.0f, hit = 0.0f, most = 0.0f;
     int64_t id = -1;
     bool empty = false;
 #pragma unroll
     for (int u = 0; u < kBackPieces; ++u) {
         if (ROWS || u == 0) {
-            // -p (g + ge (log p + entropy)) / temperature = 2^y (c0 + c1 y)
+            // -p (g + ge (log p + entropy)) / temperature = 2^y (c0 + c1 y); `most`: the given token's where it is the largest logit,
+            // of which 1 - p = rest / (1 + rest)
             const int64_t at = row[u];
             m = a.stats[at * 2];
-            const float sum = a.stats[at * 2 + 1];
+            const float rest = a.stats[at * 2 + 1], sum = 1.0f + rest;
             id = a.g_logp ? a.ids[at] : -1;
             const bool given = id >= 0 && id < V;
             const float g = given ? a.g_logp[at] : 0.0f, ge = a.g_entropy ? a.g_entropy[at] : 0.0f;
-            const float shift = a.g_entropy ? a.entropy[at] - logf(sum) : 0.0f, inv = -a.inv_temperature / sum;
+            const float shift = a.g_entropy ? a.entropy[at] - log_1p(rest) : 0.0f, inv = -a.inv_temperature / sum;
             c0 = inv * (g + ge * shift);
+            most = inv * (ge * shift - g * rest);
             c1 = inv * ge * kLn2;
             hit = g * a.inv_temperature;
             empty = m == -INFINITY;
@@ -474,9 +524,13 @@ __global__ __launch_bounds__(256) void logprob_back_kernel(LogprobCall a)
             const float y = (v[k] - m) * a.scale;
             v[k] = empty ? 0.0f : __builtin_amdgcn_exp2f(y) * __builtin_fmaf(c1, fmaxf(y, kFar), c0);
         }
-        if (id >= c[u] && id < c[u] + N)
+        if (id >= c[u] && id < c[u] + N) {
+            float logit[N];
+            unpack(r[u], logit);
 #pragma unroll
-            for (int k = 0; k < N; ++k) v[k] += c[u] + k == id ? hit : 0.0f;
+            for (int k = 0; k < N; ++k)
+                if (c[u] + k == id) v[k] = logit[k] == m ? most : v[k] + hit;
+        }
         store_at<N, true>((T *)a.glogits + row[u] * V, c[u], V, v);
     }
 }
@@ -567,7 +621,7 @@ extern "C" size_t kan_token_logprob_workspace_bytes(int64_t R, int64_t V, int32_
 {
     if (V <= 0 || top < 0 || top > KAN_TOP_MAX) return 0;
     const int parts = parts_of(R, V);
-    return parts > 1 ? align_up((size_t)R * parts * sizeof(Sums)) + align_up((size_t)R * parts * top * sizeof(uint64_t)) : 0;
+    return parts > 1 ? align_up((size_t)R * parts * sizeof(Part)) + align_up((size_t)R * parts * top * sizeof(uint64_t)) : 0;
 }
 
 extern "C" int kan_token_logprob_forward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, const int64_t *ids,
@@ -599,8 +653,8 @@ extern "C" int kan_token_logprob_forward(int64_t R, int64_t V, const void *logit
     a.top_ids = top_ids;
     a.top_logp = top_logp;
     a.parts = parts_of(R, V);
-    a.part_sums = (Sums *)ws;
-    a.part_keys = (uint64_t *)((char *)ws + align_up((size_t)R * a.parts * sizeof(Sums)));
+    a.part_sums = (Part *)ws;
+    a.part_keys = (uint64_t *)((char *)ws + align_up((size_t)R * a.parts * sizeof(Part)));
     return status_of(type == KAN_F32 ? launch_forward<float>(a, (hipStream_t)stream) : launch_forward<bf16>(a, (hipStream_t)stream));
 }
 
