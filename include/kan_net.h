@@ -34,7 +34,9 @@ enum { KAN_NORM_RMS = 0, KAN_NORM_LAYER = 1 };
      x_out = residual_scale * x + gate * u                x: the residual stream in front of it
      h     = norm(x_out) * w_pre + b_pre                  what the block behind reads
    norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps), without the mean for KAN_NORM_RMS; eps > 0.  The norm of
-   x_out is that of its 32-bit value, not of the one rounded to stream_type.
+   x_out is that of its 32-bit value, not of the one rounded to stream_type.  Rows of any finite values keep their digits, also where
+   squares or sums of them are not in a float's range.  A NaN in a row makes its norm NaN; an infinity makes a layer norm NaN and an
+   RMS norm NaN in its place and 0 in the others.
    Row b takes row b / gate_rows of the gate; gate_rows = 0: all rows share one.
    stream_type is the type of x, x_out and their gradients, branch_type that of f, h and theirs: KAN_BF16 branches need a
    KAN_BF16 stream (KAN_ERR_UNSUPPORTED otherwise).  Parameters and their gradients are fp32. */

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from oracle import net as plain
-from paper_2408_11200_amd import net
+from paper_2408_11200_amd import net, workloads
 
 pytestmark = pytest.mark.gpu
 
@@ -22,6 +22,50 @@ def dev(a, dtype=F32):
 
 def host(t):
     return t.detach().double().cpu().numpy()
+
+
+def check(got, ref, scale, ulps, name=""):
+    """|got - ref| <= ulps * u * (scale + mean scale of the row), and half a unit of a bfloat16 result."""
+    bf, got = got.dtype == BF16, host(got)
+    assert got.shape == ref.shape, (name, got.shape, ref.shape)
+    tol = ulps * U * (scale + scale.mean(-1, keepdims=True)) + (2.0 ** -8 * np.abs(ref) if bf else 0.0) + 1e-37
+    err = np.abs(got - ref)
+    assert (err <= tol).all(), (name, float((err / tol).max()))         # a NaN fails
+
+
+# ---- block norm -----------------------------------------------------------------------------
+
+def norm_rows(B, n, kind, size, eps, stream, branch, seed):
+    """Rows of x and f of the given sizes (one a row, in turn), and everything else so that all outputs are in range."""
+    rng = np.random.default_rng(seed)
+    size = np.resize(size, B)[:, None]
+    a = lambda *s: rng.standard_normal(s).astype(np.float32)
+    spec = workloads.BlockNormSpec(n, kind, float(np.float32(eps)), 0.75, 0, "f32" if branch == F32 else "bf16")
+    x, f = np.float32(np.clip(a(B, n), -1, 1) * size), np.float32(np.clip(a(B, n), -1, 1) * size[::-1])
+    x[:, n // 2] = size[:, 0]
+    p = dict(w_post=1 + 0.2 * a(n), b_post=0.2 * a(n), gate=0.5 * a(1, n) * np.float32(min(size.min(), 1.0)), w_pre=1 + 0.2 * a(n), b_pre=0.2 * a(n))
+    t = dict(x=dev(x, stream), f=dev(f, branch), gx_out=dev(a(B, n), stream), gh=dev(a(B, n), branch))
+    return spec, t, {k: dev(v) for k, v in p.items()}
+
+
+@pytest.mark.parametrize("n", [3, 40, 100, 300, 520, 1030, 2050, 4100, 8200])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("size,eps", [((1.0, 1e18, 1e19, 1e20, 1e30, 3e37, 3.3e38), 1e-5), ((1e-18, 1e-20, 1e-21, 1e-22), 1e-45), ((2e38, 1.0), 1e30)])
+def test_block_norm_of_the_largest_and_smallest_values(n, kind, types, size, eps):
+    """Rows whose squares, or whose sums, are not in a float's range, among rows of ordinary values.  Tolerances as for those: 64 u, of
+    gradients 192 u (a 1/sigma below the normal range is off by another 4 u)."""
+    spec, t, p = norm_rows(23, n, kind, size, eps, *types, n)
+    q = {k: host(v) for k, v in p.items()}
+    s = plain.block_norm(host(t["x"]), host(t["f"]), q, kind, spec.eps, spec.residual_scale, 0)
+    g, scale = plain.block_norm_backward(s, q, host(t["gx_out"]), host(t["gh"]), kind, spec.residual_scale, 0)
+    stats = torch.empty((23, 4), device="cuda")
+    x_out, h = net.kan_block_norm_forward(spec, t["x"], t["f"], p, stats=stats)
+    check(x_out, s["x_out"], s["x_out_scale"], 64, "x_out")
+    check(h, s["h"], s["h_scale"], 64, "h")
+    got = net.kan_block_norm_backward(spec, t["x"], t["f"], p, stats, t["gx_out"], t["gh"])
+    for name, v in got.items():
+        check(v, g[name], scale[name], 192, name)
 
 
 # ---- log probabilities ----------------------------------------------------------------------
