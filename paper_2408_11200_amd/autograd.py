@@ -71,5 +71,6 @@ def token_logprob(logits, ids, temperature=1.0, top=0):
 
 def clip_gradients(tensors, max_norm, out=None):
     """The norm over all `tensors` (a device tensor; nothing waits for it), and each of them times min(1, max_norm / norm): in place, or
-    into the tensors of `out`.  A norm that is not finite leaves the values as they are."""
+    into the tensors of `out`.  A norm that is not finite leaves the values as they are.  Not differentiable: tensors that require gradients are
+    refused where gradients are recorded."""
     return (_nodes or _load()).clip_gradients(list(tensors), max_norm, None if out is None else list(out))

@@ -1,13 +1,18 @@
 // Autograd nodes of the operators of kan_net.h, and the clipping of a list of gradients: nothing is computed here.  Without gradients to
-// record (a server's calls) the node is passed by and nothing is kept.
+// record (a server's calls) the node is passed by and nothing is kept.  Forward-mode tangents, which none of the operators has, go to the node,
+// which refuses them: outputs without one would stand for a derivative of zero.
 #include "kan_torch.hpp"
 #include "kan_net.h"
 #include <c10/core/DeviceGuard.h>
 
 namespace {
 
+bool has_tangent(const Tensor &t) { return t.defined() && t._fw_grad(0).defined(); }
+
 bool recorded(std::initializer_list<const Tensor *> tensors)
 {
+    for (const Tensor *t : tensors)
+        if (has_tangent(*t)) return true;
     if (!at::GradMode::is_enabled()) return false;
     for (const Tensor *t : tensors)
         if (t->defined() && t->requires_grad()) return true;
@@ -312,6 +317,8 @@ Tensor clip_gradients(const std::vector<Tensor> &grads, double max_norm, const s
     std::vector<kan_tensor_ref> list(grads.size());
     for (size_t i = 0; i < grads.size(); ++i) {
         const Tensor &g = grads[i], &o = to[i];
+        TORCH_CHECK(!has_tangent(g) && !has_tangent(o) && !(at::GradMode::is_enabled() && (g.requires_grad() || o.requires_grad())),
+                    "clip_gradients: not differentiable, its tensors must not require gradients (or call it under torch.no_grad())");
         // any order of the elements will do, where the output's is the same
         if (!g.is_cuda() || !g.is_non_overlapping_and_dense()) refuse("device-resident dense tensors only");
         same(g.is_same(o) || (o.device() == g.device() && o.scalar_type() == g.scalar_type() && o.sizes() == g.sizes() && o.strides() == g.strides()),

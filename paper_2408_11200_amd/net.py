@@ -1,5 +1,6 @@
 """ctypes front end of the operators of include/kan_net.h (block norms, embedding, token log probabilities, clipped gradients): same names as
-the header.  Argument marshalling only, as in `binding`; `autograd` has the same operators as differentiable functions.
+the header.  Argument marshalling only, as in `binding`; `autograd` has the same operators on torch's own terms, all but the clipping as
+differentiable functions.
 """
 import ctypes
 
