@@ -251,7 +251,10 @@ __device__ __forceinline__ void finish(const LogprobCall &a, int64_t row, Part s
 {
     const bool empty = s.rest == -1.0f, wrong = s.rest != s.rest || s.m == INFINITY;
     const float log_sum = empty ? 0.0f : log_1p(s.rest);
-    const auto logp_of = [&](float v) { return empty ? -INFINITY : wrong ? NAN : (v - s.m) * a.inv_temperature - log_sum; };
+    const auto logp_of = [&](float v) {
+        const float down = v - s.m;         // past a float's range, it need not be after the temperature
+        return empty ? -INFINITY : wrong ? NAN : (down == -INFINITY ? v * a.inv_temperature - s.m * a.inv_temperature : down * a.inv_temperature) - log_sum;
+    };
     if (lane == 0) {
         if (a.entropy) a.entropy[row] = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / (1.0f + s.rest));
         if (a.stats) {

@@ -122,6 +122,27 @@ def test_logprob_of_confident_rows(V, dtype, temperature, copies):
         assert (np.abs(got[:R] - want) <= tol).all(), (ga is None, gb is None, (np.abs(got[:R] - want) / tol).max())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,R", [(20, 3), (5000, 3), (40000, 3), (33000, 520)])
+@pytest.mark.parametrize("temperature", [1.0, 4.0, 1e10, 1e30])
+def test_logprob_of_logits_that_are_further_apart_than_a_float_reaches(dtype, V, R, temperature):
+    """The lowest value beside a large one: their difference over the temperature is what has to be in range.  Two roundings of each and of the
+    difference: 8 u."""
+    low, high = float(torch.finfo(dtype).min), 2e38
+    z = torch.full((R, V), low, dtype=dtype, device="cuda")
+    z[:, 3] = high
+    ids = torch.tensor([3, 5, V - 1], device="cuda").repeat(-(-R // 3))[:R]
+    o = net.kan_token_logprob_forward(z, ids, temperature, 2)
+    far = np.float64(low) - float(z[0, 3])
+    with np.errstate(over="ignore"):
+        want = np.float64(np.float32(far / np.float64(np.float32(temperature))))        # -infinity where a float does not reach
+    got = host(o["logp"])[:3]
+    assert got[0] == 0.0 and host(o["entropy"])[0] == 0.0 and host(o["top_logp"])[0, 0] == 0.0
+    for v in (got[1], got[2], host(o["top_logp"])[0, 1]):
+        assert v == want if np.isinf(want) else abs(v - want) <= 8 * U * abs(want), (v, want)
+    assert o["top_ids"][0].tolist() == [3, 0]
+
+
 # ---- derivatives that the operators do not have ---------------------------------------------
 
 @pytest.mark.parametrize("mode", [contextlib.nullcontext, torch.no_grad])
