@@ -488,9 +488,17 @@ template <class T, class Y>
 hipError_t launch_rows(int64_t count, int64_t V, int n, const int64_t *ids, const void *table, float scale, void *y, hipStream_t st)
 {
     const int pieces = div_up(n, 8);
-    prof::Timed timed("embedding_rows", st);
-    embedding_rows_kernel<T, Y><<<(unsigned)div_up(count * pieces, (int64_t)256), 256, 0, st>>>(ids, (const T *)table, (Y *)y, count, V, n, pieces, scale);
-    return hipGetLastError();
+    // a launch has less than 2^32 threads: of more, HIP starts what is left of their number in 32 bits, and reports nothing
+    const int64_t most = (1ll << 31) / pieces;
+    for (int64_t first = 0; first < count; first += most) {
+        const int64_t here = count - first < most ? count - first : most;
+        prof::Timed timed("embedding_rows", st);
+        embedding_rows_kernel<T, Y><<<(unsigned)div_up(here * pieces, (int64_t)256), 256, 0, st>>>(ids + first, (const T *)table, (Y *)y + first * n, here, V, n, pieces,
+                                                                                                   scale);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class Y, class G>
@@ -544,7 +552,6 @@ extern "C" int kan_embedding_forward(int64_t T, int64_t V, int32_t n, const int6
     if (rc != KAN_OK) return rc;
     if (T == 0) return KAN_OK;
     if (!ids || !table || !y || misplaced8(ids) || misplaced(table, table_type) || misplaced(y, y_type)) return KAN_ERR_INVALID_ARG;
-    if (T * div_up(n, 8) >= (1ll << 31) * 256) return KAN_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     return status_of(table_type == KAN_F32 ? launch_rows<float, float>(T, V, n, ids, table, scale, y, st)
                      : y_type == KAN_F32   ? launch_rows<bf16, float>(T, V, n, ids, table, scale, y, st)

@@ -143,6 +143,22 @@ def test_logprob_of_logits_that_are_further_apart_than_a_float_reaches(dtype, V,
     assert o["top_ids"][0].tolist() == [3, 0]
 
 
+# ---- embedding ------------------------------------------------------------------------------
+
+def test_embedding_of_more_pieces_than_one_launch_holds():
+    """2^32 pieces of eight channels and some: every row's first and last channels, and some rows whole"""
+    n = 4097
+    T = (1 << 32) // 513 + 100
+    table = torch.arange(3 * n, device="cuda").remainder_(251).view(3, n).to(BF16)
+    ids = torch.arange(T, device="cuda").remainder_(4).sub_(1)          # -1, 0, 1, 2, -1, ...
+    y = net.kan_embedding_forward(ids, table, 2.0)
+    want = torch.cat([torch.zeros((1, n), device="cuda", dtype=BF16), 2.0 * table])
+    for c in (0, 7, 8, n - 1):
+        assert torch.equal(y[:, c], want[:, c][ids + 1])
+    rows = torch.cat([torch.arange(0, T, 100003, device="cuda"), torch.arange(T - 50, T, device="cuda"), torch.arange(T - 250, T - 150, device="cuda")])
+    assert torch.equal(y[rows], want[ids[rows] + 1])
+
+
 # ---- derivatives that the operators do not have ---------------------------------------------
 
 @pytest.mark.parametrize("mode", [contextlib.nullcontext, torch.no_grad])
