@@ -90,12 +90,20 @@ __device__ __forceinline__ double chunk_squares(const T *p, int count)
     return t;
 }
 
+// max_norm / norm as a fraction near 1 and a power of two: the quotient can be below a float's range where the scaled values are not
+struct Factor {
+    float fraction;
+    int exponent;
+};
+
+__device__ __forceinline__ float scaled(float v, Factor f) { return __builtin_ldexpf(v * f.fraction, f.exponent); }
+
 template <int NT, class T>
-__device__ __forceinline__ void scale_chunk(const T *p, T *to, int count, float factor)
+__device__ __forceinline__ void scale_chunk(const T *p, T *to, int count, Factor factor)
 {
     each_piece<NT, false>(p, count, [&](float(&v)[16 / sizeof(T)], int i) {
 #pragma unroll
-        for (int k = 0; k < 16 / (int)sizeof(T); ++k) v[k] *= factor;
+        for (int k = 0; k < 16 / (int)sizeof(T); ++k) v[k] = scaled(v[k], factor);
         store_at<16 / sizeof(T), true>(to, i, count, v);
     });
 }
@@ -133,14 +141,20 @@ __device__ __forceinline__ double squares_at(const ClipCall &a, const Place &p)
 }
 
 template <int NT>
-__device__ __forceinline__ void scale_at(const ClipCall &a, const Place &p, float factor)
+__device__ __forceinline__ void scale_at(const ClipCall &a, const Place &p, Factor factor)
 {
-    if (factor == 1.0f && a.out[p.i] == a.data[p.i]) return;        // in place, and nothing to change
+    if (factor.fraction == 1.0f && factor.exponent == 0 && a.out[p.i] == a.data[p.i]) return;        // in place, and nothing to change
     if (a.type[p.i] == KAN_F32) scale_chunk<NT>((const float *)a.data[p.i] + p.at, (float *)a.out[p.i] + p.at, p.count, factor);
     else scale_chunk<NT>((const bf16 *)a.data[p.i] + p.at, (bf16 *)a.out[p.i] + p.at, p.count, factor);
 }
 
-__device__ __forceinline__ float factor_of(float norm, float max_norm) { return norm < INFINITY && norm > max_norm ? max_norm / norm : 1.0f; }
+__device__ __forceinline__ Factor factor_of(float norm, float max_norm)
+{
+    if (!(norm < INFINITY && norm > max_norm)) return Factor{1.0f, 0};
+    int most = 0, all = 0;
+    const float f = frexpf(max_norm, &most) / frexpf(norm, &all);
+    return Factor{f, most - all};
+}
 
 __global__ __launch_bounds__(kThreads) void clip_squares_kernel(ClipCall a)
 {
@@ -164,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipCall a)
     __shared__ double lds[kThreads / 64];
     const float norm = norm_of(a, lds);
     if (a.writes_norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
-    const float factor = factor_of(norm, a.max_norm);
+    const Factor factor = factor_of(norm, a.max_norm);
     const uint32_t all = a.first[a.n];
     for (uint32_t c = blockIdx.x; c < all; c += gridDim.x) scale_at<kThreads>(a, place_of(a, all - 1 - c), factor);
 }
@@ -204,11 +218,11 @@ __global__ __launch_bounds__(1024) void clip_small_kernel(ClipCall a, bool clip)
     const float norm = (float)sqrt(block_sum<1024>(t, lds));
     if (threadIdx.x == 0) *a.norm = norm;
     if (!clip) return;
-    const float factor = factor_of(norm, a.max_norm);
+    const Factor factor = factor_of(norm, a.max_norm);
     for (uint32_t q = wave; q < quarters; q += 16) {
         const Place p = quarter_of(a, q);
-        if (a.type[p.i] == KAN_F32) each_element((const float *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((float *)a.out[p.i] + p.at + i, v * factor); });
-        else each_element((const bf16 *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((bf16 *)a.out[p.i] + p.at + i, v * factor); });
+        if (a.type[p.i] == KAN_F32) each_element((const float *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((float *)a.out[p.i] + p.at + i, scaled(v, factor)); });
+        else each_element((const bf16 *)a.data[p.i] + p.at, p.count, [&](float v, int i) { put((bf16 *)a.out[p.i] + p.at + i, scaled(v, factor)); });
     }
 }
 

@@ -159,6 +159,28 @@ def test_embedding_of_more_pieces_than_one_launch_holds():
     assert torch.equal(y[rows], want[ids[rows] + 1])
 
 
+# ---- clipped gradients ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("sizes", [(5,), (300, 1, 7000), (100000, 333), (9000001,), (257, 514, 8193, 16641)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,max_norm", [(1e10, 1e-30), (1e30, 1e-10), (1e34, 1e-37), (1.0, 1e-30), (1e-25, 1e-37)])
+def test_clip_by_factors_that_are_no_floats(sizes, dtype, size, max_norm):
+    """max_norm / norm below a float's range, the scaled gradients within it: the norm's, the quotient's and the product's roundings, 4 u; and in
+    place, where a tensor's end is read over its neighbour's elements."""
+    rng = np.random.default_rng(30)
+    tensors = [dev(np.float32(size * rng.standard_normal(s)), dtype) for s in sizes]
+    norm, factor = plain.clip([host(t) for t in tensors], np.float64(np.float32(max_norm)))
+    out = [torch.empty_like(t) for t in tensors]
+    got = net.kan_clip_gradients(tensors, max_norm, out=out)
+    assert abs(float(got) - norm) <= 2 * U * norm
+    for t, o in zip(tensors, out):
+        want = host(t) * factor
+        tol = 4 * U * np.abs(want) + (2.0 ** -8 * np.abs(want) if dtype == BF16 else 0.0) + 2.0 ** -132
+        assert (np.abs(host(o) - want) <= tol).all()
+    net.kan_clip_gradients(tensors, max_norm)
+    assert all(torch.equal(t, o) for t, o in zip(tensors, out))
+
+
 # ---- derivatives that the operators do not have ---------------------------------------------
 
 @pytest.mark.parametrize("mode", [contextlib.nullcontext, torch.no_grad])
