@@ -82,7 +82,7 @@ int kan_block_norm_backward(const kan_block_norm_desc *desc, int64_t B, const vo
 
 /* ---- embedding ------------------------------------------------------------------------------ */
 
-/* y[t] = scale * table[ids[t]], t < T: rows of n channels of a table of V < 2^31 rows; a fp32 table gives fp32 rows, a bf16
+/* y[t] = scale * table[ids[t]], t < T: rows of n <= 2^30 channels of a table of V < 2^31 - 1 rows; a fp32 table gives fp32 rows, a bf16
    table either.  An id outside 0 .. V-1 (-1 for a place without a token) gives a row of zeros. */
 int kan_embedding_forward(int64_t T, int64_t V, int32_t n, const int64_t *ids, const void *table, int32_t table_type, float scale,
                           void *y, int32_t y_type, void *stream);
@@ -96,7 +96,7 @@ int kan_embedding_backward(int64_t T, int64_t V, int32_t n, const int64_t *ids, 
 
 /* ---- log probabilities of tokens ------------------------------------------------------------ */
 
-/* For R rows of V < 2^31 logits, row r at logits + r * row_stride elements (row_stride >= V), z = logits / temperature:
+/* For R rows of V < 2^31 - 1 logits, row r at logits + r * row_stride elements (row_stride >= V), z = logits / temperature:
      logp[r]    = z[ids[r]] - log sum_v exp(z[v])          an id outside 0 .. V-1 gives 0
      entropy[r] = - sum_v p_v log p_v,  p = softmax(z)
      top_ids[r][j], top_logp[r][j], j < top: the most likely tokens, best first, equal ones by the lowest index

@@ -19,6 +19,7 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxDigit = 10;
 constexpr int kMaxBlocks = 64;        // of a sort pass: every block reads all blocks' counts
 constexpr int kPiece = 16;
+constexpr int kMaxChannels = 1 << 30;
 
 template <class T, class Y>
 __global__ __launch_bounds__(256) void embedding_rows_kernel(const int64_t *ids, const T *table, Y *y, int64_t T_, int64_t V, int n, int pieces, float scale)
@@ -474,7 +475,8 @@ Layout layout_of(int64_t T, int64_t V, int n)
 int check(int64_t T, int64_t V, int32_t n)
 {
     if (T < 0 || V <= 0 || n <= 0) return KAN_ERR_INVALID_ARG;
-    if (T >= (1ll << 31) - 65536 || V >= (1ll << 31) - 1) return KAN_ERR_UNSUPPORTED;
+    // channels are counted in 32 bits, up to two workgroups' width past a row's end
+    if (T >= (1ll << 31) - 65536 || V >= (1ll << 31) - 1 || n > kMaxChannels) return KAN_ERR_UNSUPPORTED;
     return KAN_OK;
 }
 
