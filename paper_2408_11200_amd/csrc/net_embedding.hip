@@ -1,6 +1,6 @@
 // Embedding rows and their gradient (kan_net.h).
 //
-// Forward: a copy of rows, bound by HBM (by latency for a few tokens: 8 x 512 2.2 us).  65536 rows of 2048 bf16 87 us (441 MB with what of the table
+// Forward: a copy of rows, bound by HBM (by latency for a few tokens: 8 x 512 2.0 us).  65536 rows of 2048 bf16 87 us (441 MB with what of the table
 // comes from memory, 5.1 TB/s), 16384 of 512 fp32 10.2.
 //
 // Backward: tokens are sorted by id, stably (least significant digit first, up to ten bits a pass), and the sorted list is cut into pieces
@@ -9,7 +9,7 @@
 // the piece it starts in joins them (of long runs, sixteen pieces at a time have been added before).  Rows without a token are zeroed by
 // other workgroups of the same launch.  So the work is cut by places of the list, however often a token occurs, every row of the
 // table is written once, and a row's sum has one order: no atomics on values.  Bound by HBM behind the sort: 65536 tokens, table of 131072 x 2048 bf16,
-// sort 27 us, pieces 178 (835 MB, 4.7 TB/s), groups and joins 31; 16384 tokens, 50001 x 512 fp32, 15, 26 (138 MB, 5.3 TB/s) and 8.
+// sort 27 us, pieces 179 (805 MB, 4.5 TB/s), groups and joins 31-34; 16384 tokens, 50001 x 512 fp32, 14, 26 (136 MB, 5.2 TB/s) and 8.
 #include "net_device.hpp"
 
 namespace kannet {
@@ -420,7 +420,7 @@ __device__ __forceinline__ void join_run(const SumCall &a, G *gtable, uint32_t p
 }
 
 // The runs that leave the piece they start in, a workgroup each: its workers share the run's fragments.  Latency (a list entry, ids, fragments):
-// 7.7 us for 16384 tokens, 26 for 65536.
+// 7.6 us for 16384 tokens, 26-28 for 65536.
 template <class G>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumCall a, G *gtable)
 {

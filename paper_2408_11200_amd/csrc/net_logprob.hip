@@ -10,13 +10,15 @@
 // has added to it, so its pieces, one in 64 or 256, are summed once more without it and added to the other threads' sums.  From
 // there on a row is known by that rest.
 // Four pieces a thread are in flight while four are worked on: with one, 8192 x 131072 bf16 ran at 2.2 TB/s.  Measured: 4093 x 50001 fp32 135-141 us
-// (819 MB, 5.9 TB/s), bound by HBM; 8192 x 131072 bf16 with eight top tokens 410-500 us (2.15 GB, 4.3-5.2 TB/s), bound by its vector instructions:
-// some twelve issue slots an element (widen, compare, subtract, scale, the exponential's four, two clamped sums) are 330 us by themselves.
+// (819 MB, 5.9 TB/s), bound by HBM; 8192 x 131072 bf16 with eight top tokens 390-420 us (2.15 GB, 5.1-5.5 TB/s) and with none 383-390, bound by its vector
+// instructions, and so by the clock: the first twenty launches behind a pause take up to 510.  Some twelve issue slots an element (widen, compare, subtract,
+// scale, the exponential's four, two clamped sums) are 330 us by themselves.  Rows of one likely token cost 2 % more.
 //
 // The most likely tokens come out of the same read.  The `top`-th largest of the threads' largest logits is a bound that `top` logits reach: after
 // the first round of pieces, still in registers, those that reach its bound are kept, and of every later piece those that reach it; behind
 // the row the bound of all of it leaves hardly more than `top` of them, put in order by counting for each how many are above it.  (Reading
-// the pieces of the threads that have the bound once more, at the end, cost a quarter of the row: they lie in as many lines.)
+// the pieces of the threads that have the bound once more, at the end, cost a quarter of the row: they lie in as many lines.)  The first round's bound
+// stays to the row's end: where it is low for the row, more logits reach it than there is room for, and a second search reads the row again.
 #include "net_device.hpp"
 
 namespace kannet {
@@ -409,9 +411,10 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobCall a)
             __syncthreads();
             if (wave == 0 && lane < (uint32_t)a.top) found = chosen[lane];
         } else {
-            // More than there is room for (rising logits, many equal ones, rows with NaN): the pieces of the threads whose largest logit reaches
-            // the bound are read again, by every wave into a sorted list of its own.  2048 x 32768 bf16, top 8: 159 us of equal logits by one
-            // wave, 122 by all four; 52 us of random ones.
+            // A NaN in the row, or more candidates than there is room for (likely tokens behind the first round, rising logits, many equal ones; of 131072
+            // random ones with 64 top tokens, some 1200 bf16 or 2300 fp32 reach the first round's bound): the pieces of the threads whose largest logit
+            // reaches the bound are read again, by every wave into a sorted list of its own.  2048 x 32768 bf16, top 8: 159 us of equal logits
+            // by one wave, 122 by all four; 52 us of random ones.
             if (begin + tid < end && (all || most >= bound)) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
             __syncthreads();
             const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
@@ -548,6 +551,7 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, float temperat
 // How a row is cut: few rows of a large vocabulary are shared among workgroups, four a CU, of 4096 logits at least, and joined by a launch more.
 // Whole and cut, us, bf16: 1 x 131072 with five alternatives 31.6 and 11.6, without 27.9 and 7.6; 64 x 131072 with twenty 34.8 and 21.6;
 // 16 x 32768 with five 14.2 and 10.2, 128 x 32768 14.8 and 13.8, 1 x 16384 10.3 and 10.4; fp32: 64 x 50001 24.1 and 15.1, 400 x 100000 54.6 and 53.8.
+// Where between 16384 and 32768 cutting begins to pay has not been measured.
 int parts_of(int64_t R, int64_t V)
 {
     if (R <= 0 || R > 512 || V < 32768) return 1;

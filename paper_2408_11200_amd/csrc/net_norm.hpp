@@ -3,8 +3,8 @@
 // Both passes are bound by HBM: a row is read into registers once (eight channels a lane and piece, TPR lanes a row), and everything that
 // needs the whole row (mean, mean square, the two projections of the backward pass) is a sum over those lanes.  Workers are the groups of
 // TPR lanes; rows of up to 512 channels lie within a wave, so that their sums are DPP moves and need no barrier.  Forward and backward, us and
-// TB/s of what a pass has to move: 16384 x 512 fp32 layer norm 23.7 (5.7) and 38.8 (5.2); 8190 x 771 bf16 stream and fp32 branch, a gate each 117
-// rows, 20.5 (3.7) and 32 (3.6); 16384 x 4096 bf16 RMS norm 104 (5.2) and 152 (5.3); 5461 x 6144 fp32 layer norm 115 (4.7) and 157 (5.1).
+// TB/s of what a pass has to move: 16384 x 512 fp32 layer norm 23.0-25.7 (5.8-5.2) and 39.1 (5.1); 8190 x 771 bf16 stream and fp32 branch, a gate each
+// 117 rows, 21.8 (3.5) and 32.4 (3.5); 16384 x 4096 bf16 RMS norm 100.5 (5.3) and 149 (5.4); 5461 x 6144 fp32 layer norm 116 (4.6) and 157 (5.1).
 #pragma once
 #include <atomic>
 #include "net_device.hpp"
@@ -35,8 +35,8 @@ constexpr int forward_threads() { return TPR > 64 ? TPR : 256; }
 template <int TPR>
 constexpr int backward_threads() { return TPR > 512 ? TPR : 512; }
 
-// Waves wholly behind a row's end are not launched, where there can be any: bf16 layer norm forward, 27962 x 1200 103 us with 256 lanes, 79 with 192;
-// 13421 x 2500 104 with 512, 87 with 320 (but 73 and 80 of its RMS norm).  The backward pass has one workgroup a CU whichever, and gains with
+// Waves wholly behind a row's end are not launched, where there can be any: bf16 forward, 27962 x 1200 layer norm 83 us with 256 lanes, 72 with 192, RMS norm
+// 53 and 47; 13421 x 2500 90 with 512, 73 with 320, and 58 and 55; fp32 22369 x 1500 90.3 and 89.9.  The backward pass has one workgroup a CU whichever, and gains with
 // 768 lanes (7456 x 4500 119 us, 101 with 576); 1024 have no register left for it.
 template <int TPR>
 constexpr bool kForwardTrims = TPR > 128 && TPR < 1024;
