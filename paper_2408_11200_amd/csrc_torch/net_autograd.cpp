@@ -4,15 +4,20 @@
 #include "kan_torch.hpp"
 #include "kan_net.h"
 #include <c10/core/DeviceGuard.h>
+#include <torch/csrc/autograd/forward_grad.h>
 
 namespace {
+
+// whether there can be tangents at all: asked once a call, a list of 180 tensors would ask for 3 us
+bool forward_mode() { return torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr; }
 
 bool has_tangent(const Tensor &t) { return t.defined() && t._fw_grad(0).defined(); }
 
 bool recorded(std::initializer_list<const Tensor *> tensors)
 {
-    for (const Tensor *t : tensors)
-        if (has_tangent(*t)) return true;
+    if (forward_mode())
+        for (const Tensor *t : tensors)
+            if (has_tangent(*t)) return true;
     if (!at::GradMode::is_enabled()) return false;
     for (const Tensor *t : tensors)
         if (t->defined() && t->requires_grad()) return true;
@@ -315,9 +320,10 @@ Tensor clip_gradients(const std::vector<Tensor> &grads, double max_norm, const s
     const auto &to = out ? *out : grads;
     same(!grads.empty() && to.size() == grads.size(), "a list of gradients, and as many outputs");
     std::vector<kan_tensor_ref> list(grads.size());
+    const bool forward = forward_mode(), graph = at::GradMode::is_enabled();
     for (size_t i = 0; i < grads.size(); ++i) {
         const Tensor &g = grads[i], &o = to[i];
-        TORCH_CHECK(!has_tangent(g) && !has_tangent(o) && !(at::GradMode::is_enabled() && (g.requires_grad() || o.requires_grad())),
+        TORCH_CHECK(!(forward && (has_tangent(g) || has_tangent(o))) && !(graph && (g.requires_grad() || o.requires_grad())),
                     "clip_gradients: not differentiable, its tensors must not require gradients (or call it under torch.no_grad())");
         // any order of the elements will do, where the output's is the same
         if (!g.is_cuda() || !g.is_non_overlapping_and_dense()) refuse("device-resident dense tensors only");
