@@ -35,7 +35,7 @@ constexpr int forward_threads() { return TPR > 64 ? TPR : 256; }
 template <int TPR>
 constexpr int backward_threads() { return TPR > 512 ? TPR : 512; }
 
-// Waves wholly behind a row's end are not launched, where there can be any: bf16 forward, 27962 x 1200 layer norm 83 us with 256 lanes, 72 with 192, RMS norm
+// Waves wholly behind a row's end are not launched, where there can be any: bf16 forward, 27962 x 1200 layer norm 83 us with 256 lanes, 69-72 with 192, RMS norm
 // 53 and 47; 13421 x 2500 90 with 512, 73 with 320, and 58 and 55; fp32 22369 x 1500 90.3 and 89.9.  The backward pass has one workgroup a CU whichever, and gains with
 // 768 lanes (7456 x 4500 119 us, 101 with 576); 1024 have no register left for it.
 template <int TPR>
@@ -86,7 +86,7 @@ __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, in
             load_param_eight<PAIR>(w, q * tpr * 8, lane, tpr, n, v[q]);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[q][k] = none;
+            for (int k = 0; k < 8; ++k) v[q][k] = channel_of<PAIR>(q * tpr * 8, lane, tpr, k) < n ? none : 0.0f;
         }
     }
 }
@@ -105,9 +105,9 @@ __device__ __forceinline__ void store_row(void *base, int64_t row, int lane, int
 // kLeast (where squares that count would lose digits), has its sums taken once more of values times 2^-80 or 2^80.
 constexpr float kDown = 0x1p-80f, kUp = 0x1p80f, kLeast = 0x1p-90f;
 
-// n as a value the compiler knows nothing of: the masks of a row's end are made for each row, where all of them, kept over the rows, do not fit the
-// scalar registers and are fetched from lanes of vector registers (32768 x 200 bf16 layer norm forward 18.3 us, 14.2 so; 8190 x 771 in two types 20.0
-// and 18.9; but bf16 rows of whole waves lose by it, 13421 x 2500 73 and 76).
+// n as a value the compiler knows nothing of, for the layer norm of bf16 streams: the masks of a row's end are made for each row, where all of them, kept
+// over the rows, do not fit the scalar registers and are fetched from lanes of vector registers (32768 x 200 bf16 forward 18.1 us, 14.1 so; 8190 x 771 in
+// two types 20.0 and 18.9).  Others lose by it: bf16 rows of whole waves, 13421 x 2500 73 and 76, rows in two types within a wave, 280360 x 82 58 and 62.
 __device__ __forceinline__ int afresh(int n)
 {
     asm volatile("" : "+s"(n));
@@ -161,7 +161,7 @@ __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int lanes,
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 float c = v[q][k] * scale;
-                asm volatile("" : "+v"(c), "+v"(s[0]), "+v"(s[1]));        // one after the other: no registers for many at once
+                if (P > 1) asm volatile("" : "+v"(c), "+v"(s[0]), "+v"(s[1]));        // one after the other: two pieces leave no registers for many at once
                 if (LAYER) s[1] += c;
                 s[0] += c * c;
             }
@@ -176,8 +176,7 @@ __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int lanes,
     for (int q = 0; q < P; ++q)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            if (LAYER) v[q][k] = channel_of<PAIR>(q * TPR * 8, lane, lanes, k) < n ? (v[q][k] - rest) * rs : 0.0f;
-            else v[q][k] *= rs;
+            v[q][k] = LAYER ? (v[q][k] - rest) * rs : v[q][k] * rs;
         }
 }
 
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(forward_threads<TPR>(), (forward_waves<X, F, TPR>()
     read_ahead(first + sub);
     for (; first + sub < a.B; first += step) {
         const int64_t row = first + sub;
-        const int n = TPR < 64 || PAIR ? afresh(a.n) : a.n;
+        const int n = LAYER && sizeof(X) == 2 && (sizeof(F) == 2) == (TPR < 64) ? afresh(a.n) : a.n;
         float v[P][8], u[P][8], st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int q = 0; q < P; ++q) {
