@@ -255,7 +255,7 @@ __device__ __forceinline__ void finish(const LogprobCall &a, int64_t row, Part s
     const float log_sum = empty ? 0.0f : log_1p(s.rest);
     const auto logp_of = [&](float v) {
         const float down = v - s.m;         // past a float's range, it need not be after the temperature
-        return empty ? -INFINITY : wrong ? NAN : (down == -INFINITY ? v * a.inv_temperature - s.m * a.inv_temperature : down * a.inv_temperature) - log_sum;
+        return empty ? -INFINITY : wrong ? NAN : (down == -INFINITY && v > -INFINITY ? v * a.inv_temperature - s.m * a.inv_temperature : down * a.inv_temperature) - log_sum;
     };
     if (lane == 0) {
         if (a.entropy) a.entropy[row] = empty ? 0.0f : wrong ? NAN : log_sum - kLn2 * (s.t / (1.0f + s.rest));

@@ -143,6 +143,19 @@ def test_logprob_of_logits_that_are_further_apart_than_a_float_reaches(dtype, V,
     assert o["top_ids"][0].tolist() == [3, 0]
 
 
+@pytest.mark.parametrize("V,R", [(20, 4), (40000, 4), (33000, 520)])
+def test_logprob_of_masked_tokens_at_a_tiny_temperature(V, R):
+    """-infinity beside a largest logit that is itself past a float's range once divided: still -infinity, not their difference."""
+    z = torch.full((R, V), -float("inf"), device="cuda")
+    z[:, 2], z[1::2, 2] = -1e10, 1e10
+    ids = torch.full((R,), 7, device="cuda")
+    ids[2::4] = 2
+    ids[3::4] = 2
+    o = net.kan_token_logprob_forward(z, ids, 1e-30, 2)
+    assert o["logp"][:4].tolist() == [-np.inf, -np.inf, 0.0, 0.0] and not o["entropy"].any()
+    assert o["top_logp"][:4].tolist() == [[0.0, -np.inf]] * 4
+
+
 # ---- embedding ------------------------------------------------------------------------------
 
 def test_embedding_of_more_pieces_than_one_launch_holds():
