@@ -152,7 +152,7 @@ __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int lanes,
     join();
     const float square = variance() + kPart * eps;
     float rest = s[1] * inv_n, rs = 1.0f / sqrtf(square);
-    // for a whole wave, and with it all waves of a row, whose sums have the same bits; the wave's other rows get what they had
+    // for a whole wave, and with it all waves of a row, whose sums have the same bits; the wave's other rows keep what they have
     if (__ballot(!(s[0] < INFINITY) || square < kLeast)) {
         const float scale = !(s[0] < INFINITY) ? kDown : square < kLeast ? kUp : 1.0f;
         s[0] = s[1] = 0.0f;
@@ -167,8 +167,10 @@ __device__ __forceinline__ void normalise(float (&v)[P][8], int lane, int lanes,
             }
         join();
         total(0.0f);            // the sets of slots are taken in turn: an even number of sums here
-        rest = s[1] * inv_n / scale;
-        rs = 1.0f / sqrtf(variance() + eps * scale * (kPart * scale)) * scale;
+        if (TPR >= 64 || scale != 1.0f) {
+            rest = s[1] * inv_n / scale;
+            rs = 1.0f / sqrtf(variance() + eps * scale * (kPart * scale)) * scale;
+        }
     }
     r = LAYER ? 0.5f * rs : rs;
     mean = LAYER ? 2.0f * (half_mean + rest) : 0.0f;

@@ -71,6 +71,29 @@ def test_block_norm_of_the_largest_and_smallest_values(n, kind, types, size, eps
         check(v, g[name], scale[name], 192, name)
 
 
+@pytest.mark.parametrize("n", [6, 100, 520, 1200, 2050, 4100, 6150, 8199])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+def test_block_norm_of_infinities_and_nan(n, kind, types):
+    """What they lead to in their row, and nothing in the others, of rows within a wave and over several."""
+    spec, t, p = norm_rows(40, n, kind, (1.0,), 1e-5, *types, n)
+    x_out, h = net.kan_block_norm_forward(spec, t["x"], t["f"], p)
+    at = {"nan f": (3, n - 1), "inf f": (7, 0), "nan x": (11, n // 2), "inf x": (20, n - 1)}
+    t["f"][at["nan f"]], t["f"][at["inf f"]], t["x"][at["nan x"]], t["x"][at["inf x"]] = float("nan"), -float("inf"), float("nan"), float("inf")
+    x2, h2 = net.kan_block_norm_forward(spec, t["x"], t["f"], p)
+    good = [r for r in range(40) if r not in (3, 7, 11, 20)]
+    assert torch.equal(x2[good], x_out[good]) and torch.equal(h2[good], h[good])
+    assert x2[3].isnan().all() and h2[3].isnan().all() and h2[7].isnan().all() and h2[11].isnan().all()
+    assert x2[11].isnan().sum() == 1 and x2[20].isinf().sum() == 1 and not x2[20].isnan().any()
+    if kind == "layer":
+        assert x2[7].isnan().all() and h2[20].isnan().all()
+        return
+    rest = [c for c in range(n) if c != 0]
+    want = 0.75 * t["x"][7].double() + p["gate"][0].double() * p["b_post"].double()
+    assert x2[7, 0].isnan() and bool(((x2[7].double() - want).abs()[rest] <= (2.0 ** -8 if types[0] == BF16 else 4 * U) * (want.abs() + 1)[rest]).all())
+    assert h2[20, n - 1].isnan() and torch.equal(h2[20, :-1].float(), p["b_pre"][:-1].to(types[1]).float())
+
+
 # ---- log probabilities ----------------------------------------------------------------------
 
 GAPS = [0.0, 0.5, 1.0, 2.0, 4.0, 7.0, 11.0, 15.0, 20.0, 25.0, 28.0, 40.0, 60.0]
