@@ -77,6 +77,7 @@ __device__ __forceinline__ void store_param(float *w, int lane, int tpr, int n, 
     for (int q = 0; q < P; ++q) store_param_eight<PAIR>(w, q * tpr * 8, lane, tpr, n, v[q]);
 }
 
+// `none` where there is no such parameter; 0 past the row's end in either case
 template <int P, bool PAIR>
 __device__ __forceinline__ void load_param(const float *w, int lane, int tpr, int n, float none, float (&v)[P][8])
 {
@@ -100,7 +101,7 @@ __device__ __forceinline__ void store_row(void *base, int64_t row, int lane, int
     for (int q = 0; q < P; ++q) store_eight<PAIR, true>((T *)base + row * n, q * tpr * 8, lane, tpr, n, v[q]);
 }
 
-// Rows of the largest and the smallest values keep their digits, at no instruction more for the others: a mean's sum is taken times 2^-20, the centred
+// Rows of the largest and the smallest values keep their digits, and the others their instructions: a mean's sum is taken times 2^-20, the centred
 // values by half (so neither overflows; powers of two change no digit), and a row whose sum of squares overflows, or whose variance with eps is below
 // kLeast (where squares that count would lose digits), has its sums taken once more of values times 2^-80 or 2^80.
 constexpr float kDown = 0x1p-80f, kUp = 0x1p80f, kLeast = 0x1p-90f;
@@ -117,7 +118,7 @@ __device__ __forceinline__ int afresh(int n)
 // half of v - mean
 __device__ __forceinline__ float half_centred(float v, float half_mean) { return __builtin_fmaf(v, 0.5f, -half_mean); }
 
-// v becomes norm(v) (0 in channels past the row's end); mean and 1/sigma.  The variance is that of the centred values: the mean of the
+// v becomes norm(v); mean and 1/sigma.  What it leaves in channels past the row's end counts nowhere: parameters are 0 there (load_param).  The variance is that of the centred values: the mean of the
 // squares less the squared mean would lose all digits where the mean is large.  What the mean's own rounding left in the centred values
 // is their mean, from the same sums as the variance.
 template <int TPR, int P, bool PAIR, bool LAYER>
