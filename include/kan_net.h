@@ -3,8 +3,9 @@
  *
  * What a stack of KAN layers needs beside them: the norms before and after a block with its gate
  * and residual scale, the rows of an embedding table with their gradient, log probabilities of
- * tokens with the gradient of a loss on them, and the norm of all gradients with the gradients
- * scaled to it.  Same library (libkan_hip.so) and same conventions as kan.h (device memory owned by
+ * tokens with the gradient of a loss on them, the divergence from a teacher's likely tokens with its
+ * gradient, the norm of all gradients with the gradients scaled to it, and the steps of a beam search:
+ * which beams go on with which tokens, and their states in the new order.  Same library (libkan_hip.so) and same conventions as kan.h (device memory owned by
  * the caller, descriptors and lists on the host and read during the call, nothing allocated, nothing
  * kept between calls, work enqueued on `stream`, a kan_status returned and nothing thrown), except:
  *   - data are fp32 or bf16 (kan_type); what is computed is held in 32 bits or more and rounded once,
@@ -137,6 +138,76 @@ int kan_gradient_norm(int32_t n, const kan_tensor_ref *list, float *norm, void *
    (out = data), for the caller to see in *norm.  max_norm >= 0, finite.  Outputs must not overlap other tensors of the list. */
 int kan_clip_gradients(int32_t n, const kan_tensor_ref *list, float max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
 size_t kan_clip_workspace_bytes(int32_t n);
+
+/* ---- divergence from a teacher's likely tokens ---------------------------------------------- */
+
+/* What a teacher says of a row: K tokens, teacher_ids[r][K], and a value for each, teacher[r][K] of teacher_type.
+   KAN_TEACHER_LOGP    log probabilities, as top_logp of kan_token_logprob_forward is: p_k = exp(value).  What they leave of 1 is the
+                       probability of all other tokens together, one outcome more: p_r = max(0, 1 - sum_k p_k).
+   KAN_TEACHER_LOGITS  logits: p = softmax(value / temperature) over the row's list, p_r = 0.
+   An entry whose id is outside 0 .. V-1 stands for nothing (a shorter list).  A row none of whose entries has a probability above 0 has no
+   teacher: its loss and its gradients are 0 whatever its logits are. */
+enum { KAN_TEACHER_LOGP = 0, KAN_TEACHER_LOGITS = 1 };
+#define KAN_TEACHER_MAX 256
+
+/* For R rows of V < 2^31 - 1 logits as kan_token_logprob_forward takes them, q = softmax(logits / temperature), q_r the sum of q over the tokens that
+   are not in the row's list:
+     loss[r] = sum_k p_k (log p_k - log q[ids_k]) + p_r (log p_r - log q_r)
+   terms without p are 0; so is that of the rest where q_r < 1e-300 (the other tokens masked, or none), p_r counting as 0 then.  A token that is
+   in a list twice counts with both entries.  A row that is -infinity throughout has loss +infinity (and no gradient), so has one with a listed token of -infinity and p_k > 0;
+   a NaN or +infinity in a row makes its loss and gradients NaN.  Sums over the vocabulary are held in 32 bits, what the list adds to them and the differences of
+   logarithms in 64: a loss keeps its digits where student and teacher nearly agree.
+   1 <= K <= KAN_TEACHER_MAX (it may be above V).  stats[R][K + 2] is for the backward pass.  loss and stats may be NULL. */
+int kan_token_distill_forward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K, const int64_t *teacher_ids,
+                              const void *teacher, int32_t teacher_type, int32_t teacher_form, float temperature, float *loss, float *stats,
+                              void *ws, size_t ws_bytes, void *stream);
+
+/* glogits[r][v] = g_loss[r] / temperature * ( q_v P - sum_{k: ids_k = v} p_k )          for the tokens of the list
+                   g_loss[r] / temperature * ( q_v P - p_r q_v / q_r ),                  P = sum_k p_k + p_r, for the others
+   contiguous rows of V in the type of the logits, from the forward call's stats.  The teacher has no gradient.  glogits may be logits where row_stride is V. */
+int kan_token_distill_backward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K, const int64_t *teacher_ids,
+                               float temperature, const float *stats, const float *g_loss, void *glogits, void *stream);
+
+/* Both in one, for a training step that knows the weights g_loss of its rows before it has their losses (a mean's 1 / R): a row's gradients
+   are written while the caches have its logits.  Same results as the two calls'.  loss may be NULL; glogits may be logits where row_stride is V. */
+int kan_token_distill_step(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K, const int64_t *teacher_ids,
+                           const void *teacher, int32_t teacher_type, int32_t teacher_form, float temperature, const float *g_loss, float *loss,
+                           void *glogits, void *ws, size_t ws_bytes, void *stream);
+size_t kan_token_distill_workspace_bytes(int64_t R, int64_t V, int32_t K);        /* of the forward call and the step */
+
+/* ---- beam search ---------------------------------------------------------------------------- */
+
+/* One step of N searches of B <= KAN_BEAM_MAX beams each: the `top` best continuations of each search, best first.  Beam b of search n has the log probability
+   scores[n][b] and row n B + b of the logits (V of them, as kan_token_logprob_forward takes them):
+     score(b, v) = scores[n][b] + log softmax(logits / temperature)[v]      the candidates of a beam that goes on, tokens of -infinity left out
+     score(b, end_id) = scores[n][b]                                        the one candidate of a beam with ended[n][b] != 0, whose logits are not read
+   A beam has no candidates, and its logits are not read, if its score is not finite (-infinity: a place without a beam; before the first step all
+   but one); nor has one that goes on with a NaN, a +infinity or nothing but -infinity among its logits.  Scores below a float's range are no candidates either.
+   Candidates are ordered by score * rank_scale[n][b] (NULL: 1; positive and finite, otherwise the beam has none), in 64 bits, equal ones by beam, then by token;
+   in a beam by logit, equal ones by token.
+   out_scores[n][j] (without rank_scale), tokens[n][j], parents[n][j] (0 .. B-1), out_ended[n][j] = the parent has ended or the token is end_id; where there are fewer
+   than `top` candidates -infinity, -1, 0, 0.  ended NULL: none has; out_ended may be NULL.  end_id is a token, or -1 for none (ended NULL then).  1 <= top <= KAN_TOP_MAX, top <= B V.
+   Outputs must not overlap inputs. */
+#define KAN_BEAM_MAX 64
+size_t kan_beam_select_workspace_bytes(int64_t N, int32_t B, int64_t V, int32_t top);
+int kan_beam_select(int64_t N, int32_t B, int64_t V, const void *logits, int32_t type, int64_t row_stride, const float *scores, const uint8_t *ended,
+                    const float *rank_scale, int64_t end_id, float temperature, int32_t top, float *out_scores, int64_t *tokens, int64_t *parents,
+                    uint8_t *out_ended, void *ws, size_t ws_bytes, void *stream);
+
+/* What the beams keep (windows of tokens, streams, caches): `outer` blocks of rows, a row for each beam, `inner` runs of `bytes` bytes in a
+   row; stride and out_stride are the bytes from one block, row and run to the next (looked at where there is more than one; runs must not overlap).  Types and
+   alignment do not matter. */
+typedef struct kan_state_ref {
+    const void *data;
+    void *out;
+    int64_t outer, inner, bytes;
+    int64_t stride[3], out_stride[3];
+} kan_state_ref;
+
+/* Row n top + j of every out = row n B + parents[n][j] of its data, j < top <= KAN_BEAM_MAX; a parent outside 0 .. B-1 leaves row j as it was.  out may be data, with the
+   same strides, where top is B (in place: rows that are their own parents are not touched); other overlaps are not allowed, nor is an out that is in the list twice.  A tensor's rows of a search have less than 2^31 runs and
+   pieces of 16 bytes. */
+int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list, void *stream);
 
 #ifdef __cplusplus
 }

@@ -167,3 +167,104 @@ def clip(tensors, max_norm):
     """(norm, factor)"""
     norm = np.sqrt(sum((np.asarray(t, np.float64) ** 2).sum() for t in tensors))
     return norm, (max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0)
+
+
+def token_distill(logits, ids, values, temperature=1.0, teacher="logp"):
+    """dict of loss, the gradient d of each row's loss, and what their errors go by: q, q_rest, P, p_rest, y (exponents of base 2 below the others' largest logit).
+    Rows without a teacher, -infinity throughout, or with NaN or +infinity as the header says."""
+    z, t, ids = np.asarray(logits, np.float64), np.asarray(values, np.float64), np.asarray(ids)
+    R, V = z.shape
+    out = dict(loss=np.zeros(R), d=np.zeros((R, V)), q=np.zeros((R, V)), q_rest=np.zeros(R), P=np.zeros(R), p_rest=np.zeros(R), y=np.zeros((R, V)),
+               listed=np.zeros((R, V), bool))
+    for r in range(R):
+        at = [k for k in range(ids.shape[1]) if 0 <= ids[r, k] < V]
+        token, v = ids[r, at], t[r, at]
+        with np.errstate(all="ignore"):
+            if teacher == "logits" and len(at):
+                u = v / temperature
+                m = u.max() if np.isfinite(u.max()) or np.isnan(u.max()) else 0.0
+                log_p = u - m - np.log(np.exp(u - m).sum()) if (np.isnan(u) | (u > -np.inf)).any() else u
+            else:
+                log_p = v
+            p = np.exp(log_p)
+        if not (p != 0).any():
+            continue
+        p_rest = max(0.0, 1.0 - p.sum()) if teacher == "logp" else 0.0
+        row = z[r]
+        if np.isnan(row).any() or np.isposinf(row).any() or np.isnan(p).any():
+            out["loss"][r], out["d"][r] = np.nan, np.nan
+            continue
+        if np.isneginf(row).all():
+            out["loss"][r] = np.inf
+            continue
+        e = np.exp((row - row.max()) / temperature)
+        others = np.ones(V, bool)
+        others[token] = False
+        total = e[others].sum() + e[~others].sum()
+        with np.errstate(divide="ignore", invalid="ignore"):
+            log_q = (row - row.max()) / temperature - np.log(total)
+            off = row[others & (row > -np.inf)]
+            # the others' sum behind their own largest logit: it may be below what 64 bits hold beside the listed ones
+            log_rest = (off.max() - row.max()) / temperature + np.log(np.exp((off - off.max()) / temperature).sum()) - np.log(total) if len(off) else -np.inf
+            q_rest = np.exp(log_rest)
+            if q_rest < 1e-300:
+                p_rest = 0.0
+            loss = np.where(p > 0, p * (log_p - log_q[token]), 0.0).sum() + (p_rest * (np.log(p_rest) - log_rest) if p_rest > 0 else 0.0)
+        P, q = p.sum() + p_rest, e / total
+        d = q * P
+        np.subtract.at(d, token, p)
+        if len(off):
+            w = np.exp((np.where(others, row, -np.inf) - off.max()) / temperature)
+            w = w / w.sum()                                             # q_v / q_r
+            d = np.where(others, w * (q_rest * P - p_rest), d)
+            with np.errstate(invalid="ignore"):
+                out["y"][r] = np.where(others & (row > -np.inf), (off.max() - row) / temperature * np.log2(np.e), 0.0)
+            q = np.where(others, w * q_rest, q)
+        out["loss"][r], out["d"][r], out["q"][r], out["q_rest"][r], out["P"][r], out["p_rest"][r], out["listed"][r] = loss, d / temperature, q, q_rest, P, p_rest, ~others
+    return out
+
+
+def beam_select(logits, scores, top, ended=None, end_id=-1, rank_scale=None, temperature=1.0):
+    """dict of scores, tokens, parents, ended, and the ranks that order them (with the one behind the last)."""
+    scores = np.asarray(scores, np.float64)
+    N, B = scores.shape
+    z = np.asarray(logits, np.float64).reshape(N, B, -1)
+    out = {n: [] for n in ("scores", "tokens", "parents", "ended", "ranks")}
+    for n in range(N):
+        found = []
+        for b in range(B):
+            scale = 1.0 if rank_scale is None else float(rank_scale[n, b])
+            if not np.isfinite(scores[n, b]) or not (0 < scale < np.inf):
+                continue
+            if ended is not None and ended[n, b]:
+                found.append((-scores[n, b] * scale, b, 0.0, end_id, scores[n, b], True))
+                continue
+            row = z[n, b]
+            if np.isnan(row).any() or np.isposinf(row).any() or np.isneginf(row).all():
+                continue
+            down = (row - row.max()) / temperature
+            with np.errstate(invalid="ignore"):
+                score = scores[n, b] + (down - np.log(np.exp(down).sum()))
+            keep = np.where(score >= -np.finfo(np.float32).max)[0]
+            keep = keep[np.lexsort((keep, -row[keep]))][:top + 1]
+            found += [(-score[v] * scale, b, -row[v], v, score[v], v == end_id) for v in keep]
+        found.sort(key=lambda f: f[:4])
+        taken = found[:top] + [(np.inf, 0, 0, -1, -np.inf, False)] * (top - len(found))
+        out["scores"].append([f[4] for f in taken])
+        out["tokens"].append([f[3] for f in taken])
+        out["parents"].append([f[1] for f in taken])
+        out["ended"].append([f[5] for f in taken])
+        out["ranks"].append([-f[0] for f in found[:top + 1]] + [-np.inf] * (top + 1 - len(found)))
+    return {n: np.array(v) for n, v in out.items()}
+
+
+def beam_reorder(parents, state, beams, before=None, dim=0):
+    """The state's rows in the order of the parents; `before`: what the output holds where a parent is outside."""
+    state = np.moveaxis(np.asarray(state), dim, 0)
+    N, top = parents.shape
+    out = np.array(state if before is None else np.moveaxis(np.asarray(before), dim, 0))
+    for n in range(N):
+        for j in range(top):
+            if 0 <= parents[n, j] < beams:
+                out[n * top + j] = state[n * beams + parents[n, j]]
+    return np.moveaxis(out, 0, dim)

@@ -74,3 +74,28 @@ def clip_gradients(tensors, max_norm, out=None):
     into the tensors of `out`.  A norm that is not finite leaves the values as they are.  Not differentiable: tensors that require gradients are
     refused where gradients are recorded."""
     return (_nodes or _load()).clip_gradients(list(tensors), max_norm, None if out is None else list(out))
+
+
+def token_distill(logits, teacher_ids, values, temperature=1.0, teacher="logp"):
+    """The divergence of softmax(logits / temperature) from what a teacher says of each row, K tokens and a value for each: log probabilities (as
+    token_logprob's top_logp; the rest of the vocabulary is one outcome more), or teacher="logits".  Rows whose ids are all outside the vocabulary have none.
+    Differentiable in logits; the teacher's values must not require gradients where gradients are recorded."""
+    from . import net
+    return (_nodes or _load()).token_distill(logits, teacher_ids, values, temperature, net.TEACHERS[teacher])
+
+
+def beam_select(logits, scores, top=None, ended=None, end_id=-1, rank_scale=None, temperature=1.0):
+    """(scores, tokens, parents, ended), [N][top]: the `top` (default: as many as beams) best of score + log softmax(logits / temperature) over the beams and the vocabulary
+    of each search; scores [N][B], logits [N * B][V] or [N][B][V].  A beam that has ended goes on with end_id at its score, one at -infinity not at all; rank_scale
+    [N][B] is what scores are multiplied by to be compared.  Places without a candidate: -infinity, -1, 0, False.  Not differentiable: refused where gradients are recorded."""
+    return tuple((_nodes or _load()).beam_select(logits, scores, scores.shape[-1] if top is None else top, ended, end_id, rank_scale, temperature))
+
+
+def beam_reorder(parents, tensors, beams, out=None, dim=0):
+    """The rows of the tensors (dimension `dim`, `beams` for each search) in the order of parents [N][top]: row n * top + j from row n * beams + parents[n][j], in place or
+    into the tensors of `out`, which it returns.  Parents outside 0 .. beams - 1 leave their rows as they were.  Not differentiable: tensors that require
+    gradients are refused where gradients are recorded."""
+    tensors = list(tensors)
+    out = tensors if out is None else list(out)
+    (_nodes or _load()).beam_reorder(parents, tensors, beams, out, dim)
+    return out

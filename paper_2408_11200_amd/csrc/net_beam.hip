@@ -1,0 +1,395 @@
+// One step of beam searches: the best continuations over a search's beams and the vocabulary (kan_net.h).
+//
+// Of one beam no more than `top` tokens can be among the search's `top` best, and they are its `top` largest logits.  So a first launch goes through the rows
+// once, each on its own (few rows cut into parts): the sum of the exponentials, and the keys of the largest logits, in order.  The second one has a
+// workgroup for each search: it adds the beams' scores, in 64 bits, and takes the `top` best of what the rows have left.  Rows of beams that have ended
+// or are not there are not read.
+//
+// The largest logits come out of the one read: the `top`-th largest of the threads' largest ones is a bound that `top` logits reach.  What
+// reaches the first round's bound is kept, of every later piece what reaches the bound as it is by then (taken anew behind rounds 1, 2, 4, 8, ... where `top`
+// tokens a round would not fit), and what is kept is put in order by counting for each how many are above it.
+#include "net_softmax.hpp"
+
+namespace kannet {
+namespace {
+
+struct BeamCall {
+    const void *logits;
+    int64_t row_stride, V;
+    uint32_t rows;          // N * B
+    int B, top;
+    const float *scores, *rank_scale;
+    const uint8_t *ended;
+    int64_t end_id;
+    Temperature t;
+    float *out_scores;
+    int64_t *tokens, *parents;
+    uint8_t *out_ended;
+    int parts;              // of a row
+    uint32_t part_pieces;   // pieces of 16 bytes of a part
+    Mass *sums;             // [rows][parts]
+    uint64_t *keys;         // [rows][parts][top], best first; 0: none
+};
+
+__device__ __forceinline__ bool finite(float v) { return v - v == 0.0f; }
+
+// whether a beam's logits are looked at
+__device__ __forceinline__ bool goes_on(const BeamCall &a, uint32_t row) { return finite(a.scores[row]) && !(a.ended && a.ended[row]); }
+
+// A row, or part blockIdx.x % a.parts of it
+template <class T, int NT, bool STREAM>
+__global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
+{
+    constexpr int N = 16 / sizeof(T);
+    constexpr uint32_t kCandidates = 4 * NT;
+    __shared__ Mass wave_sums[NT / 64];
+    __shared__ uint64_t best[kCandidates], shortlist[NT], chosen[KAN_TOP_MAX];
+    __shared__ uint32_t candidates, kept, sources;
+    __shared__ uint16_t source[NT];
+    __shared__ float thread_most[NT];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    if (!goes_on(a, row)) return;
+    const T *z = (const T *)a.logits + (int64_t)row * a.row_stride;
+    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N;
+    const uint32_t begin = part * a.part_pieces, end = pieces - begin < a.part_pieces ? pieces : begin + a.part_pieces;
+    const float scale = a.t.scale;
+    Mass sum = {kLowest, 0.0f};
+    float most = -INFINITY, bound = NAN;
+    // all logits that are not below the bound, nor -infinity
+    const auto collect = [&](const float (&v)[N], uint32_t p) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (v[k] >= bound && v[k] > -INFINITY) {
+                const uint32_t slot = atomicAdd(&candidates, 1u);
+                if (slot < kCandidates) best[slot] = key_of(v[k], p * N + k);
+            }
+    };
+    if (tid == 0) candidates = kept = sources = 0;
+    if (tid < KAN_TOP_MAX) chosen[tid] = 0;
+    Raw<T, N> next[kRound];
+    read_round<T, NT, STREAM>(next, z, begin + tid, end, a.V);
+    __syncthreads();
+    const uint32_t rounds = (end - begin + kRound * NT - 1) / (kRound * NT);
+    const bool tighten = (uint32_t)a.top * rounds > kCandidates / 2;
+    uint32_t round = 0, again = 2;
+    for (uint32_t first = begin; first < end; first += kRound * NT) {
+        const uint32_t at = first + tid;
+        Raw<T, N> now[kRound];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) now[u] = next[u];
+        read_round<T, NT, STREAM>(next, z, at + kRound * NT, end, a.V);
+        // more than there is room for: the rest is not kept (they are searched for behind the loop)
+        if (__hip_atomic_load(&candidates, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kCandidates) bound = NAN;
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t p = at + u * NT;
+            if (p < end) {
+                float v[N];
+                piece_logits<N>(now[u], p, V, v);
+                const float m = add_mass<N>(v, scale, sum);
+                most = fmaxf(most, m);
+                if (m >= bound) collect(v, p);
+            }
+        }
+        ++round;
+        if (round == 1 || (tighten && round == again)) {
+            __syncthreads();
+            const float higher = value_of_rank<NT>(most, a.top, lane, thread_most);
+            if (round == 1) {
+                bound = higher;
+#pragma unroll
+                for (int u = 0; u < kRound; ++u) {
+                    const uint32_t p = at + u * NT;
+                    if (p < end) {
+                        float v[N];
+                        piece_logits<N>(now[u], p, V, v);
+                        collect(v, p);
+                    }
+                }
+            } else {
+                again *= 2;
+                if (bound == bound) bound = higher;
+            }
+        }
+    }
+    sum = join_mass<NT>(sum, scale, wave_sums);
+    uint64_t found = 0;
+    if (sum.s == sum.s && sum.s > 0.0f) {           // the same in all threads; a NaN's beam has no candidates
+        __syncthreads();
+        if (rounds > 1) bound = value_of_rank<NT>(most, a.top, lane, thread_most);
+        __syncthreads();
+        uint32_t n = candidates;
+        if (n <= kCandidates) {
+            for (uint32_t i = tid; i < n; i += NT) {
+                const uint64_t k = best[i];
+                if (logit_of(k) >= bound) {
+                    const uint32_t slot = atomicAdd(&kept, 1u);
+                    if (slot < NT) shortlist[slot] = k;
+                }
+            }
+            __syncthreads();
+            const bool shorter = kept <= NT;
+            const uint64_t *list = shorter ? shortlist : best;
+            n = shorter ? kept : n;
+            for (uint32_t i = tid; i < n; i += NT) {
+                const uint64_t k = list[i];
+                const int place = above(list, n, k);
+                if (place < a.top) chosen[place] = k;
+            }
+            __syncthreads();
+            if (lane < (uint32_t)a.top) found = chosen[lane];
+        } else {
+            // more than there is room for (many equal logits, rising ones): the pieces of the threads whose largest logit reaches the bound are read
+            // again, by every wave into a sorted list of its own
+            if (begin + tid < end && most >= bound && most > -INFINITY) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
+            __syncthreads();
+            const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
+            for (uint32_t first = 64 * wave; first < count; first += NT) {
+                const uint32_t i = first + lane, p = i < count ? begin + source[i / each] + i % each * NT : end;
+                float v[N];
+                piece_logits<N>(raw_at<N>(z, (int64_t)p * N, p < end ? a.V : 0), p, V, v);
+#pragma unroll
+                for (int k = 0; k < N; ++k) put_in(found, p < end && v[k] >= bound && v[k] > -INFINITY ? key_of(v[k], p * N + k) : 0, a.top, lane);
+            }
+            if (NT > 64) {
+                __syncthreads();                // the candidates' number has been read
+                best[tid] = lane < (uint32_t)a.top ? found : 0;
+                __syncthreads();
+                if (wave == 0)
+                    for (uint32_t w = 1; w < NT / 64; ++w) put_in(found, best[64 * w + lane], a.top, lane);
+            }
+        }
+    }
+    if (wave != 0) return;
+    const uint32_t slot = row * a.parts + part;
+    if (lane == 0) a.sums[slot] = sum;
+    if (lane < (uint32_t)a.top) a.keys[(uint64_t)slot * a.top + lane] = found;
+}
+
+// A candidate of a search: larger ranks first, of equal ones the lower beam, and in a beam the larger key, i.e. logit, then the lower token
+struct Candidate {
+    uint64_t rank, key;         // rank 0: none
+    uint32_t beam;
+};
+
+__device__ __forceinline__ bool before(const Candidate &a, const Candidate &b)
+{
+    return a.rank != b.rank ? a.rank > b.rank : a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
+}
+
+// larger values have larger keys, none is 0 (both zeros are one value)
+__device__ __forceinline__ uint64_t rank_key(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);
+    return (b >> 63) ? ~b : b | 0x8000000000000000ull;
+}
+
+__device__ __forceinline__ double rank_value(uint64_t key) { return __builtin_bit_cast(double, (key >> 63) ? key & 0x7FFFFFFFFFFFFFFFull : ~key); }
+
+enum { kOut = 0, kGoesOn = 1, kEnded = 2 };
+
+struct Beam {
+    double score, log_sum;          // of the log probability: score + ((z - most) / temperature - log_sum)
+    float most, rank_scale;
+    int state;
+};
+
+constexpr uint32_t kRoom = 2048;    // candidates that are put in order by counting
+
+// A workgroup for each search
+template <int NT>
+__global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
+{
+    __shared__ Beam beams[KAN_BEAM_MAX];
+    __shared__ Candidate list[kRoom];
+    __shared__ float value[NT];
+    __shared__ Candidate wave_best[NT / 64];
+    __shared__ uint32_t count;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, top = a.top, lists = a.B * a.parts, all = lists * top;
+    const uint32_t first_row = blockIdx.x * a.B;
+    const uint64_t *keys = a.keys + (uint64_t)first_row * a.parts * top;
+    if (tid == 0) count = 0;
+    for (uint32_t b = wave; b < (uint32_t)a.B; b += NT / 64) {
+        const uint32_t row = first_row + b;
+        const float score = a.scores[row], rank_scale = a.rank_scale ? a.rank_scale[row] : 1.0f;
+        Beam beam = {(double)score, 0.0, 0.0f, rank_scale, kOut};
+        if (finite(score) && rank_scale > 0.0f && finite(rank_scale)) {
+            if (a.ended && a.ended[row]) {
+                beam.state = kEnded;
+            } else {
+                Mass part = {kLowest, 0.0f};
+                if (lane < (uint32_t)a.parts) part = a.sums[row * a.parts + lane];
+                beam.most = lane_max<64>(part.m);
+                const double s = wave_sum((double)part.s * exp(((double)part.m - (double)beam.most) * a.t.inverse));
+                beam.log_sum = log(s);
+                if (s > 0.0 && s < (double)INFINITY) beam.state = kGoesOn;
+            }
+        }
+        if (lane == 0) beams[b] = beam;
+    }
+    __syncthreads();
+    // entry i of the rows' lists
+    const auto candidate = [&](uint32_t i) {
+        const uint32_t b = i / (a.parts * top);
+        const Beam beam = beams[b];
+        Candidate c = {0, 0, b};
+        double score = -(double)INFINITY;
+        if (beam.state == kEnded && i % (a.parts * top) == 0) {
+            score = beam.score;
+            c.key = key_of(0.0f, (uint32_t)a.end_id);
+        } else if (beam.state == kGoesOn) {
+            c.key = keys[i];
+            if (c.key) score = beam.score + (((double)logit_of(c.key) - (double)beam.most) * a.t.inverse - beam.log_sum);
+        }
+        if (finite((float)score)) c.rank = rank_key(score * (double)beam.rank_scale);
+        return c;
+    };
+    // a candidate's rank in 32 bits: none rounds past another
+    const auto rank_of = [&](const Candidate &c) { return c.rank ? (float)rank_value(c.rank) : -INFINITY; };
+    // a bound that `top` candidates reach: the `top`-th best of as many of the lists' first entries as there are threads
+    float bound = -INFINITY;
+    if (all > kRoom / 8) {
+        const uint32_t deep = NT / lists < top ? NT / lists : top, l = tid % lists, j = tid / lists;
+        const Candidate c = j < deep ? candidate(l * top + j) : Candidate{0, 0, 0};
+        bound = value_of_rank<NT>(rank_of(c), top, lane, value);
+        __syncthreads();
+    }
+    for (uint32_t i = tid; i < all; i += NT) {
+        const Candidate c = candidate(i);
+        if (c.rank && rank_of(c) >= bound) {
+            const uint32_t slot = atomicAdd(&count, 1u);
+            if (slot < kRoom) list[slot] = c;
+        }
+    }
+    __syncthreads();
+    const uint32_t n = count;
+    const auto write = [&](uint32_t j, const Candidate &c) {
+        const int64_t at = (int64_t)blockIdx.x * top + j;
+        const Beam beam = beams[c.beam];
+        const int64_t token = (uint32_t)~(uint32_t)c.key;
+        a.out_scores[at] = c.rank ? (float)(rank_value(c.rank) / (double)beam.rank_scale) : -INFINITY;
+        a.tokens[at] = c.rank ? token : -1;
+        a.parents[at] = c.rank ? c.beam : 0;
+        if (a.out_ended) a.out_ended[at] = c.rank && (beam.state == kEnded || token == a.end_id);
+    };
+    if (n <= kRoom) {
+        for (uint32_t i = tid; i < n; i += NT) {
+            const Candidate c = list[i];
+            uint32_t place = 0;
+#pragma unroll 4
+            for (uint32_t k = 0; k < n; ++k) place += before(list[k], c) ? 1 : 0;
+            if (place < top) write(place, c);
+        }
+        for (uint32_t j = n + tid; j < top; j += NT) write(j, Candidate{0, 0, 0});
+        return;
+    }
+    // More candidates reach the bound than there is room for (equal ones in many parts): the best one behind the last that was taken, `top` times
+    Candidate last = {0, 0, 0};
+    for (uint32_t j = 0; j < top; ++j) {
+        Candidate mine = {0, 0, 0};
+        for (uint32_t i = tid; i < all; i += NT) {
+            const Candidate c = candidate(i);
+            if (c.rank && (j == 0 || before(last, c)) && (!mine.rank || before(c, mine))) mine = c;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const Candidate o = {(uint64_t)__shfl_xor((unsigned long long)mine.rank, d, 64), (uint64_t)__shfl_xor((unsigned long long)mine.key, d, 64),
+                                 (uint32_t)__shfl_xor((int)mine.beam, d, 64)};
+            if (o.rank && (!mine.rank || before(o, mine))) mine = o;
+        }
+        if (lane == 0) wave_best[wave] = mine;
+        __syncthreads();
+        last = wave_best[0];
+        for (int w = 1; w < NT / 64; ++w)
+            if (wave_best[w].rank && (!last.rank || before(wave_best[w], last))) last = wave_best[w];
+        __syncthreads();
+        if (tid == 0) write(j, last);               // there are more than kRoom
+    }
+}
+
+// How rows are cut: few rows are shared among workgroups, four a CU
+int parts_of(int64_t rows, int64_t V)
+{
+    if (rows <= 0 || rows > 512 || V < 32768) return 1;
+    int64_t parts = 1024 / rows;
+    if (parts > V / 4096) parts = V / 4096;
+    return (int)(parts > 64 ? 64 : parts);
+}
+
+template <class T>
+hipError_t launch(BeamCall &a, int64_t N, hipStream_t st)
+{
+    constexpr uint32_t per = 16 / sizeof(T);
+    const uint32_t pieces = (uint32_t)div_up(a.V, (int64_t)per);
+    a.part_pieces = div_up(pieces, (uint32_t)a.parts);
+    a.parts = (int)div_up(pieces, a.part_pieces);
+    const unsigned grid = a.rows * (unsigned)a.parts;
+    {
+        prof::Timed timed("beam_rows", st);
+        if (a.V <= 4096) beam_rows_kernel<T, 64, false><<<grid, 64, 0, st>>>(a);
+        else beam_rows_kernel<T, 256, false><<<grid, 256, 0, st>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    prof::Timed timed("beam_join", st);
+    if ((int64_t)a.B * a.parts * a.top <= 256) beam_join_kernel<256><<<(unsigned)N, 256, 0, st>>>(a);
+    else beam_join_kernel<1024><<<(unsigned)N, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+int check(int64_t N, int32_t B, int64_t V, int32_t top)
+{
+    if (N < 0 || B < 1 || V <= 0 || top < 1) return KAN_ERR_INVALID_ARG;
+    if (B > KAN_BEAM_MAX || top > KAN_TOP_MAX || V >= (1ll << 31) - 1 || N >= (1ll << 24) / B) return KAN_ERR_UNSUPPORTED;
+    return top > B * V ? KAN_ERR_INVALID_ARG : KAN_OK;
+}
+
+size_t sums_bytes(int64_t N, int32_t B, int64_t V) { return align_up((size_t)(N * B) * parts_of(N * B, V) * sizeof(Mass)); }
+
+}  // namespace
+}  // namespace kannet
+
+using namespace kannet;
+
+extern "C" size_t kan_beam_select_workspace_bytes(int64_t N, int32_t B, int64_t V, int32_t top)
+{
+    if (check(N, B, V, top) != KAN_OK || N == 0) return 0;
+    return sums_bytes(N, B, V) + align_up((size_t)(N * B) * parts_of(N * B, V) * top * sizeof(uint64_t));
+}
+
+extern "C" int kan_beam_select(int64_t N, int32_t B, int64_t V, const void *logits, int32_t type, int64_t row_stride, const float *scores,
+                               const uint8_t *ended, const float *rank_scale, int64_t end_id, float temperature, int32_t top, float *out_scores,
+                               int64_t *tokens, int64_t *parents, uint8_t *out_ended, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check(N, B, V, top);
+    if (rc != KAN_OK) return rc;
+    if (row_stride < V || !(temperature >= 1e-30f && temperature <= 1e30f) || end_id < -1 || end_id >= V || (ended && end_id < 0)) return KAN_ERR_INVALID_ARG;
+    if (!known_type(type)) return KAN_ERR_UNSUPPORTED;
+    if (N == 0) return KAN_OK;
+    if (!logits || !scores || !out_scores || !tokens || !parents) return KAN_ERR_INVALID_ARG;
+    if (misplaced(logits, type) || misplaced(scores, KAN_F32) || misplaced(rank_scale, KAN_F32) || misplaced(out_scores, KAN_F32) || misplaced8(tokens) ||
+        misplaced8(parents))
+        return KAN_ERR_INVALID_ARG;
+    if (bad_workspace(ws, ws_bytes, kan_beam_select_workspace_bytes(N, B, V, top))) return KAN_ERR_WORKSPACE;
+    BeamCall a = {};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.V = V;
+    a.rows = (uint32_t)(N * B);
+    a.B = B;
+    a.top = top;
+    a.scores = scores;
+    a.rank_scale = rank_scale;
+    a.ended = ended;
+    a.end_id = end_id;
+    a.t = temperature_of(temperature);
+    a.out_scores = out_scores;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.out_ended = out_ended;
+    a.parts = parts_of(N * B, V);
+    a.sums = (Mass *)ws;
+    a.keys = (uint64_t *)((char *)ws + sums_bytes(N, B, V));
+    return status_of(type == KAN_F32 ? launch<float>(a, N, (hipStream_t)stream) : launch<bf16>(a, N, (hipStream_t)stream));
+}

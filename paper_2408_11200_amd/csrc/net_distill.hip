@@ -1,0 +1,520 @@
+// The divergence of a student's probabilities from a teacher's list of likely tokens, and its gradient (kan_net.h).
+//
+// A row's tokens are of two kinds: those of the teacher's list, at most 256, and the others.  One pass over the row sums the exponentials of the
+// others alone: the listed ones are marked in a bit a token in LDS (V / 8 bytes), a piece of 16 bytes of logits asks for its bits with one read,
+// and takes marked logits for -infinity.  The list's own logits are gathered beside it, and a wave adds what they do in 64 bits.  So neither
+// kind is a difference of two larger sums: the probability of the others, a thousandth in a trained network, has all its digits, and
+// so has the listed tokens' in a row where they have none.
+//   total = sum_S exp(z - M) + rest exp(m - M),   rest and m: the sum and the largest logit of the others,   q_r = rest exp(m - M) / total
+// The gradient of a token off the list is its exponential exp(z - m) times one factor of the row, g (q_r P - p_r) / (temperature rest), that of a
+// listed one g (q P - p) / temperature: both differences are taken in 64 bits, where student and teacher nearly agree in all 32 kept ones.  The forward
+// pass leaves them (K + 2 floats a row), the backward pass reads no teacher.
+#include "net_softmax.hpp"
+
+namespace kannet {
+namespace {
+
+constexpr int kEntries = KAN_TEACHER_MAX / 64;          // of the list, a lane
+constexpr uint32_t kMarked = 1u << 18;                  // tokens that are marked at a time: 32 KB
+constexpr double kNothing = 1e-300;
+
+struct DistillCall {
+    const void *logits;
+    int64_t row_stride, V, R;
+    const int64_t *ids;
+    const void *teacher;
+    int K, teacher_type, teacher_form;
+    Temperature t;
+    const float *g_loss;
+    float *loss, *stats;
+    void *glogits;
+    int parts;              // of a row, in the forward pass
+    uint32_t part_pieces;   // pieces of 16 bytes of a part
+    Mass *part_sums;        // [R][parts]
+    uint32_t chunks;        // workgroups of a row, in the backward pass
+};
+
+// The teacher's list of a row, over a wave: entry e * 64 + lane.
+struct List {
+    int64_t id[kEntries];           // -1: nothing
+    double p[kEntries], log_p[kEntries];
+    float z[kEntries];              // the student's logit
+    double p_sum, p_rest;
+    bool some;
+};
+
+template <class T>
+__device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, const T *z, int lane, List &l)
+{
+    float value[kEntries];
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        const int k = e * 64 + lane;
+        l.id[e] = -1;
+        l.z[e] = value[e] = -INFINITY;
+        if (k < a.K) {
+            const int64_t at = row * a.K + k, id = a.ids[at];
+            if (id >= 0 && id < a.V) {
+                l.id[e] = id;
+                value[e] = a.teacher_type == KAN_F32 ? ((const float *)a.teacher)[at] : widen(((const bf16 *)a.teacher)[at]);
+                l.z[e] = widen(z[id]);
+            }
+        }
+    }
+    double most = 0.0, log_sum = 0.0, sum = 0.0;
+    if (a.teacher_form == KAN_TEACHER_LOGITS) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) m = fmaxf(m, value[e]);
+        most = (double)lane_max<64>(m);
+        if (most == -(double)INFINITY) most = 0.0;
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (e * 64 < a.K && l.id[e] >= 0) sum += exp(((double)value[e] - most) * a.t.inverse);
+        log_sum = log(wave_sum(sum));
+    }
+    sum = 0.0;
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        l.p[e] = l.log_p[e] = 0.0;
+        if (e * 64 < a.K && l.id[e] >= 0) {
+            const bool logits = a.teacher_form == KAN_TEACHER_LOGITS && value[e] != -INFINITY;
+            l.log_p[e] = logits ? ((double)value[e] - most) * a.t.inverse - log_sum : (double)value[e];
+            l.p[e] = exp(l.log_p[e]);
+            sum += l.p[e];
+            some = some || l.p[e] != 0.0;
+        }
+    }
+    l.p_sum = wave_sum(sum);
+    l.p_rest = a.teacher_form == KAN_TEACHER_LOGP ? fmax(0.0, 1.0 - l.p_sum) : 0.0;
+    l.some = __any(some);
+}
+
+// What a row's gradients are made of
+struct RowGradient {
+    float m, factor;            // of a token off the list: exp2((z - m) * scale) * factor
+    float listed[kEntries];     // of the list's
+};
+
+// A row's loss and gradients from its list and the sum over the other tokens, by one wave.  `twice`: a token may be in the list more than once;
+// `tokens` [K] is room in LDS for finding out which.
+__device__ __forceinline__ double finish_row(const DistillCall &a, const List &l, Mass others, bool twice, uint32_t *tokens, int lane, RowGradient &g)
+{
+    bool first[kEntries];
+    double p_all[kEntries];         // of all entries of a token
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        first[e] = l.id[e] >= 0;
+        p_all[e] = l.p[e];
+    }
+    if (twice) {
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (e * 64 + lane < a.K) tokens[e * 64 + lane] = (uint32_t)l.id[e];
+        double *p = (double *)(tokens + KAN_TEACHER_MAX);
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (e * 64 + lane < a.K) p[e * 64 + lane] = l.p[e];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            if (l.id[e] < 0) continue;
+            p_all[e] = 0.0;
+            for (int k = 0; k < a.K; ++k)
+                if (tokens[k] == (uint32_t)l.id[e]) {
+                    p_all[e] += p[k];
+                    if (k < e * 64 + lane) first[e] = false;
+                }
+        }
+    }
+    const bool rest = !(others.s == 0.0f);          // a NaN counts
+    float m = rest ? others.m : -INFINITY;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) m = fmaxf(m, l.z[e]);
+    const double M = (double)lane_max<64>(m);
+    const bool empty = M == -(double)INFINITY && !rest;
+    double weight[kEntries], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        weight[e] = 0.0;
+        if (e * 64 < a.K && l.id[e] >= 0) {
+            weight[e] = exp(((double)l.z[e] - M) * a.t.inverse);
+            if (first[e]) sum += weight[e];
+        }
+    }
+    const double down = ((double)others.m - M) * a.t.inverse, off = rest ? (double)others.s * exp(down) : 0.0;
+    const double total = wave_sum(sum) + off, inverse = 1.0 / total, log_total = log(total), q_rest = off * inverse;
+    const double p_rest = q_rest >= kNothing ? l.p_rest : 0.0, P = l.p_sum + p_rest;
+    double loss = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        g.listed[e] = 0.0f;
+        if (e * 64 < a.K && l.id[e] >= 0) {
+            if (l.p[e] != 0.0) loss += l.p[e] * (l.log_p[e] - (((double)l.z[e] - M) * a.t.inverse - log_total));
+            if (l.some && !empty) g.listed[e] = (float)((weight[e] * inverse * P - p_all[e]) * a.t.inverse);
+        }
+    }
+    loss = wave_sum(loss);
+    if (p_rest > 0.0) loss += p_rest * (log(p_rest) - (down + log((double)others.s) - log_total));
+    // (without others no token asks for the factor but the masked ones of a row with a NaN among the listed)
+    g.m = rest && l.some ? others.m : 0.0f;
+    g.factor = !l.some || empty ? 0.0f : rest ? (float)((q_rest * P - p_rest) * a.t.inverse / (double)others.s) : total == total ? 0.0f : NAN;
+    return !l.some ? 0.0 : empty ? (double)INFINITY : loss;
+}
+
+__device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, double loss, const RowGradient &g, int lane)
+{
+    if (lane == 0 && a.loss) a.loss[row] = (float)loss;
+    if (!a.stats) return;
+    float *s = a.stats + row * (a.K + 2);
+    if (lane == 0) {
+        s[0] = g.m;
+        s[1] = g.factor;
+    }
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e)
+        if (e * 64 + lane < a.K) s[2 + e * 64 + lane] = g.listed[e];
+}
+
+// the gradient of a piece's tokens as if none were listed; factor 0: zeros, whatever the logits are
+template <int N>
+__device__ __forceinline__ void piece_gradient(float (&v)[N], float m, float factor, float scale)
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = factor == 0.0f ? 0.0f : power(v[k], m, scale) * factor;
+}
+
+// A row, or part blockIdx.x % a.parts of it (few rows are cut; distill_join_kernel does the rest).  STEP: and its gradients.
+template <class T, int NT, bool STREAM, bool STEP>
+__global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
+{
+    constexpr int N = 16 / sizeof(T);
+    extern __shared__ uint32_t marks[];
+    __shared__ Mass wave_sums[NT / 64];
+    __shared__ double room[KAN_TEACHER_MAX + KAN_TEACHER_MAX / 2];
+    __shared__ uint32_t twice, some;
+    __shared__ float row_m, row_factor;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x / a.parts;
+    const uint32_t part = blockIdx.x % a.parts, V = (uint32_t)a.V, pieces = (V + N - 1) / N;
+    const uint32_t begin = part * a.part_pieces, end = pieces - begin < a.part_pieces ? pieces : begin + a.part_pieces;
+    const T *z = (const T *)a.logits + row * a.row_stride;
+    const float scale = a.t.scale;
+    Raw<T, N> next[kRound];
+    read_round<T, NT, STREAM>(next, z, begin + tid, end, a.V);
+    if (tid == 0) twice = 0;
+    List list;
+    if (wave == 0 && a.parts == 1) {
+        read_list(a, row, z, lane, list);
+        if (lane == 0) some = list.some;
+    }
+    Mass sum = {kLowest, 0.0f};
+    for (uint32_t base = begin; base < end; base += kMarked / N) {
+        const uint32_t stop = end - base < kMarked / N ? end : base + kMarked / N;
+        const uint32_t words = ((stop - base) * N + 31) / 32;
+        if (base != begin) __syncthreads();
+        for (uint32_t w = tid; w < words; w += NT) marks[w] = 0;
+        __syncthreads();
+        if (a.parts == 1 && !some) break;               // no teacher: the row is not read
+        for (int k = tid; k < a.K; k += NT) {
+            const int64_t id = a.ids[row * a.K + k];
+            if (id < (int64_t)base * N || id >= (int64_t)stop * N || id >= a.V) continue;
+            const uint32_t at = (uint32_t)(id - (int64_t)base * N);
+            if (atomicOr(&marks[at / 32], 1u << at % 32) >> at % 32 & 1) twice = 1;
+        }
+        __syncthreads();
+        for (uint32_t first = base; first < stop; first += kRound * NT) {
+            const uint32_t at = first + tid;
+            Raw<T, N> now[kRound];
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) now[u] = next[u];
+            // behind the last round, what the next slice begins with
+            const uint32_t after = first + kRound * NT < stop ? at + kRound * NT : stop + tid;
+            read_round<T, NT, STREAM>(next, z, after, end, a.V);
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) {
+                const uint32_t p = at + u * NT;
+                if (p >= stop) continue;
+                float v[N];
+                piece_logits<N>(now[u], p, V, v);
+                const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
+                if (bits)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[k] = bits >> k & 1 ? -INFINITY : v[k];
+                add_mass<N>(v, scale, sum);
+            }
+        }
+    }
+    sum = join_mass<NT>(sum, scale, wave_sums);
+    if (a.parts > 1) {
+        if (tid == 0) a.part_sums[row * a.parts + part] = sum;
+        return;
+    }
+    RowGradient g;
+    float weight = 0.0f;
+    if (wave == 0) {
+        const double loss = finish_row(a, list, sum, twice != 0, (uint32_t *)room, lane, g);
+        write_row(a, row, loss, g, lane);
+        if constexpr (STEP) {
+            weight = a.g_loss[row];
+            if (lane == 0) {
+                row_m = g.m;
+                row_factor = g.factor == 0.0f ? 0.0f : g.factor * weight;
+            }
+        }
+    }
+    if constexpr (STEP) {
+        T *to = (T *)a.glogits + row * a.V;
+        __syncthreads();
+        const float m = row_m, factor = row_factor;
+        const int64_t n = factor == 0.0f ? 0 : a.V;         // zeros are written without a look at the logits
+        for (uint32_t first = 0; first < pieces; first += kRound * NT) {
+            Raw<T, N> r[kRound];
+            read_round<T, NT, false>(r, z, first + tid, pieces, n);
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) {
+                const uint32_t p = first + tid + u * NT;
+                if (p >= pieces) continue;
+                float v[N];
+                settle(r[u], (int64_t)p * N, a.V);
+                unpack(r[u], v);
+                piece_gradient<N>(v, m, factor, scale);
+                store_at<N, true>(to, (int64_t)p * N, a.V, v);
+            }
+        }
+        __syncthreads();        // the listed tokens' gradients go on top
+        if (wave == 0)
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (list.id[e] >= 0) put(to + list.id[e], g.listed[e] == 0.0f ? 0.0f : g.listed[e] * weight);
+    }
+}
+
+// A wave for each row that was cut, at most 64 parts
+template <class T>
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillCall a)
+{
+    __shared__ double room[KAN_TEACHER_MAX + KAN_TEACHER_MAX / 2];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    Mass sum = {kLowest, 0.0f};
+    if (lane < a.parts) sum = a.part_sums[row * a.parts + lane];
+    List list;
+    read_list(a, row, (const T *)a.logits + row * a.row_stride, lane, list);
+    sum = join_wave(sum, a.t.scale);
+    RowGradient g;
+    const double loss = finish_row(a, list, sum, true, (uint32_t *)room, lane, g);
+    write_row(a, row, loss, g, lane);
+}
+
+// The gradient's row from what the forward pass has left: elements are independent, a read and a write of the logits.
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
+{
+    constexpr int N = 16 / sizeof(T);
+    const int64_t row = blockIdx.x / a.chunks;
+    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, first = blockIdx.x % a.chunks * (kRound * NT), tid = threadIdx.x;
+    const T *z = (const T *)a.logits + row * a.row_stride;
+    T *to = (T *)a.glogits + row * a.V;
+    Raw<T, N> r[kRound];
+    read_round<T, NT, false>(r, z, first + tid, pieces, a.V);
+    const float *s = a.stats + row * (a.K + 2);
+    const float g = a.g_loss[row], m = s[0], factor = s[1] == 0.0f ? 0.0f : s[1] * g;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+        const uint32_t p = first + tid + u * NT;
+        if (p >= pieces) continue;
+        float v[N];
+        settle(r[u], (int64_t)p * N, a.V);
+        unpack(r[u], v);
+        piece_gradient<N>(v, m, factor, a.t.scale);
+        store_at<N, true>(to, (int64_t)p * N, a.V, v);
+    }
+    __syncthreads();            // the listed tokens' gradients go on top
+    const int64_t from = (int64_t)first * N, until = from + kRound * NT * N < a.V ? from + kRound * NT * N : a.V;
+    for (int k = tid; k < a.K; k += NT) {
+        const int64_t id = a.ids[row * a.K + k];
+        if (id < from || id >= until) continue;
+        const float d = s[2 + k];
+        put(to + id, d == 0.0f ? 0.0f : d * g);
+    }
+}
+
+int parts_of(int64_t R, int64_t V)
+{
+    if (R <= 0 || R > 512 || V < 32768) return 1;
+    int64_t parts = 1024 / R;
+    if (parts > V / 4096) parts = V / 4096;
+    return (int)(parts > 64 ? 64 : parts);
+}
+
+constexpr int64_t kRows = 1 << 21;      // of a launch: less than 2^32 threads
+
+DistillCall rows_from(DistillCall a, int64_t first, int64_t most, size_t size)
+{
+    a.R = a.R - first < most ? a.R - first : most;
+    a.logits = (const char *)a.logits + (size_t)(first * a.row_stride) * size;
+    a.ids += first * a.K;
+    if (a.teacher) a.teacher = (const char *)a.teacher + (size_t)(first * a.K) * size_of(a.teacher_type);
+    if (a.g_loss) a.g_loss += first;
+    if (a.loss) a.loss += first;
+    if (a.stats) a.stats += first * (a.K + 2);
+    if (a.glogits) a.glogits = (char *)a.glogits + (size_t)(first * a.V) * size;
+    return a;
+}
+
+template <class T>
+hipError_t launch_backward(const DistillCall &all, hipStream_t st)
+{
+    constexpr int N = 16 / sizeof(T);
+    prof::Timed timed("token_distill_backward", st);
+    const int64_t pieces = div_up(all.V, (int64_t)N);
+    const int threads = pieces <= 64 * kRound ? 64 : 256;
+    const int64_t chunks = div_up(pieces, (int64_t)threads * kRound), most = (1ll << 23) / chunks > 1 ? (1ll << 23) / chunks : 1;
+    for (int64_t first = 0; first < all.R; first += most) {
+        DistillCall a = rows_from(all, first, most, sizeof(T));
+        a.chunks = (uint32_t)chunks;
+        const unsigned grid = (unsigned)(a.R * chunks);
+        if (threads == 64) distill_back_kernel<T, 64><<<grid, 64, 0, st>>>(a);
+        else distill_back_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class T, bool STEP>
+hipError_t launch_rows(const DistillCall &all, hipStream_t st)
+{
+    prof::Timed timed(STEP ? "token_distill_step" : "token_distill", st);
+    constexpr uint32_t N = 16 / sizeof(T);
+    const uint32_t tokens = all.part_pieces * N < kMarked ? all.part_pieces * N : kMarked, lds = (tokens + 31) / 32 * 4;
+    for (int64_t first = 0; first < all.R; first += kRows) {
+        const DistillCall a = rows_from(all, first, kRows, sizeof(T));
+        const unsigned grid = (unsigned)(a.R * a.parts);
+        if (a.V <= 4096) distill_kernel<T, 64, false, STEP><<<grid, 64, lds, st>>>(a);
+        else distill_kernel<T, 256, false, STEP><<<grid, 256, lds, st>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class T>
+hipError_t launch_forward(DistillCall &a, bool step, hipStream_t st)
+{
+    constexpr uint32_t N = 16 / sizeof(T);
+    const uint32_t pieces = (uint32_t)div_up(a.V, (int64_t)N);
+    a.part_pieces = div_up(pieces, (uint32_t)a.parts);
+    a.parts = (int)div_up(pieces, a.part_pieces);
+    if (a.parts == 1) return step ? launch_rows<T, true>(a, st) : launch_rows<T, false>(a, st);
+    hipError_t e = launch_rows<T, false>(a, st);
+    if (e != hipSuccess) return e;
+    {
+        prof::Timed timed("token_distill_join", st);
+        distill_join_kernel<T><<<(unsigned)a.R, 64, 0, st>>>(a);
+        e = hipGetLastError();
+    }
+    return e != hipSuccess || !step ? e : launch_backward<T>(a, st);
+}
+
+int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, int32_t K, float temperature)
+{
+    if (R < 0 || V <= 0 || row_stride < V || K < 1 || !(temperature >= 1e-30f && temperature <= 1e30f)) return KAN_ERR_INVALID_ARG;
+    if (!known_type(type) || R >= (1ll << 31) || V >= (1ll << 31) - 1 || K > KAN_TEACHER_MAX) return KAN_ERR_UNSUPPORTED;
+    return KAN_OK;
+}
+
+size_t sums_bytes(int64_t R, int64_t V)
+{
+    const int parts = parts_of(R, V);
+    return parts > 1 ? align_up((size_t)R * parts * sizeof(Mass)) : 0;
+}
+
+// the forward call, and the step where `glogits` is there
+int run(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K, const int64_t *ids, const void *teacher,
+        int32_t teacher_type, int32_t teacher_form, float temperature, bool step, const float *g_loss, float *loss, float *stats, void *glogits, void *ws,
+        size_t ws_bytes, hipStream_t st)
+{
+    const int rc = check(R, V, type, row_stride, K, temperature);
+    if (rc != KAN_OK) return rc;
+    if (!known_type(teacher_type) || (teacher_form != KAN_TEACHER_LOGP && teacher_form != KAN_TEACHER_LOGITS)) return KAN_ERR_UNSUPPORTED;
+    if (R == 0) return KAN_OK;
+    if (!logits || !ids || !teacher || misplaced(logits, type) || misplaced8(ids) || misplaced(teacher, teacher_type) || misplaced(loss, KAN_F32) ||
+        misplaced(stats, KAN_F32))
+        return KAN_ERR_INVALID_ARG;
+    if (step && (!g_loss || !glogits || misplaced(g_loss, KAN_F32) || misplaced(glogits, type))) return KAN_ERR_INVALID_ARG;
+    if (bad_workspace(ws, ws_bytes, kan_token_distill_workspace_bytes(R, V, K))) return KAN_ERR_WORKSPACE;
+    DistillCall a = {};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.V = V;
+    a.R = R;
+    a.ids = ids;
+    a.teacher = teacher;
+    a.K = K;
+    a.teacher_type = teacher_type;
+    a.teacher_form = teacher_form;
+    a.t = temperature_of(temperature);
+    a.g_loss = g_loss;
+    a.loss = loss;
+    a.parts = parts_of(R, V);
+    a.part_sums = (Mass *)ws;
+    a.stats = step && a.parts > 1 ? (float *)((char *)ws + sums_bytes(R, V)) : stats;
+    a.glogits = glogits;
+    return status_of(type == KAN_F32 ? launch_forward<float>(a, step, st) : launch_forward<bf16>(a, step, st));
+}
+
+}  // namespace
+}  // namespace kannet
+
+using namespace kannet;
+
+// nothing where rows are not cut; otherwise sums of the parts, and what the step keeps between its passes
+extern "C" size_t kan_token_distill_workspace_bytes(int64_t R, int64_t V, int32_t K)
+{
+    if (V <= 0 || K < 1 || K > KAN_TEACHER_MAX) return 0;
+    const size_t sums = sums_bytes(R, V);
+    return sums ? sums + align_up((size_t)R * (K + 2) * sizeof(float)) : 0;
+}
+
+extern "C" int kan_token_distill_forward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K,
+                                         const int64_t *teacher_ids, const void *teacher, int32_t teacher_type, int32_t teacher_form, float temperature,
+                                         float *loss, float *stats, void *ws, size_t ws_bytes, void *stream)
+{
+    return run(R, V, logits, type, row_stride, K, teacher_ids, teacher, teacher_type, teacher_form, temperature, false, nullptr, loss, stats, nullptr, ws, ws_bytes,
+               (hipStream_t)stream);
+}
+
+extern "C" int kan_token_distill_step(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K, const int64_t *teacher_ids,
+                                      const void *teacher, int32_t teacher_type, int32_t teacher_form, float temperature, const float *g_loss, float *loss,
+                                      void *glogits, void *ws, size_t ws_bytes, void *stream)
+{
+    return run(R, V, logits, type, row_stride, K, teacher_ids, teacher, teacher_type, teacher_form, temperature, true, g_loss, loss, nullptr, glogits, ws, ws_bytes,
+               (hipStream_t)stream);
+}
+
+extern "C" int kan_token_distill_backward(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stride, int32_t K,
+                                          const int64_t *teacher_ids, float temperature, const float *stats, const float *g_loss, void *glogits,
+                                          void *stream)
+{
+    const int rc = check(R, V, type, row_stride, K, temperature);
+    if (rc != KAN_OK) return rc;
+    if (R == 0) return KAN_OK;
+    if (!logits || !teacher_ids || !stats || !g_loss || !glogits || misplaced(logits, type) || misplaced(glogits, type) || misplaced8(teacher_ids) ||
+        misplaced(stats, KAN_F32) || misplaced(g_loss, KAN_F32))
+        return KAN_ERR_INVALID_ARG;
+    DistillCall a = {};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.V = V;
+    a.R = R;
+    a.ids = teacher_ids;
+    a.K = K;
+    a.t = temperature_of(temperature);
+    a.stats = const_cast<float *>(stats);
+    a.g_loss = g_loss;
+    a.glogits = glogits;
+    return status_of(type == KAN_F32 ? launch_backward<float>(a, (hipStream_t)stream) : launch_backward<bf16>(a, (hipStream_t)stream));
+}

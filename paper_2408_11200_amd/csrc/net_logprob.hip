@@ -19,13 +19,12 @@
 // the row the bound of all of it leaves hardly more than `top` of them, put in order by counting for each how many are above it.  (Reading
 // the pieces of the threads that have the bound once more, at the end, cost a quarter of the row: they lie in as many lines.)  The first round's bound
 // stays to the row's end: where it is low for the row, more logits reach it than there is room for, and a second search reads the row again.
-#include "net_device.hpp"
+#include "net_top.hpp"
 
 namespace kannet {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFar = -200.0f;          // 2^-200 is zero in 32 bits: what a term further down adds to the second sum
 
 struct Sums {
@@ -96,134 +95,6 @@ __device__ __forceinline__ Sums join_all(Sums s, float scale, Sums *lds)
     s = lds[0];
     for (int w = 1; w < NT / 64; ++w) s = join(s, lds[w], scale);
     return s;
-}
-
-// Larger logits, and of equal ones the lower index, have the larger key; 0: none.  A NaN is above +infinity, both zeros are one value.
-__device__ __forceinline__ uint64_t key_of(float v, uint32_t index)
-{
-    uint32_t b = __builtin_bit_cast(uint32_t, v);
-    if (v != v) b = 0x7FC00000u;
-    if (v == 0.0f) b = 0u;
-    b = (b >> 31) ? ~b : b | 0x80000000u;
-    return (uint64_t)b << 32 | (uint32_t)~index;
-}
-
-__device__ __forceinline__ float logit_of(uint64_t key)
-{
-    const uint32_t b = (uint32_t)(key >> 32);
-    return __builtin_bit_cast(float, (b >> 31) ? b & 0x7FFFFFFFu : ~b);
-}
-
-// of a lane that is the same for the whole wave
-__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane)
-{
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-}
-
-// of the lane before (lane 0 keeps its own)
-__device__ __forceinline__ uint64_t of_lane_before(uint64_t v)
-{
-    const int hi = (int)(v >> 32), lo = (int)(uint32_t)v;
-    return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, 0x138, 0xF, 0xF, false) << 32 |
-           (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, 0x138, 0xF, 0xF, false);
-}
-
-// A wave's list of keys, best first, one a lane: puts in every lane's `key` (0: none) that is above entry `top` - 1
-__device__ __forceinline__ void put_in(uint64_t &list, uint64_t key, int top, int lane)
-{
-    uint64_t last = of_lane(list, top - 1);
-    uint64_t open = __ballot(key > last);
-    while (open) {
-        const uint64_t k = of_lane(key, __ffsll((unsigned long long)open) - 1);
-        open &= open - 1;
-        if (k <= last) continue;
-        const int at = __popcll(__ballot(list > k));
-        const uint64_t before = of_lane_before(list);
-        list = lane < at ? list : lane == at ? k : before;
-        last = of_lane(list, top - 1);
-    }
-}
-
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v)
-{
-    const int i = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, CTRL, 0xF, 0xF, true));
-}
-
-template <int D>
-__device__ __forceinline__ float swapped(float v, int lane)
-{
-    const f32x2 t = both_halves<2 * D>(v);
-    return (lane & D) ? t.x : t.y;
-}
-
-// of lane ^ X, X = 2^k or 2^k - 1
-template <int X>
-__device__ __forceinline__ float of_partner(float v, int lane)
-{
-    if constexpr (X == 1) return dpp<0xB1>(v);
-    else if constexpr (X == 2) return dpp<0x4E>(v);
-    else if constexpr (X == 3) return dpp<0x1B>(v);
-    else if constexpr (X == 4) return dpp<0x1B>(dpp<0x141>(v));
-    else if constexpr (X == 7) return dpp<0x141>(v);
-    else if constexpr (X == 8) return dpp<0x128>(v);
-    else if constexpr (X == 15) return dpp<0x140>(v);
-    else if constexpr (X == 16) return swapped<16>(v, lane);
-    else if constexpr (X == 31) return dpp<0x140>(swapped<16>(v, lane));
-    else if constexpr (X == 32) return swapped<32>(v, lane);
-    else return dpp<0x140>(swapped<16>(swapped<32>(v, lane), lane));
-}
-
-// the larger value to the lane of the pair whose bit D is clear
-template <int X, int D>
-__device__ __forceinline__ float ordered(float v, int lane)
-{
-    const float o = of_partner<X>(v, lane), hi = fmaxf(v, o), lo = fminf(v, o);
-    return (lane & D) ? lo : hi;
-}
-
-// a wave's values that rise and then fall (or the other way round) in falling order
-template <int D>
-__device__ __forceinline__ float merged(float v, int lane)
-{
-    v = ordered<D, D>(v, lane);
-    if constexpr (D > 1) v = merged<D / 2>(v, lane);
-    return v;
-}
-
-// a wave's values in falling order: sorted halves, the second one mirrored
-template <int S = 64>
-__device__ __forceinline__ float sorted(float v, int lane)
-{
-    if constexpr (S > 2) v = sorted<S / 2>(v, lane);
-    v = ordered<S - 1, S / 2>(v, lane);
-    if constexpr (S > 2) v = merged<S / 4>(v, lane);
-    return v;
-}
-
-// the `top`-th largest of the threads' values, the same in all threads
-template <int NT>
-__device__ __forceinline__ float value_of_rank(float v, int top, int lane, float *lds)
-{
-    v = sorted(v, lane);
-    if constexpr (NT > 64) {
-        lds[threadIdx.x] = v;
-        __syncthreads();
-        v = lds[lane];
-        // of two sorted lists, the larger ones of the first against the other one backwards are the first 64 of both
-        for (int w = 1; w < NT / 64; ++w) v = merged<32>(fmaxf(v, lds[w * 64 + 63 - lane]), lane);
-    }
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), top - 1));
-}
-
-// how many of `count` keys in LDS are above k
-__device__ __forceinline__ int above(const uint64_t *keys, uint32_t count, uint64_t k)
-{
-    int n = 0;
-#pragma unroll 8
-    for (uint32_t i = 0; i < count; ++i) n += keys[i] > k ? 1 : 0;
-    return n;
 }
 
 constexpr int kAhead = 4;

@@ -1,0 +1,241 @@
+// Rows of the states of beams in the order of the beams that have been chosen (kan_net.h).
+//
+// A copy, bound by HBM: each row that moves is written once, the row in whose place it comes is read.  In place the rows of a search can
+// change places with one another, so whoever writes a byte of one of them has to have read that byte of all: a thread has one piece of 16
+// bytes of every row of a search, reads it from the parents' rows, and writes it then.  Pieces of different threads do not overlap, a run's
+// last bytes are read and written as they are, hence no wait between threads, no buffer, and no order of the rows to find.  Rows that
+// stay are left out.  A launch takes up to kMost tensors from its arguments.
+#include "net_device.hpp"
+
+namespace kannet {
+namespace {
+
+constexpr int kMost = 32;               // tensors of a launch
+constexpr int kThreads = 256;
+constexpr int64_t kBlocks = 1 << 23;    // of a launch
+
+struct State {
+    const char *data;                   // the first search's
+    char *out;
+    int64_t stride[3], out_stride[3];
+    uint32_t blocks;                    // of a search
+    uint32_t items, inner, pieces;      // outer * inner * pieces a run
+    uint32_t whole, tail;               // pieces of a run that are whole, and bytes behind them
+    bool place;
+};
+
+struct ReorderCall {
+    State state[kMost];
+    uint32_t first[kMost + 1];          // workgroups of the tensors before
+    int64_t search[kMost];              // the first one
+    const int64_t *parents;
+    int n, B, top;
+};
+static_assert(sizeof(ReorderCall) <= 4096, "kernel arguments");
+
+typedef uint16_t u16_a1 __attribute__((aligned(1)));
+typedef uint32_t u32_a1 __attribute__((aligned(1)));
+typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
+typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
+
+// Rows that move, into[k] <- from[k], k < count <= K; the same for the whole workgroup.  Behind the last one comes the first once more, which is
+// read again, out of the cache, and not written.
+template <int K>
+struct Moves {
+    int from[K], into[K], count;
+};
+
+template <int K>
+__device__ __forceinline__ Moves<K> moves_of(int source)
+{
+    Moves<K> m;
+    uint64_t open = __ballot(source >= 0);
+    const int first = __ffsll((unsigned long long)open) - 1;
+    m.count = __popcll(open);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        m.into[k] = open ? __ffsll((unsigned long long)open) - 1 : first;
+        m.from[k] = __builtin_amdgcn_readlane(source, m.into[k]);
+        open &= open - 1;
+    }
+    return m;
+}
+
+template <int K, class P>
+__device__ __forceinline__ void move(const Moves<K> &m, const char *from, int64_t stride, char *to, int64_t out_stride)
+{
+    typedef const P *From;
+    typedef P *To;
+    P v[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = *(From)(from + m.from[k] * stride);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k < m.count) *(To)(to + m.into[k] * out_stride) = v[k];
+}
+
+template <int K, class P>
+__device__ __forceinline__ void move_item(const State &s, const ReorderCall &a, int64_t search, uint32_t item, int source)
+{
+    const Moves<K> m = moves_of<K>(source);
+    if (item >= s.items) return;
+    const uint32_t piece = item % s.pieces, run = item / s.pieces, in = run % s.inner, block = run / s.inner;
+    const char *from = s.data + search * a.B * s.stride[1] + block * s.stride[0] + in * s.stride[2] + (int64_t)piece * (int)sizeof(P);
+    char *to = s.out + search * a.top * s.out_stride[1] + block * s.out_stride[0] + in * s.out_stride[2] + (int64_t)piece * (int)sizeof(P);
+    if (piece < s.whole) {
+        move<K, P>(m, from, s.stride[1], to, s.out_stride[1]);
+        return;
+    }
+    // a run's last bytes
+    if (sizeof(P) > 8 && (s.tail & 8)) {
+        move<K, u32x2_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        from += 8, to += 8;
+    }
+    if (sizeof(P) > 4 && (s.tail & 4)) {
+        move<K, u32_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        from += 4, to += 4;
+    }
+    if (s.tail & 2) {
+        move<K, u16_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        from += 2, to += 2;
+    }
+    if (s.tail & 1) move<K, uint8_t>(m, from, s.stride[1], to, s.out_stride[1]);
+}
+
+// MOST: rows of a search; P: a piece
+template <int MOST, class P>
+__global__ __launch_bounds__(kThreads) void reorder_kernel(ReorderCall a)
+{
+    int lo = 0, hi = a.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.first[mid] <= blockIdx.x) lo = mid;
+        else hi = mid - 1;
+    }
+    const State &s = a.state[lo];
+    const uint32_t here = blockIdx.x - a.first[lo];
+    const int64_t search = here / s.blocks;
+    const int lane = threadIdx.x & 63;
+    int source = -1;
+    if (lane < a.top) {
+        const int64_t p = a.parents[(a.search[lo] + search) * a.top + lane];
+        if (p >= 0 && p < a.B && !(s.place && p == lane)) source = (int)p;
+    }
+    const int count = __popcll(__ballot(source >= 0));
+    const uint32_t item = here % s.blocks * kThreads + threadIdx.x;
+    if (count == 0) return;
+    if (MOST <= 4 || count <= 4) move_item<4, P>(s, a, search, item, source);
+    else if (MOST <= 8 || count <= 8) move_item<8, P>(s, a, search, item, source);
+    else if (MOST <= 16 || count <= 16) move_item<(MOST < 16 ? MOST : 16), P>(s, a, search, item, source);
+    else if (MOST <= 32 || count <= 32) move_item<(MOST < 32 ? MOST : 32), P>(s, a, search, item, source);
+    else move_item<MOST, P>(s, a, search, item, source);
+}
+
+// whether no two runs overlap
+bool apart(const int64_t (&count)[3], const int64_t (&stride)[3], int64_t bytes)
+{
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (stride[order[j]] > stride[order[j + 1]]) {
+                const int t = order[j];
+                order[j] = order[j + 1];
+                order[j + 1] = t;
+            }
+    __int128 extent = bytes;
+    for (int i : order) {
+        if (count[i] <= 1) continue;
+        if (stride[i] < extent) return false;
+        extent += (__int128)stride[i] * (count[i] - 1);
+    }
+    return true;
+}
+
+int piece_of(int top) { return top <= 16 ? 16 : top <= 32 ? 8 : 4; }
+
+int64_t pieces_of(const kan_state_ref &t, int piece) { return t.bytes / piece + (t.bytes % piece ? 1 : 0); }
+
+int check(int64_t N, int32_t B, int32_t top, int32_t n, const kan_state_ref *list)
+{
+    if (N < 0 || B < 1 || top < 1 || n < 0 || (n > 0 && !list)) return KAN_ERR_INVALID_ARG;
+    if (B > KAN_BEAM_MAX || top > KAN_BEAM_MAX || N >= (1ll << 31) / KAN_BEAM_MAX) return KAN_ERR_UNSUPPORTED;
+    uint64_t seen[64] = {};             // places of outputs, one bit each: the same tensor twice would change places twice, or half
+    for (int i = 0; i < n; ++i) {
+        const kan_state_ref &t = list[i];
+        if (t.outer < 0 || t.inner < 0 || t.bytes < 0) return KAN_ERR_INVALID_ARG;
+        if (t.outer == 0 || t.inner == 0 || t.bytes == 0 || N == 0) continue;
+        if (!t.data || !t.out) return KAN_ERR_INVALID_ARG;
+        const uint64_t place = (uint64_t)(uintptr_t)t.out * 0x9E3779B97F4A7C15ull >> 52, bit = 1ull << place % 64;
+        for (int k = 0; (seen[place / 64] & bit) && k < i; ++k)
+            if (list[k].out == t.out && list[k].outer && list[k].inner && list[k].bytes) return KAN_ERR_INVALID_ARG;
+        seen[place / 64] |= bit;
+        const int64_t rows[3] = {t.outer, N * top, t.inner};
+        if (!apart(rows, t.out_stride, t.bytes)) return KAN_ERR_INVALID_ARG;
+        if (t.data == t.out) {
+            if (top != B) return KAN_ERR_INVALID_ARG;
+            for (int d = 0; d < 3; ++d)
+                if (rows[d] > 1 && t.stride[d] != t.out_stride[d]) return KAN_ERR_INVALID_ARG;
+        }
+        if ((__int128)t.outer * t.inner * pieces_of(t, piece_of(top > B ? top : B)) >= (1ll << 31)) return KAN_ERR_UNSUPPORTED;
+    }
+    return KAN_OK;
+}
+
+hipError_t launch(const ReorderCall &a, hipStream_t st)
+{
+    prof::Timed timed("beam_reorder", st);
+    const unsigned grid = a.first[a.n];
+    if (a.top <= 8) reorder_kernel<8, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
+    else if (a.top <= 16) reorder_kernel<16, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
+    else if (a.top <= 32) reorder_kernel<32, u32x2_a1><<<grid, kThreads, 0, st>>>(a);
+    else reorder_kernel<64, u32_a1><<<grid, kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace kannet
+
+using namespace kannet;
+
+extern "C" int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list, void *stream)
+{
+    const int rc = check(N, B, top, n, list);
+    if (rc != KAN_OK) return rc;
+    if (N == 0 || n == 0) return KAN_OK;
+    if (!parents || misplaced8(parents)) return KAN_ERR_INVALID_ARG;
+    const int piece = piece_of(top);
+    ReorderCall a = {};
+    a.parents = parents;
+    a.B = B;
+    a.top = top;
+    const auto flush = [&]() {
+        const hipError_t e = a.n ? launch(a, (hipStream_t)stream) : hipSuccess;
+        a.n = 0;
+        return e;
+    };
+    for (int i = 0; i < n; ++i) {
+        const kan_state_ref &t = list[i];
+        if (t.outer == 0 || t.inner == 0 || t.bytes == 0) continue;
+        State s = {};
+        for (int d = 0; d < 3; ++d) s.stride[d] = t.stride[d], s.out_stride[d] = t.out_stride[d];
+        s.inner = (uint32_t)t.inner;
+        s.pieces = (uint32_t)pieces_of(t, piece);
+        s.whole = (uint32_t)(t.bytes / piece);
+        s.tail = (uint32_t)(t.bytes % piece);
+        s.items = (uint32_t)(t.outer * t.inner) * s.pieces;
+        s.blocks = div_up(s.items, (uint32_t)kThreads);
+        s.place = t.data == t.out;
+        const int64_t most = kBlocks / s.blocks;
+        for (int64_t search = 0; search < N; search += most) {
+            const int64_t here = N - search < most ? N - search : most;
+            if ((a.n == kMost || (a.n && a.first[a.n] + here * s.blocks > kBlocks)) && flush() != hipSuccess) return KAN_ERR_HIP;
+            s.data = (const char *)t.data + search * B * t.stride[1];
+            s.out = (char *)t.out + search * top * t.out_stride[1];
+            a.state[a.n] = s;
+            a.search[a.n] = search;
+            a.first[a.n + 1] = a.first[a.n] + (uint32_t)(here * s.blocks);
+            ++a.n;
+        }
+    }
+    return status_of(flush());
+}

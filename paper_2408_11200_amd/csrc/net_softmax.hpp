@@ -1,0 +1,106 @@
+// Sums of exponentials over a row of logits, in one pass: the largest logit so far and the sum relative to it, threads and waves joined the same
+// way.  Shared by the operators that need no second sum (net_distill.hip, net_beam.hip).
+#pragma once
+#include "net_top.hpp"
+
+namespace kannet {
+
+// log2(e) / temperature in 32 bits, as the streaming sums take it; what the results are made of is divided by the temperature in 64
+struct Temperature {
+    float scale;
+    double inverse;
+};
+
+inline Temperature temperature_of(float t) { return Temperature{(float)(1.4426950408889634 / (double)t), 1.0 / (double)t}; }
+
+struct Mass {
+    float m, s;         // the largest logit (at least the lowest finite value) and the sum of 2^((v - m) * scale); s = 0: nothing but -infinity
+};
+
+__device__ __forceinline__ float power(float v, float m, float scale) { return __builtin_amdgcn_exp2f((v - m) * scale); }
+
+// one piece: N logits; the largest of them.  The difference is taken before the scaling: logits of the type's lowest value stay finite.
+template <int N>
+__device__ __forceinline__ float add_mass(const float (&v)[N], float scale, Mass &a)
+{
+    float m = v[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) m = fmaxf(m, v[k]);
+    if (m > a.m) {
+        a.s *= power(a.m, m, scale);
+        a.m = m;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) a.s += power(v[k], a.m, scale);
+    return m;
+}
+
+// over a wave: everyone's sum brought to the largest logit first.  All lanes get the first one's bits: the product and the first sum become one fused
+// multiply-add, whose rounding is another one in either lane of a pair.
+__device__ __forceinline__ Mass join_wave(Mass a, float scale)
+{
+    const float m = lane_max<64>(a.m), s = lane_sum<64>(a.s * power(a.m, m, scale));
+    return Mass{m, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, s)))};
+}
+
+// over a workgroup, the same in all threads; the caller's LDS is free again behind the next barrier
+template <int NT>
+__device__ __forceinline__ Mass join_mass(Mass a, float scale, Mass *lds)
+{
+    a = join_wave(a, scale);
+    if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+        __syncthreads();
+        float m = lds[0].m;
+#pragma unroll
+        for (int w = 1; w < NT / 64; ++w) m = fmaxf(m, lds[w].m);
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) s += lds[w].s * power(lds[w].m, m, scale);
+        a = Mass{m, s};
+    }
+    return a;
+}
+
+// the sum over a wave, the same bits in all lanes
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+__device__ __forceinline__ double wave_max(double v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d, 64));
+    return v;
+}
+
+// Four pieces a thread are in flight while four are worked on
+constexpr int kRound = 4;
+
+// The pieces first + u * NT, u < kRound, of a row of `n` logits, where they lie before `end`
+template <class T, int NT, bool STREAM>
+__device__ __forceinline__ void read_round(Raw<T, 16 / (int)sizeof(T)> (&r)[kRound], const T *row, uint32_t first, uint32_t end, int64_t n)
+{
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+        const uint32_t p = first + u * NT;
+        r[u] = raw_at<N, STREAM>(row, (int64_t)p * N, p < end ? n : 0);
+    }
+}
+
+// What lies behind the row's end is -infinity.
+template <int N, class T>
+__device__ __forceinline__ void piece_logits(Raw<T, N> r, uint32_t p, uint32_t n, float (&v)[N])
+{
+    settle(r, (int64_t)p * N, (int64_t)n);
+    unpack(r, v);
+    if (p >= n / N)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = (uint64_t)p * N + k < n ? v[k] : -INFINITY;
+}
+
+}  // namespace kannet

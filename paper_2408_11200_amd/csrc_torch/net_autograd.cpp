@@ -1,4 +1,4 @@
-// Autograd nodes of the operators of kan_net.h, and the clipping of a list of gradients: nothing is computed here.  Without gradients to
+// Autograd nodes of the operators of kan_net.h, and those that have no gradient (the clipping of a list of gradients, the steps of a beam search): nothing is computed here.  Without gradients to
 // record (a server's calls) the node is passed by and nothing is kept.  Forward-mode tangents, which none of the operators has, go to the node,
 // which refuses them: outputs without one would stand for a derivative of zero.
 #include "kan_torch.hpp"
@@ -342,6 +342,159 @@ Tensor clip_gradients(const std::vector<Tensor> &grads, double max_norm, const s
     return norm;
 }
 
+// ---- divergence from a teacher's likely tokens ----------------------------------------------
+
+struct DistillCall {
+    double temperature;
+    int64_t teacher, K;
+};
+
+struct DistillRows {
+    Tensor loss, stats;
+};
+
+DistillRows distill_forward(const Tensor &logits, const Tensor &ids, const Tensor &values, const DistillCall &c, bool keep_stats)
+{
+    const Tensor rows = rows_of(logits), ic = whole(ids), vc = whole(values);
+    const int64_t R = rows.size(0), V = rows.size(1);
+    const auto f = logits.options().dtype(at::kFloat);
+    DistillRows r;
+    r.loss = at::empty(logits.sizes().slice(0, logits.dim() - 1), f);
+    if (keep_stats) r.stats = at::empty({R, c.K + 2}, f);
+    const size_t need = kan_token_distill_workspace_bytes(R, V, (int32_t)c.K);
+    const Tensor ws = need ? bytes_like(logits, need) : Tensor();
+    check(kan_token_distill_forward(R, V, rows.data_ptr(), type_of(rows.scalar_type()), row_stride(rows), (int32_t)c.K, ids_of(ic), data(vc, vc.scalar_type()),
+                                    type_of(vc.scalar_type()), (int32_t)c.teacher, (float)c.temperature, f32(r.loss), f32(r.stats),
+                                    need ? ws.data_ptr() : nullptr, need ? (size_t)ws.numel() : 0, stream()),
+          "kan_token_distill_forward");
+    return r;
+}
+
+struct TokenDistill : torch::autograd::Function<TokenDistill> {
+    static Tensor forward(AutogradContext *ctx, const Tensor &logits, const Tensor &ids, const Tensor &values, DistillCall c)
+    {
+        const DistillRows r = distill_forward(logits, ids, values, c, true);
+        ctx->saved_data["call"] = pack(c);
+        ctx->save_for_backward({logits, ids, r.stats});
+        return r.loss;
+    }
+
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        first_derivatives_only("token_distill");
+        variable_list g(4);
+        if (!ctx->needs_input_grad(0) || !grads[0].defined()) return g;
+        const DistillCall c = unpack<DistillCall>(ctx->saved_data["call"]);
+        const variable_list saved = ctx->get_saved_variables();
+        const Tensor rows = rows_of(saved[0]), ids = whole(saved[1]), g_loss = whole(grads[0]);
+        g[0] = at::empty(saved[0].sizes(), saved[0].options());
+        check(kan_token_distill_backward(rows.size(0), rows.size(1), rows.data_ptr(), type_of(rows.scalar_type()), row_stride(rows), (int32_t)c.K, ids_of(ids),
+                                         (float)c.temperature, static_cast<const float *>(kept(saved[2])), f32(g_loss), g[0].data_ptr(), stream()),
+              "kan_token_distill_backward");
+        return g;
+    }
+};
+
+Tensor token_distill(const Tensor &logits, const Tensor &ids, const Tensor &values, double temperature, int64_t teacher)
+{
+    same(logits.dim() >= 1 && logits.size(-1) > 0, "logits: rows of V values");
+    same(ids.dim() == logits.dim() && ids.sizes() == values.sizes() && ids.sizes().slice(0, ids.dim() - 1) == logits.sizes().slice(0, logits.dim() - 1),
+         "teacher: a list of ids and one of values for each row of logits");
+    same(ids.size(-1) > 0 && ids.size(-1) <= KAN_TEACHER_MAX, "teacher: 1 to 256 tokens a row");
+    together({&logits, &ids, &values});
+    const c10::DeviceGuard on(logits.device());
+    TORCH_CHECK(!recorded({&values}), "token_distill: not differentiable in the teacher's values (detach them)");
+    const DistillCall c = {temperature, teacher, ids.size(-1)};
+    if (recorded({&logits})) return TokenDistill::apply(logits, ids, values, c);
+    return distill_forward(logits, ids, values, c, false).loss;
+}
+
+// ---- beam search ----------------------------------------------------------------------------
+
+uint8_t *flags(const Tensor &t)
+{
+    if (!t.defined()) return nullptr;
+    if (t.scalar_type() != at::kBool && t.scalar_type() != at::kByte) refuse("flags of type bool or uint8");
+    return static_cast<uint8_t *>(data(t, t.scalar_type()));
+}
+
+variable_list beam_select(const Tensor &logits, const Tensor &scores, int64_t top, const Maybe &ended_, int64_t end_id, const Maybe &rank_scale_, double temperature)
+{
+    const Tensor ended = whole(or_none(ended_)), rank_scale = whole(or_none(rank_scale_)), sc = whole(scores);
+    same(scores.dim() == 2 && scores.size(1) > 0 && scores.size(1) <= KAN_BEAM_MAX, "scores: a row of 1 to 64 beams for each search");
+    const int64_t N = scores.size(0), B = scores.size(1);
+    same((logits.dim() == 2 || logits.dim() == 3) && logits.size(-1) > 0, "logits: rows of V values");
+    same(logits.dim() == 2 ? logits.size(0) == N * B : logits.size(0) == N && logits.size(1) == B, "logits: a row for each beam");
+    same((!ended.defined() || ended.sizes() == scores.sizes()) && (!rank_scale.defined() || rank_scale.sizes() == scores.sizes()), "a flag and a scale for each beam");
+    same(top > 0 && top <= KAN_TOP_MAX, "top: 1 to 64");
+    together({&logits, &scores, &ended, &rank_scale});
+    const c10::DeviceGuard on(logits.device());
+    TORCH_CHECK(!recorded({&logits, &scores, &rank_scale}), "beam_select: not differentiable (detach its inputs, or call it under torch.no_grad())");
+    const Tensor rows = rows_of(logits);
+    const int64_t V = rows.size(1);
+    const auto f = logits.options().dtype(at::kFloat);
+    const variable_list out = {at::empty({N, top}, f), at::empty({N, top}, f.dtype(at::kLong)), at::empty({N, top}, f.dtype(at::kLong)), at::empty({N, top}, f.dtype(at::kBool))};
+    const Tensor ws = bytes_like(logits, kan_beam_select_workspace_bytes(N, (int32_t)B, V, (int32_t)top));
+    check(kan_beam_select(N, (int32_t)B, V, rows.data_ptr(), type_of(rows.scalar_type()), row_stride(rows), f32(sc), flags(ended), f32(rank_scale), end_id,
+                          (float)temperature, (int32_t)top, f32(out[0]), const_cast<int64_t *>(ids_of(out[1])), const_cast<int64_t *>(ids_of(out[2])), flags(out[3]),
+                          ws.data_ptr(), (size_t)ws.numel(), stream()),
+          "kan_beam_select");
+    return out;
+}
+
+struct Dimension {
+    int64_t count = 1, stride = 0, out_stride = 0;
+    // one more dimension in front
+    void put_before(int64_t n, int64_t s, int64_t o)
+    {
+        if (n == 1) return;
+        same(count == 1 || (s == stride * count && o == out_stride * count), "states whose dimensions before the rows, and behind them, lie evenly");
+        if (count == 1) stride = s, out_stride = o;
+        count *= n;
+    }
+};
+
+// rows in dimension `dim`, a contiguous end of a row as one run, what is before and between as one dimension each
+kan_state_ref state_of(const Tensor &t, const Tensor &o, int64_t dim)
+{
+    const int64_t size = (int64_t)t.element_size();
+    int64_t run = size, d = t.dim() - 1;
+    for (; d > dim && (t.size(d) == 1 || (t.stride(d) * size == run && o.stride(d) * size == run)); --d) run *= t.size(d);
+    Dimension inner, outer;
+    for (; d > dim; --d) inner.put_before(t.size(d), t.stride(d) * size, o.stride(d) * size);
+    for (--d; d >= 0; --d) outer.put_before(t.size(d), t.stride(d) * size, o.stride(d) * size);
+    return {t.data_ptr(), o.data_ptr(), outer.count, inner.count, run, {outer.stride, t.stride(dim) * size, inner.stride},
+            {outer.out_stride, o.stride(dim) * size, inner.out_stride}};
+}
+
+void beam_reorder(const Tensor &parents, const std::vector<Tensor> &tensors, int64_t beams, const std::vector<Tensor> &out, int64_t dim)
+{
+    const Tensor order = whole(parents);
+    same(parents.dim() == 2 && parents.size(1) > 0 && parents.size(1) <= KAN_BEAM_MAX, "parents: a row of 1 to 64 for each search");
+    same(beams > 0 && beams <= KAN_BEAM_MAX, "beams: 1 to 64");
+    same(tensors.size() == out.size(), "an output for each tensor");
+    together({&parents});
+    const int64_t N = parents.size(0), top = parents.size(1);
+    std::vector<kan_state_ref> list;
+    list.reserve(tensors.size());
+    const bool forward = forward_mode(), graph = at::GradMode::is_enabled();
+    for (size_t i = 0; i < tensors.size(); ++i) {
+        const Tensor &t = tensors[i], &o = out[i];
+        const int64_t d = dim < 0 ? dim + t.dim() : dim;
+        TORCH_CHECK(!(forward && (has_tangent(t) || has_tangent(o))) && !(graph && (t.requires_grad() || o.requires_grad())),
+                    "beam_reorder: not differentiable, its tensors must not require gradients (or call it under torch.no_grad())");
+        same(t.device() == parents.device() && o.device() == parents.device() && t.scalar_type() == o.scalar_type(), "states on the device of the parents, outputs of their type");
+        same(d >= 0 && d < t.dim() && o.dim() == t.dim() && t.size(d) == N * beams && o.size(d) == N * top, "a row of a state for each beam");
+        for (int64_t k = 0; k < t.dim(); ++k) same(k == d || t.size(k) == o.size(k), "an output of a state's shape");
+        if (o.numel() && t.numel()) list.push_back(state_of(t, o, d));
+    }
+    const c10::DeviceGuard on(parents.device());
+    check(kan_beam_reorder(N, (int32_t)beams, (int32_t)top, ids_of(order), (int32_t)list.size(), list.data(), stream()), "kan_beam_reorder");
+    for (const Tensor &o : out)
+        if (!o.is_inference()) o.unsafeGetTensorImpl()->bump_version();
+}
+
+constexpr const char *kDistillOp = "paper_2408_11200_amd::token_distill", *kSelectOp = "paper_2408_11200_amd::beam_select";
 constexpr const char *kNormOp = "paper_2408_11200_amd::block_norm", *kEmbeddingOp = "paper_2408_11200_amd::embedding",
                      *kLogprobOp = "paper_2408_11200_amd::token_logprob";
 
@@ -358,6 +511,8 @@ TORCH_LIBRARY_FRAGMENT(paper_2408_11200_amd, m)
           "float residual_scale, int gate_rows, int branch_type, bool want_h) -> Tensor[]", &block_norm);
     m.def("embedding(Tensor ids, Tensor table, float scale, bool wide) -> Tensor", &embedding_op);
     m.def("token_logprob(Tensor logits, Tensor ids, float temperature, int top) -> Tensor[]", &token_logprob);
+    m.def("token_distill(Tensor logits, Tensor ids, Tensor values, float temperature, int teacher) -> Tensor", &token_distill);
+    m.def("beam_select(Tensor logits, Tensor scores, int top, Tensor? ended, int end_id, Tensor? rank_scale, float temperature) -> Tensor[]", &beam_select);
 }
 
 void define_net(pybind11::module_ &m)
@@ -372,6 +527,16 @@ void define_net(pybind11::module_ &m)
     });
     m.def("token_logprob", [](const Tensor &logits, const Tensor &ids, double temperature, int64_t top) {
         return call(kLogprobOp, &token_logprob, logits, ids, temperature, top);
+    });
+    m.def("token_distill", [](const Tensor &logits, const Tensor &ids, const Tensor &values, double temperature, int64_t teacher) {
+        return call(kDistillOp, &token_distill, logits, ids, values, temperature, teacher);
+    });
+    m.def("beam_select", [](const Tensor &logits, const Tensor &scores, int64_t top, const Maybe &ended, int64_t end_id, const Maybe &rank_scale, double temperature) {
+        return call(kSelectOp, &beam_select, logits, scores, top, ended, end_id, rank_scale, temperature);
+    });
+    m.def("beam_reorder", [](const Tensor &parents, const std::vector<Tensor> &tensors, int64_t beams, const std::vector<Tensor> &out, int64_t dim) {
+        py::gil_scoped_release unlock;
+        beam_reorder(parents, tensors, beams, out, dim);
     });
     m.def("clip_gradients", [](const std::vector<Tensor> &grads, double max_norm, const std::optional<std::vector<Tensor>> &out) {
         py::gil_scoped_release unlock;

@@ -1,6 +1,6 @@
-"""ctypes front end of the operators of include/kan_net.h (block norms, embedding, token log probabilities, clipped gradients): same names as
-the header.  Argument marshalling only, as in `binding`; `autograd` has the same operators on torch's own terms, all but the clipping as
-differentiable functions.
+"""ctypes front end of the operators of include/kan_net.h (block norms, embedding, token log probabilities, distillation, clipped gradients, beam
+search): same names as the header.  Argument marshalling only, as in `binding`; `autograd` has the same operators on torch's own terms, all but the
+clipping and the beams' as differentiable functions.
 """
 import ctypes
 
@@ -11,14 +11,20 @@ from .binding import KAN_OK, KanError, _on_stream, _ptr, _stream, _workspace
 
 EXPORTS = ["kan_block_norm_forward", "kan_block_norm_workspace_bytes", "kan_block_norm_backward", "kan_embedding_forward",
            "kan_embedding_workspace_bytes", "kan_embedding_backward", "kan_token_logprob_forward", "kan_token_logprob_workspace_bytes",
-           "kan_token_logprob_backward", "kan_gradient_norm", "kan_clip_gradients", "kan_clip_workspace_bytes"]
+           "kan_token_logprob_backward", "kan_gradient_norm", "kan_clip_gradients", "kan_clip_workspace_bytes", "kan_token_distill_forward",
+           "kan_token_distill_backward", "kan_token_distill_step", "kan_token_distill_workspace_bytes", "kan_beam_select",
+           "kan_beam_select_workspace_bytes", "kan_beam_reorder"]
 
 KAN_F32, KAN_BF16 = 0, 1
 KAN_NORM_RMS, KAN_NORM_LAYER = 0, 1
 KAN_TOP_MAX = 64
+KAN_TEACHER_LOGP, KAN_TEACHER_LOGITS = 0, 1
+KAN_TEACHER_MAX = 256
+KAN_BEAM_MAX = 64
 TYPES = {torch.float32: KAN_F32, torch.bfloat16: KAN_BF16}
 TYPE_NAMES = {"f32": KAN_F32, "bf16": KAN_BF16}
 NORMS = {"rms": KAN_NORM_RMS, "layer": KAN_NORM_LAYER}
+TEACHERS = {"logp": KAN_TEACHER_LOGP, "logits": KAN_TEACHER_LOGITS}
 PARAMS = ("w_post", "b_post", "gate", "w_pre", "b_pre")
 
 
@@ -37,6 +43,11 @@ class KanBlockNormGrads(ctypes.Structure):
 
 class KanTensorRef(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class KanStateRef(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("outer", ctypes.c_int64), ("inner", ctypes.c_int64), ("bytes", ctypes.c_int64),
+                ("stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3)]
 
 
 F32 = torch.float32
@@ -58,12 +69,18 @@ def load():
           "kan_token_logprob_forward": [i64, i64, vp, i32, i64, vp, f, i32, vp, vp, vp, vp, vp, vp, sz, vp],
           "kan_token_logprob_backward": [i64, i64, vp, i32, i64, vp, f, vp, vp, vp, vp, vp, vp],
           "kan_gradient_norm": [i32, ctypes.POINTER(KanTensorRef), vp, vp, sz, vp],
-          "kan_clip_gradients": [i32, ctypes.POINTER(KanTensorRef), f, vp, vp, sz, vp]}
+          "kan_clip_gradients": [i32, ctypes.POINTER(KanTensorRef), f, vp, vp, sz, vp],
+          "kan_token_distill_forward": [i64, i64, vp, i32, i64, i32, vp, vp, i32, i32, f, vp, vp, vp, sz, vp],
+          "kan_token_distill_backward": [i64, i64, vp, i32, i64, i32, vp, f, vp, vp, vp, vp],
+          "kan_token_distill_step": [i64, i64, vp, i32, i64, i32, vp, vp, i32, i32, f, vp, vp, vp, vp, sz, vp],
+          "kan_beam_select": [i64, i32, i64, vp, i32, i64, vp, vp, vp, i64, f, i32, vp, vp, vp, vp, vp, sz, vp],
+          "kan_beam_reorder": [i64, i32, i32, vp, i32, ctypes.POINTER(KanStateRef), vp]}
     for name, args in of.items():
         getattr(lib, name).restype = ctypes.c_int
         getattr(lib, name).argtypes = args
     for name, args in {"kan_block_norm_workspace_bytes": [d, i64], "kan_embedding_workspace_bytes": [i64, i64, i32],
-                       "kan_token_logprob_workspace_bytes": [i64, i64, i32], "kan_clip_workspace_bytes": [i32]}.items():
+                       "kan_token_logprob_workspace_bytes": [i64, i64, i32], "kan_clip_workspace_bytes": [i32],
+                       "kan_token_distill_workspace_bytes": [i64, i64, i32], "kan_beam_select_workspace_bytes": [i64, i32, i64, i32]}.items():
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = args
     _lib = lib
@@ -293,3 +310,144 @@ def kan_clip_gradients(tensors, max_norm, out=None, norm=None, ws=None, stream=N
     ws = _workspace(lib.kan_clip_workspace_bytes(len(tensors)), norm.device, stream) if ws is None else ws
     _done(lib.kan_clip_gradients(len(tensors), refs, max_norm, _of32(norm), _ptr(ws), ws.numel(), _stream(stream)), "kan_clip_gradients")
     return norm
+
+
+# ---- divergence from a teacher's likely tokens ----------------------------------------------
+
+def _teacher(teacher_ids, values, R):
+    """(K, address of the ids, of the values, their type) of a teacher's lists, [R][K]."""
+    assert teacher_ids.shape == values.shape and teacher_ids.dim() >= 1 and teacher_ids.shape[-1] > 0, "a value for each id, K of them a row"
+    K = teacher_ids.shape[-1]
+    assert teacher_ids.numel() == R * K, "a list for each row"
+    return K, _of(teacher_ids, torch.int64), _of(values, values.dtype), _type(values.dtype)
+
+
+def kan_token_distill_workspace_bytes(R, V, K):
+    return int(load().kan_token_distill_workspace_bytes(R, V, K))
+
+
+def _distill_workspace(lib, R, V, K, ws, device, stream):
+    if ws is None:
+        need = lib.kan_token_distill_workspace_bytes(R, V, K)
+        ws = _workspace(need, device, stream) if need else None
+    return ws, _ptr(ws), 0 if ws is None else ws.numel()
+
+
+def kan_token_distill_forward(logits, teacher_ids, values, temperature=1.0, teacher="logp", out=None, ws=None, stream=None):
+    """dict of loss and stats.  teacher: what the values are, "logp" (log probabilities, the rest of the vocabulary one outcome more) or "logits"."""
+    lib = load()
+    at, R, V, stride = _logits(logits)
+    K, ids_at, values_at, values_type = _teacher(teacher_ids, values, R)
+    out, dev = dict(out or {}), logits.device
+    for name, shape in (("loss", (R,)), ("stats", (R, K + 2))):
+        if name not in out:
+            out[name] = _new(shape, F32, dev, stream)
+        assert out[name].numel() == R * (1 if name == "loss" else K + 2), name
+    ws, ws_at, ws_bytes = _distill_workspace(lib, R, V, K, ws, dev, stream)
+    _done(lib.kan_token_distill_forward(R, V, at, _type(logits.dtype), stride, K, ids_at, values_at, values_type, TEACHERS[teacher], temperature,
+                                        _of32(out["loss"]), _of32(out["stats"]), ws_at, ws_bytes, _stream(stream)), "kan_token_distill_forward")
+    return out
+
+
+def kan_token_distill_backward(logits, teacher_ids, fwd, g_loss, temperature=1.0, glogits=None, stream=None):
+    """fwd: what the forward call returned (its stats)."""
+    at, R, V, stride = _logits(logits)
+    K = teacher_ids.shape[-1]
+    assert teacher_ids.numel() == R * K and fwd["stats"].numel() == R * (K + 2) and g_loss.numel() == R, "a list and a gradient for each row"
+    if glogits is None:
+        glogits = _new((R, V), logits.dtype, logits.device, stream)
+    assert glogits.numel() == R * V, "rows of V gradients"
+    _done(load().kan_token_distill_backward(R, V, at, _type(logits.dtype), stride, K, _of(teacher_ids, torch.int64), temperature, _of32(fwd["stats"]), _of32(g_loss),
+                                            _of(glogits, logits.dtype), _stream(stream)), "kan_token_distill_backward")
+    return glogits
+
+
+def kan_token_distill_step(logits, teacher_ids, values, g_loss, temperature=1.0, teacher="logp", loss=None, glogits=None, ws=None, stream=None):
+    """(loss, glogits) for weights g_loss of the rows that are known before their losses."""
+    lib = load()
+    at, R, V, stride = _logits(logits)
+    K, ids_at, values_at, values_type = _teacher(teacher_ids, values, R)
+    loss = _new((R,), F32, logits.device, stream) if loss is None else loss
+    glogits = _new((R, V), logits.dtype, logits.device, stream) if glogits is None else glogits
+    assert g_loss.numel() == R and loss.numel() == R and glogits.numel() == R * V, "a weight, a loss and a gradient for each row"
+    ws, ws_at, ws_bytes = _distill_workspace(lib, R, V, K, ws, logits.device, stream)
+    _done(lib.kan_token_distill_step(R, V, at, _type(logits.dtype), stride, K, ids_at, values_at, values_type, TEACHERS[teacher], temperature, _of32(g_loss),
+                                     _of32(loss), _of(glogits, logits.dtype), ws_at, ws_bytes, _stream(stream)), "kan_token_distill_step")
+    return loss, glogits
+
+
+# ---- beam search ----------------------------------------------------------------------------
+
+FLAGS = (torch.bool, torch.uint8)
+
+
+def _flags(t):
+    assert t is None or t.dtype in FLAGS, "flags of type bool or uint8"
+    return None if t is None else _of(t, t.dtype)
+
+
+def kan_beam_select_workspace_bytes(N, B, V, top):
+    return int(load().kan_beam_select_workspace_bytes(N, B, V, top))
+
+
+def kan_beam_select(logits, scores, top=None, ended=None, end_id=-1, rank_scale=None, temperature=1.0, out=None, ws=None, stream=None):
+    """dict of scores, tokens, parents, ended: the `top` (default: as many as beams) best continuations of every search.  scores [N][B], logits [N * B][V]."""
+    lib = load()
+    assert scores.dim() == 2 and scores.shape[1] > 0, "scores: a row of beams for each search"
+    at, rows, V, stride = _logits(logits)
+    N, B = scores.shape
+    assert rows == N * B and all(t is None or t.shape == scores.shape for t in (ended, rank_scale)), "a row of logits, a flag and a scale for each beam"
+    top = B if top is None else top
+    out, dev = dict(out or {}), logits.device
+    for name, dtype in (("scores", F32), ("tokens", torch.int64), ("parents", torch.int64), ("ended", torch.bool)):
+        if name not in out:
+            out[name] = _new((N, top), dtype, dev, stream)
+        assert out[name].numel() == N * top, name
+    if ws is None:
+        ws = _workspace(lib.kan_beam_select_workspace_bytes(N, B, V, top), dev, stream)
+    _done(lib.kan_beam_select(N, B, V, at, _type(logits.dtype), stride, _of32(scores), _flags(ended), _of32(rank_scale), end_id, temperature, top,
+                              _of32(out["scores"]), _of(out["tokens"], torch.int64), _of(out["parents"], torch.int64), _flags(out["ended"]), _ptr(ws), ws.numel(),
+                              _stream(stream)), "kan_beam_select")
+    return out
+
+
+def _evenly(dims):
+    """(count, stride, out stride) of dimensions that lie evenly behind one another; dims: sizes above 1 with the strides of both tensors."""
+    count, stride, to = 1, 0, 0
+    for n, s, o in reversed(dims):
+        if count == 1:
+            count, stride, to = n, s, o
+        else:
+            assert s == stride * count and o == to * count, "states whose dimensions before the rows, and behind them, lie evenly"
+            count *= n
+    return count, stride, to
+
+
+def _state(r, t, o, dim, size):
+    """Fills a KanStateRef: rows in dimension `dim`, a contiguous end of a row as one run, what is before and between as one dimension each."""
+    dims = [(n, a * size, b * size) for n, a, b in zip(t.shape, t.stride(), o.stride())]
+    before, behind, run = [d for d in dims[:dim] if d[0] != 1], [d for d in dims[dim + 1:] if d[0] != 1], size
+    while behind and behind[-1][1] == run == behind[-1][2]:
+        run *= behind.pop()[0]
+    r.data, r.out, r.bytes = t.data_ptr(), o.data_ptr(), run
+    r.outer, r.stride[0], r.out_stride[0] = _evenly(before)
+    r.inner, r.stride[2], r.out_stride[2] = _evenly(behind)
+    r.stride[1], r.out_stride[1] = dims[dim][1], dims[dim][2]
+
+
+def kan_beam_reorder(parents, tensors, beams, out=None, dim=0, stream=None):
+    """Row n * top + j of every tensor from its row n * beams + parents[n][j], parents [N][top]: in place, or into the tensors of `out`.  dim: the dimension of the rows."""
+    assert parents.dim() == 2 and parents.shape[1] > 0, "parents: a row for each search"
+    N, top = parents.shape
+    out = tensors if out is None else out
+    assert len(out) == len(tensors), "an output for each tensor"
+    refs, n = (KanStateRef * max(len(tensors), 1))(), 0
+    for t, o in zip(tensors, out):
+        d = dim + t.dim() if dim < 0 else dim
+        assert t.is_cuda and o.device == t.device == parents.device and o.dtype == t.dtype and o.dim() == t.dim() > d >= 0, "states on the device of the parents"
+        assert t.shape[d] == N * beams and o.shape[d] == N * top and t.shape[:d] == o.shape[:d] and t.shape[d + 1:] == o.shape[d + 1:], "a row of a state for each beam"
+        if o.numel():
+            _state(refs[n], t, o, d, t.element_size())
+            n += 1
+    _done(load().kan_beam_reorder(N, beams, top, _of(parents, torch.int64), n, refs, _stream(stream)), "kan_beam_reorder")
+    return out
