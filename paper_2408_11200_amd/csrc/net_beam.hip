@@ -34,7 +34,11 @@ struct BeamCall {
 __device__ __forceinline__ bool finite(float v) { return v - v == 0.0f; }
 
 // whether a beam's logits are looked at
-__device__ __forceinline__ bool goes_on(const BeamCall &a, uint32_t row) { return finite(a.scores[row]) && !(a.ended && a.ended[row]); }
+__device__ __forceinline__ bool goes_on(const BeamCall &a, uint32_t row)
+{
+    const bool ended = a.ended && a.ended[row];
+    return finite(a.scores[row]) && !ended;
+}
 
 // A row, or part blockIdx.x % a.parts of it
 template <class T, int NT, bool STREAM>
@@ -167,25 +171,14 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
     if (lane < (uint32_t)a.top) a.keys[(uint64_t)slot * a.top + lane] = found;
 }
 
-// A candidate of a search: larger ranks first, of equal ones the lower beam, and in a beam the larger key, i.e. logit, then the lower token
-struct Candidate {
-    uint64_t rank, key;         // rank 0: none
-    uint32_t beam;
-};
-
-__device__ __forceinline__ bool before(const Candidate &a, const Candidate &b)
+// A candidate as one number: larger ones first.  The upper 48 bits are those of its rank, ordered like the values (36 bits of the mantissa: a hundredth of a thousandth of
+// what the sum's rounding leaves open), the lower ones its place in the rows' lists, from the end: these lie in the order of beams, parts and likely tokens,
+// so of equal ranks the lower beam is first, and in a beam the lower token.  0: none.
+__device__ __forceinline__ uint64_t candidate_of(double rank, uint32_t place)
 {
-    return a.rank != b.rank ? a.rank > b.rank : a.beam != b.beam ? a.beam < b.beam : a.key > b.key;
+    const uint64_t b = __builtin_bit_cast(uint64_t, rank + 0.0), ordered = (b >> 63) ? ~b : b | 0x8000000000000000ull;     // both zeros are one value
+    return (ordered & ~0xFFFFull) | (0xFFFFu - place);
 }
-
-// larger values have larger keys, none is 0 (both zeros are one value)
-__device__ __forceinline__ uint64_t rank_key(double v)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, v + 0.0);
-    return (b >> 63) ? ~b : b | 0x8000000000000000ull;
-}
-
-__device__ __forceinline__ double rank_value(uint64_t key) { return __builtin_bit_cast(double, (key >> 63) ? key & 0x7FFFFFFFFFFFFFFFull : ~key); }
 
 enum { kOut = 0, kGoesOn = 1, kEnded = 2 };
 
@@ -195,117 +188,111 @@ struct Beam {
     int state;
 };
 
-constexpr uint32_t kRoom = 2048;    // candidates that are put in order by counting
+constexpr uint32_t kLists = 1024;       // of a search: parts of its rows, or rows; an entry's place is below kLists * KAN_TOP_MAX = 2^16
 
-// A workgroup for each search
+// A workgroup for each search: 256 threads where each has one of the lists' entries at most, 1024 otherwise.  What counts is latency: all there is to read
+// is on its way before any of it is looked at, and instead of counting for each candidate how many are above it (128 of them: 7 us) waves sort theirs in
+// registers and join them.
 template <int NT>
 __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
 {
+    constexpr uint32_t kWaves = NT / 64;
+    __shared__ Mass sums[kLists];
     __shared__ Beam beams[KAN_BEAM_MAX];
-    __shared__ Candidate list[kRoom];
-    __shared__ float value[NT];
-    __shared__ Candidate wave_best[NT / 64];
+    __shared__ uint64_t waves_best[kWaves][64];
+    __shared__ uint64_t bound;
+    __shared__ uint16_t open[kLists];
     __shared__ uint32_t count;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, top = a.top, lists = a.B * a.parts, all = lists * top;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), top = a.top, parts = a.parts, lists = a.B * parts;
     const uint32_t first_row = blockIdx.x * a.B;
-    const uint64_t *keys = a.keys + (uint64_t)first_row * a.parts * top;
-    if (tid == 0) count = 0;
-    for (uint32_t b = wave; b < (uint32_t)a.B; b += NT / 64) {
-        const uint32_t row = first_row + b;
-        const float score = a.scores[row], rank_scale = a.rank_scale ? a.rank_scale[row] : 1.0f;
-        Beam beam = {(double)score, 0.0, 0.0f, rank_scale, kOut};
-        if (finite(score) && rank_scale > 0.0f && finite(rank_scale)) {
-            if (a.ended && a.ended[row]) {
-                beam.state = kEnded;
-            } else {
-                Mass part = {kLowest, 0.0f};
-                if (lane < (uint32_t)a.parts) part = a.sums[row * a.parts + lane];
-                beam.most = lane_max<64>(part.m);
-                const double s = wave_sum((double)part.s * exp(((double)part.m - (double)beam.most) * a.t.inverse));
-                beam.log_sum = log(s);
-                if (s > 0.0 && s < (double)INFINITY) beam.state = kGoesOn;
-            }
-        }
-        if (lane == 0) beams[b] = beam;
+    const uint64_t *keys = a.keys + (uint64_t)first_row * parts * top;
+    // A wave looks at 64 entries, of as many lists as there are up to 64 and as many layers as fit beside one another: groups of lists, and of
+    // every group the `step` first layers, dealt out to the waves.
+    const uint32_t width = lists < 64 ? lists : 64, layers = 64 / width, groups = (lists + 63) / 64, group = wave % groups;
+    const uint32_t l = group * 64 + lane % width, step = kWaves / groups * layers;
+    const uint32_t j = wave / groups * layers + lane / width;
+    const bool takes = l < lists && lane < width * layers && wave / groups < kWaves / groups;
+    uint64_t key = takes && j < top ? keys[l * top + j] : 0;
+    Beam mine = {0.0, 0.0, 0.0f, 1.0f, kOut};
+    if (tid < (uint32_t)a.B) {
+        const float score = a.scores[first_row + tid];
+        if (a.rank_scale) mine.rank_scale = a.rank_scale[first_row + tid];
+        const bool ended = a.ended && a.ended[first_row + tid];
+        mine.score = (double)score;
+        if (finite(score) && mine.rank_scale > 0.0f && finite(mine.rank_scale)) mine.state = ended ? kEnded : kGoesOn;
     }
+    for (uint32_t i = tid; i < lists; i += NT) sums[i] = a.sums[(uint64_t)first_row * parts + i];
     __syncthreads();
-    // entry i of the rows' lists
-    const auto candidate = [&](uint32_t i) {
-        const uint32_t b = i / (a.parts * top);
-        const Beam beam = beams[b];
-        Candidate c = {0, 0, b};
-        double score = -(double)INFINITY;
-        if (beam.state == kEnded && i % (a.parts * top) == 0) {
-            score = beam.score;
-            c.key = key_of(0.0f, (uint32_t)a.end_id);
-        } else if (beam.state == kGoesOn) {
-            c.key = keys[i];
-            if (c.key) score = beam.score + (((double)logit_of(c.key) - (double)beam.most) * a.t.inverse - beam.log_sum);
-        }
-        if (finite((float)score)) c.rank = rank_key(score * (double)beam.rank_scale);
-        return c;
-    };
-    // a candidate's rank in 32 bits: none rounds past another
-    const auto rank_of = [&](const Candidate &c) { return c.rank ? (float)rank_value(c.rank) : -INFINITY; };
-    // a bound that `top` candidates reach: the `top`-th best of as many of the lists' first entries as there are threads
-    float bound = -INFINITY;
-    if (all > kRoom / 8) {
-        const uint32_t deep = NT / lists < top ? NT / lists : top, l = tid % lists, j = tid / lists;
-        const Candidate c = j < deep ? candidate(l * top + j) : Candidate{0, 0, 0};
-        bound = value_of_rank<NT>(rank_of(c), top, lane, value);
-        __syncthreads();
-    }
-    for (uint32_t i = tid; i < all; i += NT) {
-        const Candidate c = candidate(i);
-        if (c.rank && rank_of(c) >= bound) {
-            const uint32_t slot = atomicAdd(&count, 1u);
-            if (slot < kRoom) list[slot] = c;
-        }
-    }
-    __syncthreads();
-    const uint32_t n = count;
-    const auto write = [&](uint32_t j, const Candidate &c) {
-        const int64_t at = (int64_t)blockIdx.x * top + j;
-        const Beam beam = beams[c.beam];
-        const int64_t token = (uint32_t)~(uint32_t)c.key;
-        a.out_scores[at] = c.rank ? (float)(rank_value(c.rank) / (double)beam.rank_scale) : -INFINITY;
-        a.tokens[at] = c.rank ? token : -1;
-        a.parents[at] = c.rank ? c.beam : 0;
-        if (a.out_ended) a.out_ended[at] = c.rank && (beam.state == kEnded || token == a.end_id);
-    };
-    if (n <= kRoom) {
-        for (uint32_t i = tid; i < n; i += NT) {
-            const Candidate c = list[i];
-            uint32_t place = 0;
+    if (tid < (uint32_t)a.B) {
+        const Mass *part = sums + tid * parts;
+        float m = kLowest;
 #pragma unroll 4
-            for (uint32_t k = 0; k < n; ++k) place += before(list[k], c) ? 1 : 0;
-            if (place < top) write(place, c);
-        }
-        for (uint32_t j = n + tid; j < top; j += NT) write(j, Candidate{0, 0, 0});
-        return;
+        for (uint32_t p = 0; p < parts; ++p) m = fmaxf(m, part[p].m);
+        double s = 0.0;
+#pragma unroll 4
+        for (uint32_t p = 0; p < parts; ++p) s += (double)(part[p].s * power(part[p].m, m, a.t.scale));
+        mine.most = m;
+        mine.log_sum = log_of(s);
+        if (mine.state == kGoesOn && !(s > 0.0 && s < (double)INFINITY)) mine.state = kOut;
+        beams[tid] = mine;
     }
-    // More candidates reach the bound than there is room for (equal ones in many parts): the best one behind the last that was taken, `top` times
-    Candidate last = {0, 0, 0};
-    for (uint32_t j = 0; j < top; ++j) {
-        Candidate mine = {0, 0, 0};
-        for (uint32_t i = tid; i < all; i += NT) {
-            const Candidate c = candidate(i);
-            if (c.rank && (j == 0 || before(last, c)) && (!mine.rank || before(c, mine))) mine = c;
+    __syncthreads();
+    // the score of entry j of list l, `key` of it; -infinity: none
+    const auto score_of = [&](const Beam &beam, uint32_t j, bool first_part, uint64_t key) {
+        double score = beam.score;
+        bool there = beam.state == kGoesOn && key;
+        if (beam.state == kEnded) there = first_part && j == 0;
+        else score += ((double)logit_of(key) - (double)beam.most) * a.t.inverse - beam.log_sum;
+        return there && finite((float)score) ? score : -(double)INFINITY;
+    };
+    // entry j of list l as a candidate
+    const auto entry = [&](uint32_t l, uint32_t j, uint64_t key) -> uint64_t {
+        const uint32_t b = l / parts;
+        const Beam beam = beams[b];
+        const double score = score_of(beam, j, l == b * parts, key);
+        return score > -(double)INFINITY ? candidate_of(score * (double)beam.rank_scale, l * top + j) : 0;
+    };
+    const uint64_t first = takes && j < top ? entry(l, j, key) : 0;
+    uint64_t best = sorted(first, lane);
+    // two waves' lists at a time, to the first wave
+    const auto join = [&]() {
+#pragma unroll 1
+        for (uint32_t half = kWaves / 2; half >= 1; half /= 2) {
+            if (wave >= half && wave < 2 * half) waves_best[wave][lane] = best;
+            __syncthreads();
+            if (wave < half) best = best_of(best, waves_best[wave + half][63 - lane], lane);
         }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const Candidate o = {(uint64_t)__shfl_xor((unsigned long long)mine.rank, d, 64), (uint64_t)__shfl_xor((unsigned long long)mine.key, d, 64),
-                                 (uint32_t)__shfl_xor((int)mine.beam, d, 64)};
-            if (o.rank && (!mine.rank || before(o, mine))) mine = o;
+    };
+    join();
+    if (step < top) {
+        // What is below `top` others, or below an entry of its list that is, leads to none: left are the rests of the lists whose layers reach the `top`-th best of
+        // these, a wave each.  (All lists layer by layer: 34 us for 256 lists of 64, whose likely tokens are in every eighth one.)
+        const uint64_t seen = of_lane(best, top - 1);
+        if (tid == 0) {
+            bound = seen;
+            count = 0;
         }
-        if (lane == 0) wave_best[wave] = mine;
         __syncthreads();
-        last = wave_best[0];
-        for (int w = 1; w < NT / 64; ++w)
-            if (wave_best[w].rank && (!last.rank || before(wave_best[w], last))) last = wave_best[w];
+        if (takes && j == step - 1 && first > bound) open[atomicAdd(&count, 1u)] = (uint16_t)l;
         __syncthreads();
-        if (tid == 0) write(j, last);               // there are more than kRoom
+        if (wave != 0) best = 0;
+        for (uint32_t i = wave; i < count; i += kWaves) {
+            const uint32_t l = open[i], j = step + lane;
+            const uint64_t c = j < top ? entry(l, j, keys[l * top + j]) : 0;
+            best = best_of(best, of_partner<63>(c, lane), lane);
+        }
+        join();
     }
+    if (wave != 0 || lane >= top) return;
+    const int64_t at = (int64_t)blockIdx.x * top + lane;
+    const uint32_t place = best ? 0xFFFFu - (uint32_t)(best & 0xFFFF) : 0, list = place / top, b = list / parts;
+    const Beam parent = beams[b];
+    const uint64_t found = keys[place];
+    const int64_t token = parent.state == kEnded ? a.end_id : (int64_t)(uint32_t)~(uint32_t)found;
+    a.out_scores[at] = best ? (float)score_of(parent, place % top, list == b * parts, found) : -INFINITY;
+    a.tokens[at] = best ? token : -1;
+    a.parents[at] = best ? b : 0;
+    if (a.out_ended) a.out_ended[at] = best && (parent.state == kEnded || token == a.end_id);
 }
 
 // How rows are cut: few rows are shared among workgroups, four a CU

@@ -127,6 +127,41 @@ __device__ __forceinline__ float value_of_rank(float v, int top, int lane, float
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), top - 1));
 }
 
+// the same networks on keys
+template <int X>
+__device__ __forceinline__ uint64_t of_partner(uint64_t v, int lane)
+{
+    const float lo = of_partner<X>(__builtin_bit_cast(float, (uint32_t)v), lane), hi = of_partner<X>(__builtin_bit_cast(float, (uint32_t)(v >> 32)), lane);
+    return (uint64_t)__builtin_bit_cast(uint32_t, hi) << 32 | __builtin_bit_cast(uint32_t, lo);
+}
+
+template <int X, int D>
+__device__ __forceinline__ uint64_t ordered(uint64_t v, int lane)
+{
+    const uint64_t o = of_partner<X>(v, lane);
+    return ((v > o) != ((lane & D) != 0)) ? v : o;
+}
+
+template <int D>
+__device__ __forceinline__ uint64_t merged(uint64_t v, int lane)
+{
+    v = ordered<D, D>(v, lane);
+    if constexpr (D > 1) v = merged<D / 2>(v, lane);
+    return v;
+}
+
+template <int S = 64>
+__device__ __forceinline__ uint64_t sorted(uint64_t v, int lane)
+{
+    if constexpr (S > 2) v = sorted<S / 2>(v, lane);
+    v = ordered<S - 1, S / 2>(v, lane);
+    if constexpr (S > 2) v = merged<S / 4>(v, lane);
+    return v;
+}
+
+// of a wave's falling list and another one, backwards (entry 63 - lane), the first 64, falling
+__device__ __forceinline__ uint64_t best_of(uint64_t list, uint64_t backwards, int lane) { return merged<32>(list > backwards ? list : backwards, lane); }
+
 // how many of `count` keys in LDS are above k
 __device__ __forceinline__ int above(const uint64_t *keys, uint32_t count, uint64_t k)
 {
