@@ -7,7 +7,7 @@
 //
 // The largest logits come out of the one read: the `top`-th largest of the threads' largest ones is a bound that `top` logits reach.  What
 // reaches the first round's bound is kept, of every later piece what reaches the bound as it is by then (taken anew behind rounds 1, 2, 4, 8, ... where `top`
-// tokens a round would not fit), and what is kept is put in order by counting for each how many are above it.
+// tokens a round would not fit), and what is kept is sorted, 64 keys a wave in registers, and joined.
 #include "net_softmax.hpp"
 
 namespace kannet {
@@ -47,122 +47,95 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
     constexpr int N = 16 / sizeof(T);
     constexpr uint32_t kCandidates = 4 * NT;
     __shared__ Mass wave_sums[NT / 64];
-    __shared__ uint64_t best[kCandidates], shortlist[NT], chosen[KAN_TOP_MAX];
-    __shared__ uint32_t candidates, kept, sources;
+    __shared__ uint64_t best[kCandidates];
+    __shared__ uint32_t candidates, sources;
     __shared__ uint16_t source[NT];
     __shared__ float thread_most[NT];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     if (!goes_on(a, row)) return;
     const T *z = (const T *)a.logits + (int64_t)row * a.row_stride;
     const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N;
     const uint32_t begin = part * a.part_pieces, end = pieces - begin < a.part_pieces ? pieces : begin + a.part_pieces;
     const float scale = a.t.scale;
-    Mass sum = {kLowest, 0.0f};
+    Tally tally = no_tally();
     float most = -INFINITY, bound = NAN;
-    // all logits that are not below the bound, nor -infinity
+    // all logits that are not below the bound, nor -infinity: room for a thread's in one step, then one after another
     const auto collect = [&](const float (&v)[N], uint32_t p) {
+        uint32_t which = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) which |= v[k] >= bound && v[k] > -INFINITY ? 1u << k : 0u;
+        if (!which) return;
+        uint32_t slot = atomicAdd(&candidates, (uint32_t)__popc(which));
 #pragma unroll
         for (int k = 0; k < N; ++k)
-            if (v[k] >= bound && v[k] > -INFINITY) {
-                const uint32_t slot = atomicAdd(&candidates, 1u);
+            if (which >> k & 1) {
                 if (slot < kCandidates) best[slot] = key_of(v[k], p * N + k);
+                ++slot;
             }
     };
-    if (tid == 0) candidates = kept = sources = 0;
-    if (tid < KAN_TOP_MAX) chosen[tid] = 0;
-    Raw<T, N> next[kRound];
-    read_round<T, NT, STREAM>(next, z, begin + tid, end, a.V);
+    if (tid == 0) candidates = sources = 0;
+    Round<T, NT> next;
+    read_round<STREAM>(next, z, begin, end, V);
     __syncthreads();
     const uint32_t rounds = (end - begin + kRound * NT - 1) / (kRound * NT);
     const bool tighten = (uint32_t)a.top * rounds > kCandidates / 2;
     uint32_t round = 0, again = 2;
     for (uint32_t first = begin; first < end; first += kRound * NT) {
-        const uint32_t at = first + tid;
-        Raw<T, N> now[kRound];
-#pragma unroll
-        for (int u = 0; u < kRound; ++u) now[u] = next[u];
-        read_round<T, NT, STREAM>(next, z, at + kRound * NT, end, a.V);
+        const Round<T, NT> now = next;
+        read_round<STREAM>(next, z, first + kRound * NT, end, V);
         // more than there is room for: the rest is not kept (they are searched for behind the loop)
         if (__hip_atomic_load(&candidates, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kCandidates) bound = NAN;
-#pragma unroll
-        for (int u = 0; u < kRound; ++u) {
-            const uint32_t p = at + u * NT;
-            if (p < end) {
-                float v[N];
-                piece_logits<N>(now[u], p, V, v);
-                const float m = add_mass<N>(v, scale, sum);
-                most = fmaxf(most, m);
-                if (m >= bound) collect(v, p);
-            }
-        }
+        each_piece(now, first, end, V, [&](const float (&v)[N], uint32_t p) {
+            const float m = add_piece<N>(v, scale, tally);
+            most = fmaxf(most, m);
+            if (m >= bound) collect(v, p);
+        });
         ++round;
         if (round == 1 || (tighten && round == again)) {
             __syncthreads();
             const float higher = value_of_rank<NT>(most, a.top, lane, thread_most);
             if (round == 1) {
                 bound = higher;
-#pragma unroll
-                for (int u = 0; u < kRound; ++u) {
-                    const uint32_t p = at + u * NT;
-                    if (p < end) {
-                        float v[N];
-                        piece_logits<N>(now[u], p, V, v);
-                        collect(v, p);
-                    }
-                }
+                if (most >= bound) each_piece(now, first, end, V, collect);
             } else {
                 again *= 2;
                 if (bound == bound) bound = higher;
             }
         }
     }
-    sum = join_mass<NT>(sum, scale, wave_sums);
+    const Mass sum = join_mass<NT>(mass_of(tally, scale), scale, wave_sums);
     uint64_t found = 0;
+    __syncthreads();
+    const uint32_t n = candidates;
     if (sum.s == sum.s && sum.s > 0.0f) {           // the same in all threads; a NaN's beam has no candidates
-        __syncthreads();
-        if (rounds > 1) bound = value_of_rank<NT>(most, a.top, lane, thread_most);
-        __syncthreads();
-        uint32_t n = candidates;
         if (n <= kCandidates) {
-            for (uint32_t i = tid; i < n; i += NT) {
-                const uint64_t k = best[i];
-                if (logit_of(k) >= bound) {
-                    const uint32_t slot = atomicAdd(&kept, 1u);
-                    if (slot < NT) shortlist[slot] = k;
-                }
+            for (uint32_t first = 64 * wave; first < n; first += NT) {
+                const uint64_t k = first + lane < n ? best[first + lane] : 0;
+                found = best_of(found, of_partner<63>(sorted(k, lane), lane), lane);
             }
-            __syncthreads();
-            const bool shorter = kept <= NT;
-            const uint64_t *list = shorter ? shortlist : best;
-            n = shorter ? kept : n;
-            for (uint32_t i = tid; i < n; i += NT) {
-                const uint64_t k = list[i];
-                const int place = above(list, n, k);
-                if (place < a.top) chosen[place] = k;
-            }
-            __syncthreads();
-            if (lane < (uint32_t)a.top) found = chosen[lane];
         } else {
             // more than there is room for (many equal logits, rising ones): the pieces of the threads whose largest logit reaches the bound are read
             // again, by every wave into a sorted list of its own
+            bound = value_of_rank<NT>(most, a.top, lane, thread_most);
             if (begin + tid < end && most >= bound && most > -INFINITY) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
             __syncthreads();
             const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
             for (uint32_t first = 64 * wave; first < count; first += NT) {
                 const uint32_t i = first + lane, p = i < count ? begin + source[i / each] + i % each * NT : end;
                 float v[N];
-                piece_logits<N>(raw_at<N>(z, (int64_t)p * N, p < end ? a.V : 0), p, V, v);
-#pragma unroll
+                piece_logits<N>(raw_at<N>(z, (int64_t)p * N, (int64_t)(p < end ? V : 0)), p, V, v);
+#pragma unroll 1
                 for (int k = 0; k < N; ++k) put_in(found, p < end && v[k] >= bound && v[k] > -INFINITY ? key_of(v[k], p * N + k) : 0, a.top, lane);
             }
-            if (NT > 64) {
-                __syncthreads();                // the candidates' number has been read
-                best[tid] = lane < (uint32_t)a.top ? found : 0;
-                __syncthreads();
-                if (wave == 0)
-                    for (uint32_t w = 1; w < NT / 64; ++w) put_in(found, best[64 * w + lane], a.top, lane);
-            }
+        }
+        // two waves' lists at a time, to the first wave
+#pragma unroll 1
+        for (uint32_t half = NT / 128; half >= 1; half /= 2) {
+            __syncthreads();
+            if (wave >= half && wave < 2 * half) best[wave * 64 + lane] = found;
+            __syncthreads();
+            if (wave < half) found = best_of(found, best[(wave + half) * 64 + 63 - lane], lane);
         }
     }
     if (wave != 0) return;

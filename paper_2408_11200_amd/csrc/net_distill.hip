@@ -177,12 +177,38 @@ __device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, dou
         if (e * 64 + lane < a.K) s[2 + e * 64 + lane] = g.listed[e];
 }
 
-// the gradient of a piece's tokens as if none were listed; factor 0: zeros, whatever the logits are
-template <int N>
-__device__ __forceinline__ void piece_gradient(float (&v)[N], float m, float factor, float scale)
+// The gradients of a round's tokens as if none were listed; factor 0: zeros, whatever the logits are
+template <class T, int NT>
+__device__ __forceinline__ void write_round(const Round<T, NT> &r, T *to, uint32_t first, uint32_t V, float m, float factor, float scale)
 {
+    constexpr int N = 16 / (int)sizeof(T);
+    const uint32_t tid = threadIdx.x, pieces = (V + N - 1) / N;
+    const auto gradients = [&](float (&v)[N]) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = factor == 0.0f ? 0.0f : power(v[k], m, scale) * factor;
+        for (int k = 0; k < N; ++k) v[k] = factor == 0.0f ? 0.0f : power(v[k], m, scale) * factor;
+    };
+    if (first + kRound * NT <= V / N) {
+        typedef typename Raw<T, N>::Wide *To;
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            float v[N];
+            unpack(r.r[u], v);
+            gradients(v);
+            __builtin_nontemporal_store(pack<N>(to, v).a, (To)(to + (int64_t)(first + u * NT) * N) + tid);
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t p = first + tid + u * NT;
+            if (p >= pieces) continue;
+            Raw<T, N> own = r.r[u];
+            float v[N];
+            settle(own, (int64_t)p * N, (int64_t)V);
+            unpack(own, v);
+            gradients(v);
+            store_at<N, true>(to, (int64_t)p * N, (int64_t)V, v);
+        }
+    }
 }
 
 // A row, or part blockIdx.x % a.parts of it (few rows are cut; distill_join_kernel does the rest).  STEP: and its gradients.
@@ -201,15 +227,15 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
     const uint32_t begin = part * a.part_pieces, end = pieces - begin < a.part_pieces ? pieces : begin + a.part_pieces;
     const T *z = (const T *)a.logits + row * a.row_stride;
     const float scale = a.t.scale;
-    Raw<T, N> next[kRound];
-    read_round<T, NT, STREAM>(next, z, begin + tid, end, a.V);
+    Round<T, NT> next;
+    read_round<STREAM>(next, z, begin, end, V);
     if (tid == 0) twice = 0;
     List list;
     if (wave == 0 && a.parts == 1) {
         read_list(a, row, z, lane, list);
         if (lane == 0) some = list.some;
     }
-    Mass sum = {kLowest, 0.0f};
+    Tally tally = no_tally();
     for (uint32_t base = begin; base < end; base += kMarked / N) {
         const uint32_t stop = end - base < kMarked / N ? end : base + kMarked / N;
         const uint32_t words = ((stop - base) * N + 31) / 32;
@@ -225,28 +251,19 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         }
         __syncthreads();
         for (uint32_t first = base; first < stop; first += kRound * NT) {
-            const uint32_t at = first + tid;
-            Raw<T, N> now[kRound];
-#pragma unroll
-            for (int u = 0; u < kRound; ++u) now[u] = next[u];
+            const Round<T, NT> now = next;
             // behind the last round, what the next slice begins with
-            const uint32_t after = first + kRound * NT < stop ? at + kRound * NT : stop + tid;
-            read_round<T, NT, STREAM>(next, z, after, end, a.V);
-#pragma unroll
-            for (int u = 0; u < kRound; ++u) {
-                const uint32_t p = at + u * NT;
-                if (p >= stop) continue;
-                float v[N];
-                piece_logits<N>(now[u], p, V, v);
+            read_round<STREAM>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
+            each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p) {
                 const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
                 if (bits)
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = bits >> k & 1 ? -INFINITY : v[k];
-                add_mass<N>(v, scale, sum);
-            }
+                add_piece<N>(v, scale, tally);
+            });
         }
     }
-    sum = join_mass<NT>(sum, scale, wave_sums);
+    const Mass sum = join_mass<NT>(mass_of(tally, scale), scale, wave_sums);
     if (a.parts > 1) {
         if (tid == 0) a.part_sums[row * a.parts + part] = sum;
         return;
@@ -268,20 +285,11 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         T *to = (T *)a.glogits + row * a.V;
         __syncthreads();
         const float m = row_m, factor = row_factor;
-        const int64_t n = factor == 0.0f ? 0 : a.V;         // zeros are written without a look at the logits
+        const uint32_t n = factor == 0.0f ? 0 : V;          // zeros are written without a look at the logits
         for (uint32_t first = 0; first < pieces; first += kRound * NT) {
-            Raw<T, N> r[kRound];
-            read_round<T, NT, false>(r, z, first + tid, pieces, n);
-#pragma unroll
-            for (int u = 0; u < kRound; ++u) {
-                const uint32_t p = first + tid + u * NT;
-                if (p >= pieces) continue;
-                float v[N];
-                settle(r[u], (int64_t)p * N, a.V);
-                unpack(r[u], v);
-                piece_gradient<N>(v, m, factor, scale);
-                store_at<N, true>(to, (int64_t)p * N, a.V, v);
-            }
+            Round<T, NT> r;
+            read_round<false>(r, z, first, pieces, n);
+            write_round(r, to, first, V, m, factor, scale);
         }
         __syncthreads();        // the listed tokens' gradients go on top
         if (wave == 0)
@@ -317,20 +325,11 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
     const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, first = blockIdx.x % a.chunks * (kRound * NT), tid = threadIdx.x;
     const T *z = (const T *)a.logits + row * a.row_stride;
     T *to = (T *)a.glogits + row * a.V;
-    Raw<T, N> r[kRound];
-    read_round<T, NT, false>(r, z, first + tid, pieces, a.V);
+    Round<T, NT> r;
+    read_round<false>(r, z, first, pieces, V);
     const float *s = a.stats + row * (a.K + 2);
     const float g = a.g_loss[row], m = s[0], factor = s[1] == 0.0f ? 0.0f : s[1] * g;
-#pragma unroll
-    for (int u = 0; u < kRound; ++u) {
-        const uint32_t p = first + tid + u * NT;
-        if (p >= pieces) continue;
-        float v[N];
-        settle(r[u], (int64_t)p * N, a.V);
-        unpack(r[u], v);
-        piece_gradient<N>(v, m, factor, a.t.scale);
-        store_at<N, true>(to, (int64_t)p * N, a.V, v);
-    }
+    write_round(r, to, first, V, m, factor, a.t.scale);
     __syncthreads();            // the listed tokens' gradients go on top
     const int64_t from = (int64_t)first * N, until = from + kRound * NT * N < a.V ? from + kRound * NT * N : a.V;
     for (int k = tid; k < a.K; k += NT) {

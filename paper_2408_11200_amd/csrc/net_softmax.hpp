@@ -19,19 +19,42 @@ struct Mass {
 
 __device__ __forceinline__ float power(float v, float m, float scale) { return __builtin_amdgcn_exp2f((v - m) * scale); }
 
-// one piece: N logits; the largest of them.  The difference is taken before the scaling: logits of the type's lowest value stay finite.
+// A thread's sum while it goes over its pieces.  The exponents are v * scale - reference with one rounding, the reference being m * scale rounded to 32 bits:
+// an exact number that all terms share, so what its rounding is off by is made up for once, in the end (a subtraction and a scaling take an instruction an
+// element more).  Where m * scale is not small beside 2^24 that would be too much, or the product not finite: there `reference` is a NaN, and the difference is taken first, which
+// keeps logits of the type's lowest value, and temperatures near 0, finite.
+struct Tally {
+    float m, s, reference;
+};
+
+__device__ __forceinline__ Tally no_tally() { return Tally{kLowest, 0.0f, NAN}; }
+
+// what the terms of a tally are too large by, as an exponent
+__device__ __forceinline__ float excess(const Tally &a, float scale) { return a.reference == a.reference ? __builtin_fmaf(a.m, scale, -a.reference) : 0.0f; }
+
+__device__ __forceinline__ Mass mass_of(const Tally &a, float scale) { return Mass{a.m, a.s * __builtin_amdgcn_exp2f(-excess(a, scale))}; }
+
+// one piece: N logits; the largest of them
 template <int N>
-__device__ __forceinline__ float add_mass(const float (&v)[N], float scale, Mass &a)
+__device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Tally &a)
 {
     float m = v[0];
 #pragma unroll
     for (int k = 1; k < N; ++k) m = fmaxf(m, v[k]);
     if (m > a.m) {
-        a.s *= power(a.m, m, scale);
+        const Mass before = mass_of(a, scale);
+        const float reference = m * scale;
         a.m = m;
+        a.reference = fabsf(reference) <= 4194304.0f ? reference : NAN;
+        a.s = before.s * power(before.m, m, scale) * __builtin_amdgcn_exp2f(excess(a, scale));
     }
+    if (a.reference == a.reference) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) a.s += power(v[k], a.m, scale);
+        for (int k = 0; k < N; ++k) a.s += __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale, -a.reference));
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) a.s += power(v[k], a.m, scale);
+    }
     return m;
 }
 
@@ -99,18 +122,36 @@ __device__ __forceinline__ double log_of(double x)
     return __builtin_fma((double)e, 0.69314718055994531, half + half);
 }
 
-// Four pieces a thread are in flight while four are worked on
+// Four pieces a thread are in flight while four are worked on: a round
 constexpr int kRound = 4;
 
-// The pieces first + u * NT, u < kRound, of a row of `n` logits, where they lie before `end`
-template <class T, int NT, bool STREAM>
-__device__ __forceinline__ void read_round(Raw<T, 16 / (int)sizeof(T)> (&r)[kRound], const T *row, uint32_t first, uint32_t end, int64_t n)
+template <class T, int NT>
+struct Round {
+    static constexpr int N = 16 / (int)sizeof(T);
+    Raw<T, N> r[kRound];
+};
+
+// The pieces first + tid + u * NT, u < kRound, of a row of n logits, where they lie before `end`.  A round all of whose pieces are whole ones needs no look at
+// any of them, and a scalar address.
+template <bool STREAM, class T, int NT>
+__device__ __forceinline__ void read_round(Round<T, NT> &to, const T *row, uint32_t first, uint32_t end, uint32_t n)
 {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = 16 / (int)sizeof(T);
+    const uint32_t tid = threadIdx.x, whole = n / N < end ? n / N : end;
+    if (first + kRound * NT <= whole) {
+        typedef const typename Raw<T, N>::Wide *From;
 #pragma unroll
-    for (int u = 0; u < kRound; ++u) {
-        const uint32_t p = first + u * NT;
-        r[u] = raw_at<N, STREAM>(row, (int64_t)p * N, p < end ? n : 0);
+        for (int u = 0; u < kRound; ++u) {
+            const From from = (From)(row + (int64_t)(first + u * NT) * N) + tid;
+            if constexpr (STREAM) to.r[u].a = __builtin_nontemporal_load(from);
+            else to.r[u].a = *from;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t p = first + tid + u * NT;
+            to.r[u] = raw_at<N, STREAM>(row, (int64_t)p * N, (int64_t)(p < end ? n : 0));
+        }
     }
 }
 
@@ -123,6 +164,31 @@ __device__ __forceinline__ void piece_logits(Raw<T, N> r, uint32_t p, uint32_t n
     if (p >= n / N)
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = (uint64_t)p * N + k < n ? v[k] : -INFINITY;
+}
+
+// f(logits, piece) for each piece of a round
+template <class T, int NT, class F>
+__device__ __forceinline__ void each_piece(const Round<T, NT> &of, uint32_t first, uint32_t end, uint32_t n, F f)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const uint32_t tid = threadIdx.x, whole = n / N < end ? n / N : end;
+    if (first + kRound * NT <= whole) {
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            float v[N];
+            unpack(of.r[u], v);
+            f(v, first + tid + u * NT);
+        }
+    } else {
+#pragma unroll 1
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t p = first + tid + u * NT;
+            if (p >= end) continue;
+            float v[N];
+            piece_logits<N>(u == 0 ? of.r[0] : u == 1 ? of.r[1] : u == 2 ? of.r[2] : of.r[3], p, n, v);
+            f(v, p);
+        }
+    }
 }
 
 }  // namespace kannet
