@@ -5,9 +5,10 @@
 // workgroup for each search: it adds the beams' scores, in 64 bits, and takes the `top` best of what the rows have left.  Rows of beams that have ended
 // or are not there are not read.
 //
-// The largest logits come out of the one read: the `top`-th largest of the threads' largest ones is a bound that `top` logits reach.  What
-// reaches the first round's bound is kept, of every later piece what reaches the bound as it is by then (taken anew behind rounds 1, 2, 4, 8, ... where `top`
-// tokens a round would not fit), and what is kept is sorted, 64 keys a wave in registers, and joined.
+// The largest logits come out of the one read: the `top`-th largest of the threads' largest ones is a bound that `top` logits reach.  Of the first round's pieces
+// and of every later one that reach the bound after the first round (taken anew behind rounds 2, 4, 8, ... where as many would not fit), a wave notes which they are, with their largest
+// logits; behind the row those that reach the bound of all of it, hardly more than `top` of them, are read again, and their logits that do are put in order.
+// (Logits picked from each piece as it passed took the waves through some hundred instructions a piece more where no tokens stand out: 64 x 8 x 131072 bf16 48 us.)
 #include "net_softmax.hpp"
 
 namespace kannet {
@@ -45,8 +46,13 @@ template <class T, int NT, bool STREAM>
 __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
 {
     constexpr int N = 16 / sizeof(T);
-    constexpr uint32_t kCandidates = 4 * NT;
-    __shared__ Mass wave_sums[NT / 64];
+    constexpr uint32_t kCandidates = 4 * NT, kNotes = 512, kWaves = NT / 64;
+    struct Note {
+        float most;
+        uint32_t piece;
+    };
+    __shared__ Mass wave_sums[kWaves];
+    __shared__ Note notes[kWaves][kNotes];
     __shared__ uint64_t best[kCandidates];
     __shared__ uint32_t candidates, sources;
     __shared__ uint16_t source[NT];
@@ -60,64 +66,70 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
     const float scale = a.t.scale;
     Tally tally = no_tally();
     float most = -INFINITY, bound = NAN;
-    // all logits that are not below the bound, nor -infinity: room for a thread's in one step, then one after another
-    const auto collect = [&](const float (&v)[N], uint32_t p) {
-        uint32_t which = 0;
-#pragma unroll
-        for (int k = 0; k < N; ++k) which |= v[k] >= bound && v[k] > -INFINITY ? 1u << k : 0u;
+    uint32_t noted = 0;             // by this wave
+    const auto note = [&](float m, uint32_t p) {
+        const uint64_t which = __ballot(m >= bound && m > -INFINITY);
         if (!which) return;
-        uint32_t slot = atomicAdd(&candidates, (uint32_t)__popc(which));
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (which >> k & 1) {
-                if (slot < kCandidates) best[slot] = key_of(v[k], p * N + k);
-                ++slot;
-            }
+        const uint32_t at = noted + __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, 0));
+        if ((which >> lane & 1) && at < kNotes) notes[wave][at] = Note{m, p};
+        noted += __popcll(which);
     };
     if (tid == 0) candidates = sources = 0;
     Round<T, NT> next;
     read_round<STREAM>(next, z, begin, end, V);
-    __syncthreads();
     const uint32_t rounds = (end - begin + kRound * NT - 1) / (kRound * NT);
-    const bool tighten = (uint32_t)a.top * rounds > kCandidates / 2;
+    const bool tighten = (uint32_t)a.top * rounds > kNotes * kWaves / 4;
     uint32_t round = 0, again = 2;
     for (uint32_t first = begin; first < end; first += kRound * NT) {
         const Round<T, NT> now = next;
         read_round<STREAM>(next, z, first + kRound * NT, end, V);
-        // more than there is room for: the rest is not kept (they are searched for behind the loop)
-        if (__hip_atomic_load(&candidates, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kCandidates) bound = NAN;
-        each_piece(now, first, end, V, [&](const float (&v)[N], uint32_t p) {
+        float piece_most[kRound] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        each_piece(now, first, end, V, [&](const float (&v)[N], uint32_t, int u) {
             const float m = add_piece<N>(v, scale, tally);
             most = fmaxf(most, m);
-            if (m >= bound) collect(v, p);
+            if (u == 0) piece_most[0] = m;
+            else if (u == 1) piece_most[1] = m;
+            else if (u == 2) piece_most[2] = m;
+            else piece_most[3] = m;
         });
-        ++round;
-        if (round == 1 || (tighten && round == again)) {
-            __syncthreads();
-            const float higher = value_of_rank<NT>(most, a.top, lane, thread_most);
-            if (round == 1) {
-                bound = higher;
-                if (most >= bound) each_piece(now, first, end, V, collect);
-            } else {
+        if (++round == 1 || (tighten && round == again)) {
+            if (round > 1) {
+                __syncthreads();
                 again *= 2;
-                if (bound == bound) bound = higher;
             }
+            bound = value_of_rank<NT>(most, a.top, lane, thread_most);
         }
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) note(piece_most[u], first + tid + u * NT);
     }
     const Mass sum = join_mass<NT>(mass_of(tally, scale), scale, wave_sums);
     uint64_t found = 0;
-    __syncthreads();
-    const uint32_t n = candidates;
+    uint32_t n = 0;
     if (sum.s == sum.s && sum.s > 0.0f) {           // the same in all threads; a NaN's beam has no candidates
-        if (n <= kCandidates) {
-            for (uint32_t first = 64 * wave; first < n; first += NT) {
-                const uint64_t k = first + lane < n ? best[first + lane] : 0;
-                found = best_of(found, of_partner<63>(sorted(k, lane), lane), lane);
-            }
-        } else {
+        __syncthreads();
+        if (rounds > 1) bound = value_of_rank<NT>(most, a.top, lane, thread_most);
+        for (uint32_t i = lane; i < (noted < kNotes ? noted : kNotes); i += 64) {
+            const Note from = notes[wave][i];
+            if (from.most < bound) continue;
+            float v[N];
+            piece_logits<N>(raw_at<N>(z, (int64_t)from.piece * N, (int64_t)V), from.piece, V, v);
+            uint32_t which = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k) which |= v[k] >= bound && v[k] > -INFINITY ? 1u << k : 0u;
+            uint32_t slot = atomicAdd(&candidates, (uint32_t)__popc(which));
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (which >> k & 1) {
+                    if (slot < kCandidates) best[slot] = key_of(v[k], from.piece * N + k);
+                    ++slot;
+                }
+        }
+        if (lane == 0 && noted > kNotes) atomicAdd(&candidates, kCandidates + 1u);
+        __syncthreads();
+        n = candidates;
+        if (n > kCandidates) {
             // more than there is room for (many equal logits, rising ones): the pieces of the threads whose largest logit reaches the bound are read
             // again, by every wave into a sorted list of its own
-            bound = value_of_rank<NT>(most, a.top, lane, thread_most);
             if (begin + tid < end && most >= bound && most > -INFINITY) source[atomicAdd(&sources, 1u)] = (uint16_t)tid;
             __syncthreads();
             const uint32_t each = (end - begin + NT - 1) / NT, count = sources * each;
@@ -128,10 +140,15 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
 #pragma unroll 1
                 for (int k = 0; k < N; ++k) put_in(found, p < end && v[k] >= bound && v[k] > -INFINITY ? key_of(v[k], p * N + k) : 0, a.top, lane);
             }
+        } else if (n > 64) {
+            for (uint32_t first = 64 * wave; first < n; first += NT) {
+                const uint64_t k = first + lane < n ? best[first + lane] : 0;
+                found = best_of(found, of_partner<63>(sorted(k, lane), lane), lane);
+            }
         }
         // two waves' lists at a time, to the first wave
 #pragma unroll 1
-        for (uint32_t half = NT / 128; half >= 1; half /= 2) {
+        for (uint32_t half = n > 64 ? kWaves / 2 : 0; half >= 1; half /= 2) {
             __syncthreads();
             if (wave >= half && wave < 2 * half) best[wave * 64 + lane] = found;
             __syncthreads();
@@ -141,7 +158,17 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
     if (wave != 0) return;
     const uint32_t slot = row * a.parts + part;
     if (lane == 0) a.sums[slot] = sum;
-    if (lane < (uint32_t)a.top) a.keys[(uint64_t)slot * a.top + lane] = found;
+    uint64_t *to = a.keys + (uint64_t)slot * a.top;
+    if (n > 64) {
+        if (lane < (uint32_t)a.top) to[lane] = found;
+        return;
+    }
+    // few: each one's place is the number of those above it
+    const uint64_t mine = lane < n ? best[lane] : 0;
+    uint32_t place = 0;
+    for (uint32_t i = 0; i < n; ++i) place += of_lane(mine, i) > mine ? 1 : 0;
+    if (lane >= n) place = lane;
+    if (place < (uint32_t)a.top) to[place] = mine;
 }
 
 // A candidate as one number: larger ones first.  The upper 48 bits are those of its rank, ordered like the values (36 bits of the mantissa: a hundredth of a thousandth of

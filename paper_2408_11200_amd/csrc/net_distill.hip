@@ -254,7 +254,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
             const Round<T, NT> now = next;
             // behind the last round, what the next slice begins with
             read_round<STREAM>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
-            each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p) {
+            each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p, int) {
                 const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
                 if (bits)
 #pragma unroll

@@ -166,7 +166,7 @@ __device__ __forceinline__ void piece_logits(Raw<T, N> r, uint32_t p, uint32_t n
         for (int k = 0; k < N; ++k) v[k] = (uint64_t)p * N + k < n ? v[k] : -INFINITY;
 }
 
-// f(logits, piece) for each piece of a round
+// f(logits, piece, its number in the round) for each piece of a round
 template <class T, int NT, class F>
 __device__ __forceinline__ void each_piece(const Round<T, NT> &of, uint32_t first, uint32_t end, uint32_t n, F f)
 {
@@ -177,7 +177,7 @@ __device__ __forceinline__ void each_piece(const Round<T, NT> &of, uint32_t firs
         for (int u = 0; u < kRound; ++u) {
             float v[N];
             unpack(of.r[u], v);
-            f(v, first + tid + u * NT);
+            f(v, first + tid + u * NT, u);
         }
     } else {
 #pragma unroll 1
@@ -186,7 +186,7 @@ __device__ __forceinline__ void each_piece(const Round<T, NT> &of, uint32_t firs
             if (p >= end) continue;
             float v[N];
             piece_logits<N>(u == 0 ? of.r[0] : u == 1 ? of.r[1] : u == 2 ? of.r[2] : of.r[3], p, n, v);
-            f(v, p);
+            f(v, p, u);
         }
     }
 }
