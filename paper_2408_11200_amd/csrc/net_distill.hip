@@ -14,7 +14,7 @@
 namespace kannet {
 namespace {
 
-constexpr int kEntries = KAN_TEACHER_MAX / 64;          // of the list, a lane
+constexpr int kEntries = KAN_TEACHER_MAX / 64;          // of the list, a lane: E of them, one for up to 64 tokens
 constexpr uint32_t kMarked = 1u << 18;                  // tokens that are marked at a time: 32 KB
 constexpr double kNothing = 1e-300;
 
@@ -35,27 +35,28 @@ struct DistillCall {
 };
 
 // The teacher's list of a row, over a wave: entry e * 64 + lane.
+template <int E>
 struct List {
-    int64_t id[kEntries];           // -1: nothing
-    double p[kEntries], log_p[kEntries];
-    float z[kEntries];              // the student's logit
+    int32_t id[E];                  // -1: nothing
+    double p[E], log_p[E];
+    float z[E];                     // the student's logit
     double p_sum, p_rest;
     bool some;
 };
 
-template <class T>
-__device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, const T *z, int lane, List &l)
+template <class T, int E>
+__device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, const T *z, int lane, List<E> &l)
 {
-    float value[kEntries];
+    float value[E];
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {
+    for (int e = 0; e < E; ++e) {
         const int k = e * 64 + lane;
         l.id[e] = -1;
         l.z[e] = value[e] = -INFINITY;
         if (k < a.K) {
             const int64_t at = row * a.K + k, id = a.ids[at];
             if (id >= 0 && id < a.V) {
-                l.id[e] = id;
+                l.id[e] = (int32_t)id;
                 value[e] = a.teacher_type == KAN_F32 ? ((const float *)a.teacher)[at] : widen(((const bf16 *)a.teacher)[at]);
                 l.z[e] = widen(z[id]);
             }
@@ -65,23 +66,23 @@ __device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, con
     if (a.teacher_form == KAN_TEACHER_LOGITS) {
         float m = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) m = fmaxf(m, value[e]);
+        for (int e = 0; e < E; ++e) m = fmaxf(m, value[e]);
         most = (double)lane_max<64>(m);
         if (most == -(double)INFINITY) most = 0.0;
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e)
-            if (e * 64 < a.K && l.id[e] >= 0) sum += exp(((double)value[e] - most) * a.t.inverse);
-        log_sum = log(wave_sum(sum));
+        for (int e = 0; e < E; ++e)
+            if (e * 64 < a.K && l.id[e] >= 0) sum += exp_of(((double)value[e] - most) * a.t.inverse);
+        log_sum = log_of(wave_sum(sum));
     }
     sum = 0.0;
     bool some = false;
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {
+    for (int e = 0; e < E; ++e) {
         l.p[e] = l.log_p[e] = 0.0;
         if (e * 64 < a.K && l.id[e] >= 0) {
             const bool logits = a.teacher_form == KAN_TEACHER_LOGITS && value[e] != -INFINITY;
             l.log_p[e] = logits ? ((double)value[e] - most) * a.t.inverse - log_sum : (double)value[e];
-            l.p[e] = exp(l.log_p[e]);
+            l.p[e] = exp_of(l.log_p[e]);
             sum += l.p[e];
             some = some || l.p[e] != 0.0;
         }
@@ -92,63 +93,75 @@ __device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, con
 }
 
 // What a row's gradients are made of
+template <int E>
 struct RowGradient {
     float m, factor;            // of a token off the list: exp2((z - m) * scale) * factor
-    float listed[kEntries];     // of the list's
+    float listed[E];            // of the list's
 };
 
-// A row's loss and gradients from its list and the sum over the other tokens, by one wave.  `twice`: a token may be in the list more than once;
-// `tokens` [K] is room in LDS for finding out which.
-__device__ __forceinline__ double finish_row(const DistillCall &a, const List &l, Mass others, bool twice, uint32_t *tokens, int lane, RowGradient &g)
+// Whether a token is in the list more than once, the same in all lanes
+template <int E>
+__device__ __forceinline__ bool repeats(const List<E> &l, int K, int lane)
 {
-    bool first[kEntries];
-    double p_all[kEntries];         // of all entries of a token
+    bool again = false;
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {
+    for (int of = 0; of < E; ++of)
+        for (int k = 0; k < 64 && of * 64 + k < K; ++k) {
+            const int32_t id = __builtin_amdgcn_readlane(l.id[of], k);
+#pragma unroll
+            for (int e = 0; e < E; ++e) again = again || (id >= 0 && l.id[e] == id && (e != of || lane != k));
+        }
+    return __any(again);
+}
+
+// A row's loss and gradients from its list and the sum over the other tokens, by one wave.  `twice`: a token is in the list more than once.
+template <int E>
+__device__ __forceinline__ double finish_row(const DistillCall &a, const List<E> &l, Mass others, bool twice, int lane, RowGradient<E> &g)
+{
+    bool first[E];
+    double p_all[E];                // of all entries of a token
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
         first[e] = l.id[e] >= 0;
         p_all[e] = l.p[e];
     }
     if (twice) {
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e)
-            if (e * 64 + lane < a.K) tokens[e * 64 + lane] = (uint32_t)l.id[e];
-        double *p = (double *)(tokens + KAN_TEACHER_MAX);
+        for (int e = 0; e < E; ++e) p_all[e] = 0.0;
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e)
-            if (e * 64 + lane < a.K) p[e * 64 + lane] = l.p[e];
-        __builtin_amdgcn_wave_barrier();
+        for (int of = 0; of < E; ++of)
+            for (int k = 0; k < 64 && of * 64 + k < a.K; ++k) {
+                const int32_t id = __builtin_amdgcn_readlane(l.id[of], k);
+                const double p = __builtin_bit_cast(double, of_lane(__builtin_bit_cast(uint64_t, l.p[of]), k));
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) {
-            if (l.id[e] < 0) continue;
-            p_all[e] = 0.0;
-            for (int k = 0; k < a.K; ++k)
-                if (tokens[k] == (uint32_t)l.id[e]) {
-                    p_all[e] += p[k];
-                    if (k < e * 64 + lane) first[e] = false;
-                }
-        }
+                for (int e = 0; e < E; ++e)
+                    if (l.id[e] == id) {
+                        p_all[e] += p;
+                        if (of * 64 + k < e * 64 + lane) first[e] = false;
+                    }
+            }
     }
     const bool rest = !(others.s == 0.0f);          // a NaN counts
     float m = rest ? others.m : -INFINITY;
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) m = fmaxf(m, l.z[e]);
+    for (int e = 0; e < E; ++e) m = fmaxf(m, l.z[e]);
     const double M = (double)lane_max<64>(m);
     const bool empty = M == -(double)INFINITY && !rest;
-    double weight[kEntries], sum = 0.0;
+    double weight[E], sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {
+    for (int e = 0; e < E; ++e) {
         weight[e] = 0.0;
         if (e * 64 < a.K && l.id[e] >= 0) {
-            weight[e] = exp(((double)l.z[e] - M) * a.t.inverse);
+            weight[e] = exp_of(((double)l.z[e] - M) * a.t.inverse);
             if (first[e]) sum += weight[e];
         }
     }
-    const double down = ((double)others.m - M) * a.t.inverse, off = rest ? (double)others.s * exp(down) : 0.0;
-    const double total = wave_sum(sum) + off, inverse = 1.0 / total, log_total = log(total), q_rest = off * inverse;
+    const double down = ((double)others.m - M) * a.t.inverse, off = rest ? (double)others.s * exp_of(down) : 0.0;
+    const double total = wave_sum(sum) + off, inverse = 1.0 / total, log_total = log_of(total), q_rest = off * inverse;
     const double p_rest = q_rest >= kNothing ? l.p_rest : 0.0, P = l.p_sum + p_rest;
     double loss = 0.0;
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) {
+    for (int e = 0; e < E; ++e) {
         g.listed[e] = 0.0f;
         if (e * 64 < a.K && l.id[e] >= 0) {
             if (l.p[e] != 0.0) loss += l.p[e] * (l.log_p[e] - (((double)l.z[e] - M) * a.t.inverse - log_total));
@@ -156,14 +169,15 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List &l
         }
     }
     loss = wave_sum(loss);
-    if (p_rest > 0.0) loss += p_rest * (log(p_rest) - (down + log((double)others.s) - log_total));
+    if (p_rest > 0.0) loss += p_rest * (log_of(p_rest) - (down + log_of((double)others.s) - log_total));
     // (without others no token asks for the factor but the masked ones of a row with a NaN among the listed)
     g.m = rest && l.some ? others.m : 0.0f;
     g.factor = !l.some || empty ? 0.0f : rest ? (float)((q_rest * P - p_rest) * a.t.inverse / (double)others.s) : total == total ? 0.0f : NAN;
     return !l.some ? 0.0 : empty ? (double)INFINITY : loss;
 }
 
-__device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, double loss, const RowGradient &g, int lane)
+template <int E>
+__device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, double loss, const RowGradient<E> &g, int lane)
 {
     if (lane == 0 && a.loss) a.loss[row] = (float)loss;
     if (!a.stats) return;
@@ -173,7 +187,7 @@ __device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, dou
         s[1] = g.factor;
     }
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e)
+    for (int e = 0; e < E; ++e)
         if (e * 64 + lane < a.K) s[2 + e * 64 + lane] = g.listed[e];
 }
 
@@ -212,13 +226,12 @@ __device__ __forceinline__ void write_round(const Round<T, NT> &r, T *to, uint32
 }
 
 // A row, or part blockIdx.x % a.parts of it (few rows are cut; distill_join_kernel does the rest).  STEP: and its gradients.
-template <class T, int NT, bool STREAM, bool STEP>
+template <class T, int NT, int E, bool STEP>
 __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
 {
     constexpr int N = 16 / sizeof(T);
     extern __shared__ uint32_t marks[];
     __shared__ Mass wave_sums[NT / 64];
-    __shared__ double room[KAN_TEACHER_MAX + KAN_TEACHER_MAX / 2];
     __shared__ uint32_t twice, some;
     __shared__ float row_m, row_factor;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -228,9 +241,9 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
     const T *z = (const T *)a.logits + row * a.row_stride;
     const float scale = a.t.scale;
     Round<T, NT> next;
-    read_round<STREAM>(next, z, begin, end, V);
+    read_round<false>(next, z, begin, end, V);
     if (tid == 0) twice = 0;
-    List list;
+    List<E> list;
     if (wave == 0 && a.parts == 1) {
         read_list(a, row, z, lane, list);
         if (lane == 0) some = list.some;
@@ -253,7 +266,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         for (uint32_t first = base; first < stop; first += kRound * NT) {
             const Round<T, NT> now = next;
             // behind the last round, what the next slice begins with
-            read_round<STREAM>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
+            read_round<false>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
             each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p, int) {
                 const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
                 if (bits)
@@ -268,10 +281,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         if (tid == 0) a.part_sums[row * a.parts + part] = sum;
         return;
     }
-    RowGradient g;
+    RowGradient<E> g;
     float weight = 0.0f;
     if (wave == 0) {
-        const double loss = finish_row(a, list, sum, twice != 0, (uint32_t *)room, lane, g);
+        const double loss = finish_row(a, list, sum, twice != 0, lane, g);
         write_row(a, row, loss, g, lane);
         if constexpr (STEP) {
             weight = a.g_loss[row];
@@ -294,25 +307,24 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         __syncthreads();        // the listed tokens' gradients go on top
         if (wave == 0)
 #pragma unroll
-            for (int e = 0; e < kEntries; ++e)
+            for (int e = 0; e < E; ++e)
                 if (list.id[e] >= 0) put(to + list.id[e], g.listed[e] == 0.0f ? 0.0f : g.listed[e] * weight);
     }
 }
 
 // A wave for each row that was cut, at most 64 parts
-template <class T>
+template <class T, int E>
 __global__ __launch_bounds__(64) void distill_join_kernel(DistillCall a)
 {
-    __shared__ double room[KAN_TEACHER_MAX + KAN_TEACHER_MAX / 2];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
     Mass sum = {kLowest, 0.0f};
     if (lane < a.parts) sum = a.part_sums[row * a.parts + lane];
-    List list;
+    List<E> list;
     read_list(a, row, (const T *)a.logits + row * a.row_stride, lane, list);
     sum = join_wave(sum, a.t.scale);
-    RowGradient g;
-    const double loss = finish_row(a, list, sum, true, (uint32_t *)room, lane, g);
+    RowGradient<E> g;
+    const double loss = finish_row(a, list, sum, repeats(list, a.K, lane), lane, g);
     write_row(a, row, loss, g, lane);
 }
 
@@ -392,8 +404,10 @@ hipError_t launch_rows(const DistillCall &all, hipStream_t st)
     for (int64_t first = 0; first < all.R; first += kRows) {
         const DistillCall a = rows_from(all, first, kRows, sizeof(T));
         const unsigned grid = (unsigned)(a.R * a.parts);
-        if (a.V <= 4096) distill_kernel<T, 64, false, STEP><<<grid, 64, lds, st>>>(a);
-        else distill_kernel<T, 256, false, STEP><<<grid, 256, lds, st>>>(a);
+        if (a.K <= 64 && a.V <= 4096) distill_kernel<T, 64, 1, STEP><<<grid, 64, lds, st>>>(a);
+        else if (a.K <= 64) distill_kernel<T, 256, 1, STEP><<<grid, 256, lds, st>>>(a);
+        else if (a.V <= 4096) distill_kernel<T, 64, kEntries, STEP><<<grid, 64, lds, st>>>(a);
+        else distill_kernel<T, 256, kEntries, STEP><<<grid, 256, lds, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -412,7 +426,8 @@ hipError_t launch_forward(DistillCall &a, bool step, hipStream_t st)
     if (e != hipSuccess) return e;
     {
         prof::Timed timed("token_distill_join", st);
-        distill_join_kernel<T><<<(unsigned)a.R, 64, 0, st>>>(a);
+        if (a.K <= 64) distill_join_kernel<T, 1><<<(unsigned)a.R, 64, 0, st>>>(a);
+        else distill_join_kernel<T, kEntries><<<(unsigned)a.R, 64, 0, st>>>(a);
         e = hipGetLastError();
     }
     return e != hipSuccess || !step ? e : launch_backward<T>(a, st);
