@@ -142,6 +142,12 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
             }
     }
     const bool rest = !(others.s == 0.0f);          // a NaN counts
+    double rest_sum = (double)others.s;
+    if (others.s > 1024.0f) {       // a reference far below the largest logit: one near it, which leaves the factor in a float's range
+        const float from = others.m;
+        others.m += __builtin_amdgcn_logf(others.s) / a.t.scale;
+        rest_sum *= exp_of(((double)from - (double)others.m) * a.t.inverse);
+    }
     float m = rest ? others.m : -INFINITY;
 #pragma unroll
     for (int e = 0; e < E; ++e) m = fmaxf(m, l.z[e]);
@@ -156,7 +162,7 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
             if (first[e]) sum += weight[e];
         }
     }
-    const double down = ((double)others.m - M) * a.t.inverse, off = rest ? (double)others.s * exp_of(down) : 0.0;
+    const double down = ((double)others.m - M) * a.t.inverse, off = rest ? rest_sum * exp_of(down) : 0.0;
     const double total = wave_sum(sum) + off, inverse = 1.0 / total, log_total = log_of(total), q_rest = off * inverse;
     const double p_rest = q_rest >= kNothing ? l.p_rest : 0.0, P = l.p_sum + p_rest;
     double loss = 0.0;
@@ -169,10 +175,10 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
         }
     }
     loss = wave_sum(loss);
-    if (p_rest > 0.0) loss += p_rest * (log_of(p_rest) - (down + log_of((double)others.s) - log_total));
+    if (p_rest > 0.0) loss += p_rest * (log_of(p_rest) - (down + log_of(rest_sum) - log_total));
     // (without others no token asks for the factor but the masked ones of a row with a NaN among the listed)
     g.m = rest && l.some ? others.m : 0.0f;
-    g.factor = !l.some || empty ? 0.0f : rest ? (float)((q_rest * P - p_rest) * a.t.inverse / (double)others.s) : total == total ? 0.0f : NAN;
+    g.factor = !l.some || empty ? 0.0f : rest ? (float)((q_rest * P - p_rest) * a.t.inverse / rest_sum) : total == total ? 0.0f : NAN;
     return !l.some ? 0.0 : empty ? (double)INFINITY : loss;
 }
 
@@ -191,35 +197,60 @@ __device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, dou
         if (e * 64 + lane < a.K) s[2 + e * 64 + lane] = g.listed[e];
 }
 
-// The gradients of a round's tokens as if none were listed; factor 0: zeros, whatever the logits are
+// What makes a row's gradients as if no token were listed, the same for a workgroup: 2^(v * scale - reference) * factor, as in a tally, or where the reference is
+// too large for that (a NaN) 2^((v - m) * scale) * factor; factor 0: zeros, whatever the logits are.
+struct RowFactor {
+    float m, reference, factor;
+};
+
+__device__ __forceinline__ RowFactor row_factor(float m, float factor, float scale)
+{
+    m = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, m)));
+    factor = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, factor)));
+    const float reference = m * scale;
+    const bool near = fabsf(reference) <= kNear;
+    return RowFactor{m, near ? reference : NAN, near ? factor * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -reference)) : factor};
+}
+
+template <int N>
+__device__ __forceinline__ void gradients(float (&v)[N], const RowFactor &g, float scale)
+{
+    if (g.factor == 0.0f) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = 0.0f;
+    } else if (g.reference == g.reference) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale, -g.reference)) * g.factor;
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = power(v[k], g.m, scale) * g.factor;
+    }
+}
+
 template <class T, int NT>
-__device__ __forceinline__ void write_round(const Round<T, NT> &r, T *to, uint32_t first, uint32_t V, float m, float factor, float scale)
+__device__ __forceinline__ void write_round(const Round<T, NT> &r, T *to, uint32_t first, uint32_t V, const RowFactor &g, float scale)
 {
     constexpr int N = 16 / (int)sizeof(T);
     const uint32_t tid = threadIdx.x, pieces = (V + N - 1) / N;
-    const auto gradients = [&](float (&v)[N]) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = factor == 0.0f ? 0.0f : power(v[k], m, scale) * factor;
-    };
     if (first + kRound * NT <= V / N) {
         typedef typename Raw<T, N>::Wide *To;
 #pragma unroll
         for (int u = 0; u < kRound; ++u) {
             float v[N];
             unpack(r.r[u], v);
-            gradients(v);
+            gradients(v, g, scale);
             __builtin_nontemporal_store(pack<N>(to, v).a, (To)(to + (int64_t)(first + u * NT) * N) + tid);
         }
     } else {
-#pragma unroll
+#pragma unroll 1
         for (int u = 0; u < kRound; ++u) {
             const uint32_t p = first + tid + u * NT;
             if (p >= pieces) continue;
-            Raw<T, N> own = r.r[u];
+            Raw<T, N> own = u == 0 ? r.r[0] : u == 1 ? r.r[1] : u == 2 ? r.r[2] : r.r[3];
             float v[N];
             settle(own, (int64_t)p * N, (int64_t)V);
             unpack(own, v);
-            gradients(v);
+            gradients(v, g, scale);
             store_at<N, true>(to, (int64_t)p * N, (int64_t)V, v);
         }
     }
@@ -233,7 +264,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
     extern __shared__ uint32_t marks[];
     __shared__ Mass wave_sums[NT / 64];
     __shared__ uint32_t twice, some;
-    __shared__ float row_m, row_factor;
+    __shared__ float of_row[2];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / a.parts;
     const uint32_t part = blockIdx.x % a.parts, V = (uint32_t)a.V, pieces = (V + N - 1) / N;
@@ -267,13 +298,19 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
             const Round<T, NT> now = next;
             // behind the last round, what the next slice begins with
             read_round<false>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
-            each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p, int) {
+            const auto unmarked = [&](float (&v)[N], uint32_t p) {
                 const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
                 if (bits)
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = bits >> k & 1 ? -INFINITY : v[k];
-                add_piece<N>(v, scale, tally);
-            });
+            };
+            const bool whole = first + kRound * NT <= (V / N < stop ? V / N : stop);
+            if (!whole || tally.reference != tally.reference ||
+                !add_whole_round(now, scale, tally, [&](float (&v)[N], int u) { unmarked(v, first + tid + u * NT); }))
+                each_piece(now, first, stop, V, [&](float (&v)[N], uint32_t p, int) {
+                    unmarked(v, p);
+                    add_piece<N>(v, scale, tally);
+                });
         }
     }
     const Mass sum = join_mass<NT>(mass_of(tally, scale), scale, wave_sums);
@@ -289,20 +326,24 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         if constexpr (STEP) {
             weight = a.g_loss[row];
             if (lane == 0) {
-                row_m = g.m;
-                row_factor = g.factor == 0.0f ? 0.0f : g.factor * weight;
+                of_row[0] = g.m;
+                of_row[1] = g.factor == 0.0f ? 0.0f : g.factor * weight;
             }
         }
     }
     if constexpr (STEP) {
         T *to = (T *)a.glogits + row * a.V;
         __syncthreads();
-        const float m = row_m, factor = row_factor;
-        const uint32_t n = factor == 0.0f ? 0 : V;          // zeros are written without a look at the logits
-        for (uint32_t first = 0; first < pieces; first += kRound * NT) {
-            Round<T, NT> r;
-            read_round<false>(r, z, first, pieces, n);
-            write_round(r, to, first, V, m, factor, scale);
+        const RowFactor rest = row_factor(of_row[0], of_row[1], scale);
+        const uint32_t n = rest.factor == 0.0f ? 0 : V;          // zeros are written without a look at the logits
+        // from the row's end, where it has been read last
+        const uint32_t rounds = (pieces + kRound * NT - 1) / (kRound * NT);
+        Round<T, NT> r;
+        read_round<true>(r, z, (rounds - 1) * kRound * NT, pieces, n);
+        for (uint32_t i = rounds; i-- > 0;) {
+            const Round<T, NT> now = r;
+            if (i) read_round<true>(r, z, (i - 1) * kRound * NT, pieces, n);
+            write_round(now, to, i * kRound * NT, V, rest, scale);
         }
         __syncthreads();        // the listed tokens' gradients go on top
         if (wave == 0)
@@ -340,8 +381,8 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
     Round<T, NT> r;
     read_round<false>(r, z, first, pieces, V);
     const float *s = a.stats + row * (a.K + 2);
-    const float g = a.g_loss[row], m = s[0], factor = s[1] == 0.0f ? 0.0f : s[1] * g;
-    write_round(r, to, first, V, m, factor, a.t.scale);
+    const float g = a.g_loss[row];
+    write_round(r, to, first, V, row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale), a.t.scale);
     __syncthreads();            // the listed tokens' gradients go on top
     const int64_t from = (int64_t)first * N, until = from + kRound * NT * N < a.V ? from + kRound * NT * N : a.V;
     for (int k = tid; k < a.K; k += NT) {

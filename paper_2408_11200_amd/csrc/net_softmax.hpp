@@ -14,15 +14,26 @@ struct Temperature {
 inline Temperature temperature_of(float t) { return Temperature{(float)(1.4426950408889634 / (double)t), 1.0 / (double)t}; }
 
 struct Mass {
-    float m, s;         // the largest logit (at least the lowest finite value) and the sum of 2^((v - m) * scale); s = 0: nothing but -infinity
+    float m, s;         // a logit, the largest one or near it, and the sum of 2^((v - m) * scale); the lowest finite value and 0: nothing but -infinity
 };
 
 __device__ __forceinline__ float power(float v, float m, float scale) { return __builtin_amdgcn_exp2f((v - m) * scale); }
+
+// Four pieces a thread are in flight while four are worked on: a round
+constexpr int kRound = 4;
+
+template <class T, int NT>
+struct Round {
+    static constexpr int N = 16 / (int)sizeof(T);
+    Raw<T, N> r[kRound];
+};
 
 // A thread's sum while it goes over its pieces.  The exponents are v * scale - reference with one rounding, the reference being m * scale rounded to 32 bits:
 // an exact number that all terms share, so what its rounding is off by is made up for once, in the end (a subtraction and a scaling take an instruction an
 // element more).  Where m * scale is not small beside 2^24 that would be too much, or the product not finite: there `reference` is a NaN, and the difference is taken first, which
 // keeps logits of the type's lowest value, and temperatures near 0, finite.
+constexpr float kNear = 4194304.0f;     // 2^22
+
 struct Tally {
     float m, s, reference;
 };
@@ -45,7 +56,7 @@ __device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Tal
         const Mass before = mass_of(a, scale);
         const float reference = m * scale;
         a.m = m;
-        a.reference = fabsf(reference) <= 4194304.0f ? reference : NAN;
+        a.reference = fabsf(reference) <= kNear ? reference : NAN;
         a.s = before.s * power(before.m, m, scale) * __builtin_amdgcn_exp2f(excess(a, scale));
     }
     if (a.reference == a.reference) {
@@ -56,6 +67,31 @@ __device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Tal
         for (int k = 0; k < N; ++k) a.s += power(v[k], a.m, scale);
     }
     return m;
+}
+
+// A round of whole pieces without a look for their largest logits: the reference is one of the row's logits, so the sum is 1 at least, what it is short of the
+// largest one does not matter to 32 bits, and a sum past kHigh (or a NaN), which asks for a larger reference, is seen in the end.  masked(v, u) may take logits
+// out of piece u.
+constexpr float kHigh = 7.9e28f;        // 2^96
+
+template <class T, int NT, class F>
+__device__ __forceinline__ bool add_whole_round(const Round<T, NT> &of, float scale, Tally &a, F masked)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    float t[kRound];
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) {
+        float v[N];
+        unpack(of.r[u], v);
+        masked(v, u);
+        t[u] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[u] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[k], scale, -a.reference));
+    }
+    const float s = a.s + ((t[0] + t[1]) + (t[2] + t[3]));
+    if (!(s < kHigh)) return false;
+    a.s = s;
+    return true;
 }
 
 // over a wave: everyone's sum brought to the largest logit first.  All lanes get the first one's bits: the product and the first sum become one fused
@@ -142,15 +178,6 @@ __device__ __forceinline__ double exp_of(double x)
     t = __builtin_fma(t * r, r, r) + 1.0;
     return x < -745.0 ? 0.0 : __builtin_ldexp(t, (int)n);
 }
-
-// Four pieces a thread are in flight while four are worked on: a round
-constexpr int kRound = 4;
-
-template <class T, int NT>
-struct Round {
-    static constexpr int N = 16 / (int)sizeof(T);
-    Raw<T, N> r[kRound];
-};
 
 // The pieces first + tid + u * NT, u < kRound, of a row of n logits, where they lie before `end`.  A round all of whose pieces are whole ones needs no look at
 // any of them, and a scalar address.
