@@ -257,7 +257,7 @@ __device__ __forceinline__ void write_round(const Round<T, NT> &r, T *to, uint32
 }
 
 // A row, or part blockIdx.x % a.parts of it (few rows are cut; distill_join_kernel does the rest).  STEP: and its gradients.
-template <class T, int NT, int E, bool STEP>
+template <class T, int NT, int E, bool STREAM, bool STEP>
 __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
     const T *z = (const T *)a.logits + row * a.row_stride;
     const float scale = a.t.scale;
     Round<T, NT> next;
-    read_round<false>(next, z, begin, end, V);
+    read_round<STREAM>(next, z, begin, end, V);
     if (tid == 0) twice = 0;
     List<E> list;
     if (wave == 0 && a.parts == 1) {
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         for (uint32_t first = base; first < stop; first += kRound * NT) {
             const Round<T, NT> now = next;
             // behind the last round, what the next slice begins with
-            read_round<false>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
+            read_round<STREAM>(next, z, first + kRound * NT < stop ? first + kRound * NT : stop, end, V);
             const auto unmarked = [&](float (&v)[N], uint32_t p) {
                 const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p - base] : ((const uint8_t *)marks)[(p - base) / 2] >> ((p - base) % 2 * 4) & 15;
                 if (bits)
@@ -333,17 +333,16 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
     }
     if constexpr (STEP) {
         T *to = (T *)a.glogits + row * a.V;
+        // the row once more, from its end, where it has been read last; rows without a teacher get zeros without a look at them
+        const uint32_t rounds = (pieces + kRound * NT - 1) / (kRound * NT), n = some ? V : 0;
+        Round<T, NT> r;
+        read_round<true>(r, z, (rounds - 1) * (kRound * NT), pieces, n);
         __syncthreads();
         const RowFactor rest = row_factor(of_row[0], of_row[1], scale);
-        const uint32_t n = rest.factor == 0.0f ? 0 : V;          // zeros are written without a look at the logits
-        // from the row's end, where it has been read last
-        const uint32_t rounds = (pieces + kRound * NT - 1) / (kRound * NT);
-        Round<T, NT> r;
-        read_round<true>(r, z, (rounds - 1) * kRound * NT, pieces, n);
         for (uint32_t i = rounds; i-- > 0;) {
             const Round<T, NT> now = r;
-            if (i) read_round<true>(r, z, (i - 1) * kRound * NT, pieces, n);
-            write_round(now, to, i * kRound * NT, V, rest, scale);
+            if (i) read_round<true>(r, z, (i - 1) * (kRound * NT), pieces, n);
+            write_round(now, to, i * (kRound * NT), V, rest, scale);
         }
         __syncthreads();        // the listed tokens' gradients go on top
         if (wave == 0)
@@ -370,27 +369,39 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillCall a)
 }
 
 // The gradient's row from what the forward pass has left: elements are independent, a read and a write of the logits.
-template <class T, int NT>
+template <class T, int NT, int E>
 __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
 {
     constexpr int N = 16 / sizeof(T);
     const int64_t row = blockIdx.x / a.chunks;
-    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, first = blockIdx.x % a.chunks * (kRound * NT), tid = threadIdx.x;
+    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, first = blockIdx.x % a.chunks * (kRound * NT);
     const T *z = (const T *)a.logits + row * a.row_stride;
     T *to = (T *)a.glogits + row * a.V;
     Round<T, NT> r;
     read_round<false>(r, z, first, pieces, V);
     const float *s = a.stats + row * (a.K + 2);
     const float g = a.g_loss[row];
-    write_round(r, to, first, V, row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale), a.t.scale);
-    __syncthreads();            // the listed tokens' gradients go on top
+    // the listed tokens that lie here, by every wave for itself: most workgroups have none, and nothing to wait for
     const int64_t from = (int64_t)first * N, until = from + kRound * NT * N < a.V ? from + kRound * NT * N : a.V;
-    for (int k = tid; k < a.K; k += NT) {
-        const int64_t id = a.ids[row * a.K + k];
-        if (id < from || id >= until) continue;
-        const float d = s[2 + k];
-        put(to + id, d == 0.0f ? 0.0f : d * g);
+    int64_t id[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) id[e] = (int)(e * 64 + (threadIdx.x & 63)) < a.K ? a.ids[row * a.K + e * 64 + (threadIdx.x & 63)] : -1;
+    write_round(r, to, first, V, row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale), a.t.scale);
+    bool here = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (id[e] < from || id[e] >= until) id[e] = -1;
+        here = here || id[e] >= 0;
     }
+    if (!__any(here)) return;
+    __syncthreads();            // their gradients go on top
+    if (threadIdx.x < 64)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (id[e] >= 0) {
+                const float d = s[2 + e * 64 + threadIdx.x];
+                put(to + id[e], d == 0.0f ? 0.0f : d * g);
+            }
 }
 
 int parts_of(int64_t R, int64_t V)
@@ -428,12 +439,26 @@ hipError_t launch_backward(const DistillCall &all, hipStream_t st)
         DistillCall a = rows_from(all, first, most, sizeof(T));
         a.chunks = (uint32_t)chunks;
         const unsigned grid = (unsigned)(a.R * chunks);
-        if (threads == 64) distill_back_kernel<T, 64><<<grid, 64, 0, st>>>(a);
-        else distill_back_kernel<T, 256><<<grid, 256, 0, st>>>(a);
+        if (a.K <= 64 && threads == 64) distill_back_kernel<T, 64, 1><<<grid, 64, 0, st>>>(a);
+        else if (a.K <= 64) distill_back_kernel<T, 256, 1><<<grid, 256, 0, st>>>(a);
+        else if (threads == 64) distill_back_kernel<T, 64, kEntries><<<grid, 64, 0, st>>>(a);
+        else distill_back_kernel<T, 256, kEntries><<<grid, 256, 0, st>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <class T, int E, bool STEP>
+void launch_kernel(const DistillCall &a, unsigned grid, unsigned lds, hipStream_t st)
+{
+    const bool stream = !STEP && (double)a.R * (double)a.V * sizeof(T) >= 512e6;
+    const bool wide = (double)a.V * sizeof(T) >= 128e3 && a.parts == 1;
+    if (a.V <= 4096) distill_kernel<T, 64, E, false, STEP><<<grid, 64, lds, st>>>(a);
+    else if (wide && stream) distill_kernel<T, 512, E, !STEP, STEP><<<grid, 512, lds, st>>>(a);
+    else if (wide) distill_kernel<T, 512, E, false, STEP><<<grid, 512, lds, st>>>(a);
+    else if (stream) distill_kernel<T, 256, E, !STEP, STEP><<<grid, 256, lds, st>>>(a);
+    else distill_kernel<T, 256, E, false, STEP><<<grid, 256, lds, st>>>(a);
 }
 
 template <class T, bool STEP>
@@ -445,10 +470,8 @@ hipError_t launch_rows(const DistillCall &all, hipStream_t st)
     for (int64_t first = 0; first < all.R; first += kRows) {
         const DistillCall a = rows_from(all, first, kRows, sizeof(T));
         const unsigned grid = (unsigned)(a.R * a.parts);
-        if (a.K <= 64 && a.V <= 4096) distill_kernel<T, 64, 1, STEP><<<grid, 64, lds, st>>>(a);
-        else if (a.K <= 64) distill_kernel<T, 256, 1, STEP><<<grid, 256, lds, st>>>(a);
-        else if (a.V <= 4096) distill_kernel<T, 64, kEntries, STEP><<<grid, 64, lds, st>>>(a);
-        else distill_kernel<T, 256, kEntries, STEP><<<grid, 256, lds, st>>>(a);
+        if (a.K <= 64) launch_kernel<T, 1, STEP>(a, grid, lds, st);
+        else launch_kernel<T, kEntries, STEP>(a, grid, lds, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
