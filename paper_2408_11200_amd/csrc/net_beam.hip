@@ -295,12 +295,14 @@ __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
     if (a.out_ended) a.out_ended[at] = best && (parent.state == kEnded || token == a.end_id);
 }
 
-// How rows are cut: few rows are shared among workgroups, four a CU
-int parts_of(int64_t rows, int64_t V)
+// How rows are cut: few rows are shared among workgroups, two a CU, of a round of pieces (16 KB) at least.  Both launches, us, whole rows, two workgroups
+// a CU and four: 1 x 4 x 16384 bf16 11.1, 9.6, 9.5; 32 x 4 x 16384 12.3, 10.8, 10.8; 24 x 4 x 50001 fp32 with twelve -, 15.0, 18.4; 16 x 8 x 131072 bf16 with sixteen -, 19.3, 21.3; half
+// a round: 1 x 4 x 32768 bf16 10.3 for 9.7, 1 x 8 x 131072 16.5 for 14.7.
+int parts_of(int64_t rows, int64_t V, size_t size)
 {
-    if (rows <= 0 || rows > 512 || V < 32768) return 1;
-    int64_t parts = 1024 / rows;
-    if (parts > V / 4096) parts = V / 4096;
+    const int64_t rounds = V / (int64_t)(16384 / size);
+    if (rows <= 0 || rows > 256 || rounds < 2) return 1;
+    const int64_t parts = 512 / rows < rounds ? 512 / rows : rounds;
     return (int)(parts > 64 ? 64 : parts);
 }
 
@@ -332,7 +334,8 @@ int check(int64_t N, int32_t B, int64_t V, int32_t top)
     return top > B * V ? KAN_ERR_INVALID_ARG : KAN_OK;
 }
 
-size_t sums_bytes(int64_t N, int32_t B, int64_t V) { return align_up((size_t)(N * B) * parts_of(N * B, V) * sizeof(Mass)); }
+// for the type whose rows are cut into more parts
+size_t sums_bytes(int64_t N, int32_t B, int64_t V) { return align_up((size_t)(N * B) * parts_of(N * B, V, 4) * sizeof(Mass)); }
 
 }  // namespace
 }  // namespace kannet
@@ -342,7 +345,7 @@ using namespace kannet;
 extern "C" size_t kan_beam_select_workspace_bytes(int64_t N, int32_t B, int64_t V, int32_t top)
 {
     if (check(N, B, V, top) != KAN_OK || N == 0) return 0;
-    return sums_bytes(N, B, V) + align_up((size_t)(N * B) * parts_of(N * B, V) * top * sizeof(uint64_t));
+    return sums_bytes(N, B, V) + align_up((size_t)(N * B) * parts_of(N * B, V, 4) * top * sizeof(uint64_t));
 }
 
 extern "C" int kan_beam_select(int64_t N, int32_t B, int64_t V, const void *logits, int32_t type, int64_t row_stride, const float *scores,
@@ -375,7 +378,7 @@ extern "C" int kan_beam_select(int64_t N, int32_t B, int64_t V, const void *logi
     a.tokens = tokens;
     a.parents = parents;
     a.out_ended = out_ended;
-    a.parts = parts_of(N * B, V);
+    a.parts = parts_of(N * B, V, size_of(type));
     a.sums = (Mass *)ws;
     a.keys = (uint64_t *)((char *)ws + sums_bytes(N, B, V));
     return status_of(type == KAN_F32 ? launch<float>(a, N, (hipStream_t)stream) : launch<bf16>(a, N, (hipStream_t)stream));

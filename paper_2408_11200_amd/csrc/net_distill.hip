@@ -454,7 +454,7 @@ void launch_kernel(const DistillCall &a, unsigned grid, unsigned lds, hipStream_
 {
     const bool stream = !STEP && (double)a.R * (double)a.V * sizeof(T) >= 512e6;
     const bool wide = (double)a.V * sizeof(T) >= 128e3 && a.parts == 1;
-    if (a.V <= 4096) distill_kernel<T, 64, E, false, STEP><<<grid, 64, lds, st>>>(a);
+    if (a.V <= 8192) distill_kernel<T, 64, E, false, STEP><<<grid, 64, lds, st>>>(a);
     else if (wide && stream) distill_kernel<T, 512, E, !STEP, STEP><<<grid, 512, lds, st>>>(a);
     else if (wide) distill_kernel<T, 512, E, false, STEP><<<grid, 512, lds, st>>>(a);
     else if (stream) distill_kernel<T, 256, E, !STEP, STEP><<<grid, 256, lds, st>>>(a);

@@ -121,18 +121,18 @@ __device__ __forceinline__ Mass join_mass(Mass a, float scale, Mass *lds)
     return a;
 }
 
-// the sum over a wave, the same bits in all lanes
+// the sum over a wave, the same bits in all lanes (sums of two lanes each, whichever of them asks).  Between registers: through LDS six exchanges of two
+// halves are a microsecond.
 __device__ __forceinline__ double wave_sum(double v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
-__device__ __forceinline__ double wave_max(double v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d, 64));
+    const int lane = threadIdx.x & 63;
+    const auto with = [&](uint64_t partner) { v += __builtin_bit_cast(double, partner); };
+    with(of_partner<1>(__builtin_bit_cast(uint64_t, v), lane));
+    with(of_partner<2>(__builtin_bit_cast(uint64_t, v), lane));
+    with(of_partner<7>(__builtin_bit_cast(uint64_t, v), lane));
+    with(of_partner<15>(__builtin_bit_cast(uint64_t, v), lane));
+    with(of_partner<16>(__builtin_bit_cast(uint64_t, v), lane));
+    with(of_partner<32>(__builtin_bit_cast(uint64_t, v), lane));
     return v;
 }
 

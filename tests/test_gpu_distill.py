@@ -1,7 +1,7 @@
 """The divergence from a teacher's likely tokens and its gradient against the plain form in 64 bits.
 
 Tolerances, from the arithmetic: u = 2^-24 is the rounding of a 32-bit operation.  Only the sum over the tokens off the list is held in 32 bits.  Its relative
-error is `delta`: a thread adds one term in 64 (rows of up to 4096 tokens) or 256, at most u of the sum each; 16 more levels join threads, waves and
+error is `delta`: a thread adds one term in 64 (rows of up to 8192 tokens) or 256, at most u of the sum each; 16 more levels join threads, waves and
 parts, with a rescaling of 8 u each time the largest logit rises (at most 12 of weight) or sums are joined; an exponent y of base 2 is three roundings, 2.1 u |y| of its term, weighted by
 the term itself (|y| <= 20 where terms have weight), and the exponential 2 u: delta = (V / threads + 16 + 12 * 8 + 44) u.
 What follows from it: the loss has d loss / d log sum = q_r P - p_r, and half a second derivative of at most q_r P; a listed token's gradient q P q_r; the
@@ -39,7 +39,7 @@ def agree(got, ref, tol, name):
 
 
 def delta_of(V):
-    return (V / (64 if V <= 4096 else 256) + 16 + 12 * 8 + 44) * U
+    return (V / (64 if V <= 8192 else 256) + 16 + 12 * 8 + 44) * U
 
 
 def check(f, T, V, loss=None, glogits=None, g=None):
