@@ -3,9 +3,10 @@
 The next token from the `context` tokens before it: their rows of an embedding table side by side are the residual stream, every block is a
 norm, a KAN layer as wide as the stream, and a second norm with a gate and the residual scale (fused over the boundary between two blocks);
 a last KAN layer gives the logits.  The norms keep what the layers read on their grids.  A step is the log probabilities' loss with its
-gradient, the gradients clipped to a norm, and Adam; every operator of it but Adam runs in the HIP library.
+gradient, the gradients clipped to a norm, and Adam; every operator of it but Adam runs in the HIP library.  A trained network teaches a
+smaller one by its most likely tokens, and answers with more than one token by a beam search.
 
-    python -m paper_2408_11200_amd.tokens --steps 300
+    python -m paper_2408_11200_amd.tokens --steps 300 --student 8 --answer 4
 """
 import argparse
 import math
@@ -13,7 +14,7 @@ import math
 import numpy as np
 import torch
 
-from . import autograd, workloads
+from . import autograd, net, workloads
 
 GRID = 3.0          # the layers' grids are [-3, 3]: three deviations of a normed channel
 
@@ -61,6 +62,33 @@ class TokenNet:
         _, _, tokens, logp = autograd.token_logprob(z, torch.full((z.shape[0],), -1, device=z.device), temperature, top)
         return tokens, logp
 
+    def distill_loss(self, ids, teacher_ids, values, temperature=1.0, teacher="logp"):
+        """Mean divergence from what a teacher says of the rows (as autograd.token_distill takes it), rows without a teacher left out."""
+        loss = autograd.token_distill(self.logits(ids), teacher_ids, values, temperature, teacher)
+        return loss.sum() / ((teacher_ids >= 0) & (teacher_ids < self.vocab)).any(-1).sum().clamp(min=1)
+
+    @torch.no_grad()
+    def search(self, ids, length, beams=4, end_id=-1, length_power=0.0, temperature=1.0):
+        """(tokens [N][beams][length], scores [N][beams]): the most likely answers to ids[N][context], best first, by a beam search.  An answer that has
+        end_id ends there (end_id to its end); scores are log probabilities, compared divided by length^length_power; -1: no such answer."""
+        N = ids.shape[0]
+        window = ids.repeat_interleave(beams, 0)
+        answers = torch.full((N * beams, length), -1, dtype=torch.int64, device=ids.device)
+        lengths = torch.zeros((N * beams,), device=ids.device)
+        scores = torch.full((N, beams), -math.inf, device=ids.device)
+        scores[:, 0] = 0.0
+        ended = torch.zeros((N, beams), dtype=torch.bool, device=ids.device) if end_id >= 0 else None
+        for at in range(length):
+            grown = lengths.view(N, beams) + (1.0 if ended is None else (~ended).float())
+            scores, tokens, parents, now = autograd.beam_select(self.logits(window), scores, beams, ended, end_id,
+                                                                grown.clamp(min=1.0) ** -length_power if length_power else None, temperature)
+            lengths = grown.view(-1)
+            autograd.beam_reorder(parents, [window, answers, lengths], beams)
+            answers[:, at] = tokens.view(-1)
+            window = torch.cat([window[:, 1:], tokens.view(-1, 1)], 1)
+            ended = None if ended is None else now
+        return answers.view(N, beams, length), scores
+
 
 def train(net, ids, target, steps, batch=4096, lr=3e-3, max_norm=1.0, seed=0, log_every=0):
     """Adam on clipped gradients over random batches; the loss and the gradients' norm before clipping, for each step."""
@@ -80,20 +108,53 @@ def train(net, ids, target, steps, batch=4096, lr=3e-3, max_norm=1.0, seed=0, lo
     return [float(v) for v in losses], [float(v) for v in norms]
 
 
+def train_from_teacher(student, teacher, ids, steps, top=8, batch=4096, lr=3e-3, max_norm=1.0, temperature=1.0, seed=0, log_every=0):
+    """The student learns the teacher's `top` most likely tokens over random batches: the logits' gradients come with the loss, in one pass over the logits.  Returns the
+    losses and the gradients' norms before clipping."""
+    opt = torch.optim.Adam(student.tensors(), lr=lr)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    weights = torch.full((batch,), 1.0 / batch, device="cuda")
+    losses, norms = [], []
+    for step in range(steps):
+        rows = ids[torch.randint(0, ids.shape[0], (batch,), generator=gen, device="cuda")]
+        likely, logp = teacher.likely(rows, top, temperature)
+        opt.zero_grad(set_to_none=True)
+        z = student.logits(rows)
+        loss, gz = net.kan_token_distill_step(z.detach(), likely, logp, weights, temperature)
+        z.backward(gz)
+        norms.append(autograd.clip_gradients([t.grad for t in student.tensors()], max_norm))
+        opt.step()
+        losses.append(loss.mean())
+        if log_every and step % log_every == 0:
+            print("step %5d  divergence %.4f  gradient norm %.3f" % (step, losses[-1], norms[-1]), flush=True)
+    return [float(v) for v in losses], [float(v) for v in norms]
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--vocab", type=int, default=64)
     ap.add_argument("--steps", type=int, default=300)
     ap.add_argument("--batch", type=int, default=4096)
+    ap.add_argument("--student", type=int, default=0, help="channels a token of a smaller network that learns from the first one")
+    ap.add_argument("--answer", type=int, default=0, help="tokens of answers by beam search")
+    ap.add_argument("--beams", type=int, default=4)
     args = ap.parse_args()
     ids, target, floor = workloads.token_task(args.vocab)
     ids, target = torch.from_numpy(ids).cuda(), torch.from_numpy(target).cuda()
-    net = TokenNet(args.vocab)
-    losses, _ = train(net, ids, target, args.steps, args.batch, log_every=max(args.steps // 20, 1))
-    tokens, logp = net.likely(ids[:4])
+    model = TokenNet(args.vocab)
+    losses, _ = train(model, ids, target, args.steps, args.batch, log_every=max(args.steps // 20, 1))
+    tokens, logp = model.likely(ids[:4])
     for row in range(4):
         print("after %s: %s" % (ids[row].tolist(), "  ".join("%d (%.2f)" % (t, p) for t, p in zip(tokens[row].tolist(), logp[row].exp().tolist()))))
     print("loss %.4f -> %.4f after %d steps; %.4f is the least" % (losses[0], losses[-1], args.steps, floor))
+    if args.student:
+        student = TokenNet(args.vocab, embed=args.student, blocks=1, seed=1)
+        divergence, _ = train_from_teacher(student, model, ids, args.steps, min(8, args.vocab), args.batch, log_every=max(args.steps // 20, 1))
+        print("divergence %.4f -> %.4f; the student's loss %.4f" % (divergence[0], divergence[-1], float(student.loss(ids[:65536], target[:65536]).detach())))
+    if args.answer:
+        answers, scores = model.search(ids[:4], args.answer, args.beams)
+        for row in range(4):
+            print("after %s: %s" % (ids[row].tolist(), "  ".join("%s (%.2f)" % (a, s) for a, s in zip(answers[row].tolist(), scores[row].tolist()))))
 
 
 if __name__ == "__main__":
