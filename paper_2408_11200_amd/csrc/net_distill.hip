@@ -369,7 +369,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillCall a)
 }
 
 // The gradient's row from what the forward pass has left: elements are independent, a read and a write of the logits.
-template <class T, int NT, int E>
+template <class T, int NT, int E, bool STREAM>
 __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
 {
     constexpr int N = 16 / sizeof(T);
@@ -377,16 +377,17 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
     const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, first = blockIdx.x % a.chunks * (kRound * NT);
     const T *z = (const T *)a.logits + row * a.row_stride;
     T *to = (T *)a.glogits + row * a.V;
-    Round<T, NT> r;
-    read_round<false>(r, z, first, pieces, V);
     const float *s = a.stats + row * (a.K + 2);
     const float g = a.g_loss[row];
+    const RowFactor rest = row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale);
+    Round<T, NT> r;
+    read_round<STREAM>(r, z, first, pieces, rest.factor == 0.0f ? 0 : V);      // rows without a teacher are not read
     // the listed tokens that lie here, by every wave for itself: most workgroups have none, and nothing to wait for
     const int64_t from = (int64_t)first * N, until = from + kRound * NT * N < a.V ? from + kRound * NT * N : a.V;
     int64_t id[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) id[e] = (int)(e * 64 + (threadIdx.x & 63)) < a.K ? a.ids[row * a.K + e * 64 + (threadIdx.x & 63)] : -1;
-    write_round(r, to, first, V, row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale), a.t.scale);
+    write_round(r, to, first, V, rest, a.t.scale);
     bool here = false;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -427,22 +428,33 @@ DistillCall rows_from(DistillCall a, int64_t first, int64_t most, size_t size)
     return a;
 }
 
+// Whether the logits do not stay in the caches from one pass to the next: then they are read past them (8192 x 131072 bf16 backward 708 us, 754 through them; 2000 x 33000,
+// 132 MB, 57 and 52).
+bool passes_by(const DistillCall &a, size_t size) { return (double)a.R * (double)a.V * (double)size >= 512e6; }
+
+template <class T, int E>
+void launch_back(const DistillCall &a, int threads, bool stream, unsigned grid, hipStream_t st)
+{
+    if (threads == 64) distill_back_kernel<T, 64, E, false><<<grid, 64, 0, st>>>(a);
+    else if (stream) distill_back_kernel<T, 256, E, true><<<grid, 256, 0, st>>>(a);
+    else distill_back_kernel<T, 256, E, false><<<grid, 256, 0, st>>>(a);
+}
+
 template <class T>
 hipError_t launch_backward(const DistillCall &all, hipStream_t st)
 {
     constexpr int N = 16 / sizeof(T);
     prof::Timed timed("token_distill_backward", st);
     const int64_t pieces = div_up(all.V, (int64_t)N);
+    const bool stream = passes_by(all, sizeof(T));
     const int threads = pieces <= 64 * kRound ? 64 : 256;
     const int64_t chunks = div_up(pieces, (int64_t)threads * kRound), most = (1ll << 23) / chunks > 1 ? (1ll << 23) / chunks : 1;
     for (int64_t first = 0; first < all.R; first += most) {
         DistillCall a = rows_from(all, first, most, sizeof(T));
         a.chunks = (uint32_t)chunks;
         const unsigned grid = (unsigned)(a.R * chunks);
-        if (a.K <= 64 && threads == 64) distill_back_kernel<T, 64, 1><<<grid, 64, 0, st>>>(a);
-        else if (a.K <= 64) distill_back_kernel<T, 256, 1><<<grid, 256, 0, st>>>(a);
-        else if (threads == 64) distill_back_kernel<T, 64, kEntries><<<grid, 64, 0, st>>>(a);
-        else distill_back_kernel<T, 256, kEntries><<<grid, 256, 0, st>>>(a);
+        if (a.K <= 64) launch_back<T, 1>(a, threads, stream, grid, st);
+        else launch_back<T, kEntries>(a, threads, stream, grid, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -452,7 +464,7 @@ hipError_t launch_backward(const DistillCall &all, hipStream_t st)
 template <class T, int E, bool STEP>
 void launch_kernel(const DistillCall &a, unsigned grid, unsigned lds, hipStream_t st)
 {
-    const bool stream = !STEP && (double)a.R * (double)a.V * sizeof(T) >= 512e6;
+    const bool stream = !STEP && passes_by(a, sizeof(T));
     const bool wide = (double)a.V * sizeof(T) >= 128e3 && a.parts == 1;
     if (a.V <= 8192) distill_kernel<T, 64, E, false, STEP><<<grid, 64, lds, st>>>(a);
     else if (wide && stream) distill_kernel<T, 512, E, !STEP, STEP><<<grid, 512, lds, st>>>(a);
