@@ -405,11 +405,14 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
             }
 }
 
-int parts_of(int64_t R, int64_t V)
+// Few long rows are shared among workgroups, two a CU, and joined by a launch more.  Whole and cut, us, twenty tokens: 1 x 65536 bf16 8.2 and 7.6, 1 x 131072 11.3 and
+// 7.7, 64 x 131072 12.0 and 9.9, 128 x 131072 16.0 and 18.1, 16 x 32768 7.7 and 9.2; fp32: 64 x 50001 9.6 and 10.0, 100 x 131072 18.9 and 16.8, 200 x 131072 20.4 and
+// 22.8, 128 x 262144 32 and 27, 1 x 1000000 82 and 10.
+int parts_of(int64_t R, int64_t V, size_t size)
 {
-    if (R <= 0 || R > 512 || V < 32768) return 1;
-    int64_t parts = 1024 / R;
-    if (parts > V / 4096) parts = V / 4096;
+    const double row = (double)V * (double)size / 262144.0;
+    if (R <= 0 || R > 256 || row < 1.0 || (double)R > 96.0 * row) return 1;
+    const int64_t parts = 512 / R < V / 8192 ? 512 / R : V / 8192;
     return (int)(parts > 64 ? 64 : parts);
 }
 
@@ -516,9 +519,10 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, int32_t K, flo
     return KAN_OK;
 }
 
+// for the type whose rows are the longer ones
 size_t sums_bytes(int64_t R, int64_t V)
 {
-    const int parts = parts_of(R, V);
+    const int parts = parts_of(R, V, 4);
     return parts > 1 ? align_up((size_t)R * parts * sizeof(Mass)) : 0;
 }
 
@@ -549,7 +553,7 @@ int run(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stri
     a.t = temperature_of(temperature);
     a.g_loss = g_loss;
     a.loss = loss;
-    a.parts = parts_of(R, V);
+    a.parts = parts_of(R, V, size_of(type));
     a.part_sums = (Mass *)ws;
     a.stats = step && a.parts > 1 ? (float *)((char *)ws + sums_bytes(R, V)) : stats;
     a.glogits = glogits;

@@ -84,7 +84,7 @@ CASES = [
     (33, 157, 5, dict(dtype=BF16, pad=3)), (300, 1000, 8, dict()), (5, 1000, 256, dict(dtype=BF16, teacher="logits")), (17, 4096, 64, dict(dtype=BF16)),
     (17, 4097, 65, dict(pad=1)), (6, 8191, 200, dict(dtype=BF16, list_dtype=BF16)), (520, 8200, 16, dict(teacher="logits", T=3.0, list_dtype=BF16)),
     (1, 32768, 20, dict()), (3, 40001, 64, dict(dtype=BF16, pad=7)), (2, 65537, 256, dict(teacher="logits")), (515, 33000, 20, dict(dtype=BF16, masked=700)),
-    (4, 50001, 1, dict(masked=1000, T=0.5)), (8, 300, 7, dict(near=0.0)), (8, 20000, 64, dict(near=1e-3, short=False)), (8, 2000, 20, dict(spread=8.0)),
+    (4, 50001, 1, dict(masked=1000, T=0.5)), (3, 140001, 20, dict(dtype=BF16, pad=5)), (90, 131072, 64, dict(dtype=BF16, near=0.1)), (2, 300007, 100, dict(teacher="logits", T=0.75)), (8, 300, 7, dict(near=0.0)), (8, 20000, 64, dict(near=1e-3, short=False)), (8, 2000, 20, dict(spread=8.0)),
 ]
 
 
@@ -111,7 +111,7 @@ def test_loss_and_gradient(R, V, K, options):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("V", [24, 5000, 40000])
+@pytest.mark.parametrize("V", [24, 5000, 40000, 140000])
 @pytest.mark.parametrize("teacher", ["logp", "logits"])
 def test_rows_out_of_the_ordinary(dtype, V, teacher):
     """One kind a row; every entry point gives what the plain form says."""
@@ -198,7 +198,7 @@ def test_rows_past_32_bit_offsets():
     assert torch.equal(again, gz[rows])
 
 
-@pytest.mark.parametrize("R,V", [(700, 100003 // 20), (6, 33000)])
+@pytest.mark.parametrize("R,V", [(700, 100003 // 20), (6, 33000), (6, 140000)])
 def test_in_place_and_other_layouts(R, V):
     logits, ids, values, g = case(R, V, 12, 11, dtype=BF16)
     o = net.kan_token_distill_forward(logits, ids, values)
@@ -222,12 +222,12 @@ def test_in_place_and_other_layouts(R, V):
 
 
 def test_captured_steps_replay_to_the_eager_result():
-    logits, ids, values, g = case(40, 40000, 20, 2)
+    logits, ids, values, g = case(40, 140000, 20, 2)
     small, sids, svalues, sg = case(300, 777, 9, 4, dtype=BF16)
     keep = [t.clone() for t in (logits, small)]
     want = [net.kan_token_distill_step(logits, ids, values, g), net.kan_token_distill_step(small, sids, svalues, sg)]
     outs = [tuple(torch.empty_like(t) for t in w) for w in want]
-    ws = torch.empty(net.kan_token_distill_workspace_bytes(40, 40000, 20), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(net.kan_token_distill_workspace_bytes(40, 140000, 20), dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
