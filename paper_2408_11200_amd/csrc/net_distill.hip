@@ -519,6 +519,9 @@ int check(int64_t R, int64_t V, int32_t type, int64_t row_stride, int32_t K, flo
     return KAN_OK;
 }
 
+// whether gradients in place of the logits would lie elsewhere than their logits
+bool shifts(int64_t R, int64_t V, const void *logits, int64_t row_stride, const void *glogits) { return glogits == logits && R > 1 && row_stride != V; }
+
 // for the type whose rows are the longer ones
 size_t sums_bytes(int64_t R, int64_t V)
 {
@@ -538,7 +541,7 @@ int run(int64_t R, int64_t V, const void *logits, int32_t type, int64_t row_stri
     if (!logits || !ids || !teacher || misplaced(logits, type) || misplaced8(ids) || misplaced(teacher, teacher_type) || misplaced(loss, KAN_F32) ||
         misplaced(stats, KAN_F32))
         return KAN_ERR_INVALID_ARG;
-    if (step && (!g_loss || !glogits || misplaced(g_loss, KAN_F32) || misplaced(glogits, type))) return KAN_ERR_INVALID_ARG;
+    if (step && (!g_loss || !glogits || misplaced(g_loss, KAN_F32) || misplaced(glogits, type) || shifts(R, V, logits, row_stride, glogits))) return KAN_ERR_INVALID_ARG;
     if (bad_workspace(ws, ws_bytes, kan_token_distill_workspace_bytes(R, V, K))) return KAN_ERR_WORKSPACE;
     DistillCall a = {};
     a.logits = logits;
@@ -597,7 +600,7 @@ extern "C" int kan_token_distill_backward(int64_t R, int64_t V, const void *logi
     if (rc != KAN_OK) return rc;
     if (R == 0) return KAN_OK;
     if (!logits || !teacher_ids || !stats || !g_loss || !glogits || misplaced(logits, type) || misplaced(glogits, type) || misplaced8(teacher_ids) ||
-        misplaced(stats, KAN_F32) || misplaced(g_loss, KAN_F32))
+        misplaced(stats, KAN_F32) || misplaced(g_loss, KAN_F32) || shifts(R, V, logits, row_stride, glogits))
         return KAN_ERR_INVALID_ARG;
     DistillCall a = {};
     a.logits = logits;

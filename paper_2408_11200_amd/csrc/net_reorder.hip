@@ -155,7 +155,15 @@ int piece_of(int top) { return top <= 16 ? 16 : top <= 32 ? 8 : 4; }
 
 int64_t pieces_of(const kan_state_ref &t, int piece) { return t.bytes / piece + (t.bytes % piece ? 1 : 0); }
 
-int check(int64_t N, int32_t B, int32_t top, int32_t n, const kan_state_ref *list)
+// from an output's first byte to its last one
+__int128 span(const int64_t (&count)[3], const int64_t (&stride)[3], int64_t bytes)
+{
+    __int128 n = bytes;
+    for (int d = 0; d < 3; ++d) n += count[d] > 1 ? (__int128)stride[d] * (count[d] - 1) : 0;
+    return n;
+}
+
+int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list)
 {
     if (N < 0 || B < 1 || top < 1 || n < 0 || (n > 0 && !list)) return KAN_ERR_INVALID_ARG;
     if (B > KAN_BEAM_MAX || top > KAN_BEAM_MAX || N >= (1ll << 31) / KAN_BEAM_MAX) return KAN_ERR_UNSUPPORTED;
@@ -171,6 +179,9 @@ int check(int64_t N, int32_t B, int32_t top, int32_t n, const kan_state_ref *lis
         seen[place / 64] |= bit;
         const int64_t rows[3] = {t.outer, N * top, t.inner};
         if (!apart(rows, t.out_stride, t.bytes)) return KAN_ERR_INVALID_ARG;
+        // the parents are read while rows are written
+        const __int128 from = (uintptr_t)t.out, order = (uintptr_t)parents;
+        if (parents && order < from + span(rows, t.out_stride, t.bytes) && from < order + (__int128)N * top * 8) return KAN_ERR_INVALID_ARG;
         if (t.data == t.out) {
             if (top != B) return KAN_ERR_INVALID_ARG;
             for (int d = 0; d < 3; ++d)
@@ -199,7 +210,7 @@ using namespace kannet;
 
 extern "C" int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list, void *stream)
 {
-    const int rc = check(N, B, top, n, list);
+    const int rc = check(N, B, top, parents, n, list);
     if (rc != KAN_OK) return rc;
     if (N == 0 || n == 0) return KAN_OK;
     if (!parents || misplaced8(parents)) return KAN_ERR_INVALID_ARG;

@@ -423,16 +423,15 @@ def _evenly(dims):
     return count, stride, to
 
 
-def _state(r, t, o, dim, size):
-    """Fills a KanStateRef: rows in dimension `dim`, a contiguous end of a row as one run, what is before and between as one dimension each."""
-    dims = [(n, a * size, b * size) for n, a, b in zip(t.shape, t.stride(), o.stride())]
+def _state(shape, strides, out_strides, size, dim):
+    """A KanStateRef's numbers behind its two addresses: rows in dimension `dim`, a contiguous end of a row as one run, what is before and between as one dimension each."""
+    dims = [(n, a * size, b * size) for n, a, b in zip(shape, strides, out_strides)]
     before, behind, run = [d for d in dims[:dim] if d[0] != 1], [d for d in dims[dim + 1:] if d[0] != 1], size
     while behind and behind[-1][1] == run == behind[-1][2]:
         run *= behind.pop()[0]
-    r.data, r.out, r.bytes = t.data_ptr(), o.data_ptr(), run
-    r.outer, r.stride[0], r.out_stride[0] = _evenly(before)
-    r.inner, r.stride[2], r.out_stride[2] = _evenly(behind)
-    r.stride[1], r.out_stride[1] = dims[dim][1], dims[dim][2]
+    outer, s0, o0 = _evenly(before)
+    inner, s2, o2 = _evenly(behind)
+    return outer, inner, run, s0, dims[dim][1], s2, o0, dims[dim][2], o2
 
 
 def kan_beam_reorder(parents, tensors, beams, out=None, dim=0, stream=None):
@@ -441,13 +440,19 @@ def kan_beam_reorder(parents, tensors, beams, out=None, dim=0, stream=None):
     N, top = parents.shape
     out = tensors if out is None else out
     assert len(out) == len(tensors), "an output for each tensor"
-    refs, n = (KanStateRef * max(len(tensors), 1))(), 0
+    device, numbers, layouts = parents.device, [], {}       # tensors that lie alike are looked at once
     for t, o in zip(tensors, out):
-        d = dim + t.dim() if dim < 0 else dim
-        assert t.is_cuda and o.device == t.device == parents.device and o.dtype == t.dtype and o.dim() == t.dim() > d >= 0, "states on the device of the parents"
-        assert t.shape[d] == N * beams and o.shape[d] == N * top and t.shape[:d] == o.shape[:d] and t.shape[d + 1:] == o.shape[d + 1:], "a row of a state for each beam"
-        if o.numel():
-            _state(refs[n], t, o, d, t.element_size())
-            n += 1
-    _done(load().kan_beam_reorder(N, beams, top, _of(parents, torch.int64), n, refs, _stream(stream)), "kan_beam_reorder")
+        assert t.device == device and (o is t or o.device == device), "states on the device of the parents"
+        key = (t.shape, t.dtype, t.stride()) + (() if o is t else (o.shape, o.dtype, o.stride()))
+        layout = layouts.get(key)
+        if layout is None:
+            shape, other, d = t.shape, o.shape, dim + t.dim() if dim < 0 else dim
+            assert len(shape) == len(other) > d >= 0 and shape[d] == N * beams and other[d] == N * top and o.dtype == t.dtype, "a row of a state for each beam, and an output of its type"
+            assert shape[:d] == other[:d] and shape[d + 1:] == other[d + 1:], "an output of a state's shape"
+            layout = layouts[key] = _state(shape, t.stride(), o.stride(), t.element_size(), d) if t.numel() and o.numel() else ()
+        if layout:
+            numbers += (t.data_ptr(), o.data_ptr()) + layout
+    refs = (ctypes.c_int64 * max(len(numbers), 1))(*numbers)
+    _done(load().kan_beam_reorder(N, beams, top, _of(parents, torch.int64), len(numbers) // 11, ctypes.cast(refs, ctypes.POINTER(KanStateRef)), _stream(stream)),
+          "kan_beam_reorder")
     return out

@@ -38,6 +38,8 @@ def test_distill_refusals(lib):
     assert INVALID == forward(stride=8) == forward(values=None) == forward(values=A + 2) == forward(values=A + 1, vt=1) == forward(loss=A + 1) == forward(stats=A + 2)
     assert UNSUPPORTED == forward(vt=2) == forward(vt=-1) == forward(form=2) == forward(form=-1)
     assert INVALID == step(g=None) == step(gz=None) == step(g=A + 2) == step(gz=A + 2) == step(loss=A + 1)
+    # gradients in place of a slice of wider rows
+    assert INVALID == lib.kan_token_distill_backward(2, 9, A, 0, 10, 3, A, 1.0, A, A, A, None) == lib.kan_token_distill_step(2, 9, A, 0, 10, 3, A, A, 0, 0, 1.0, A, A, A, None, 0, None)
     assert INVALID == backward(stats=None) == backward(g=None) == backward(gz=None) == backward(stats=A + 1) == backward(gz=A + 2)
     need = lib.kan_token_distill_workspace_bytes(16, 65536, 20)
     assert need > 0 and need % 256 == 0
@@ -61,7 +63,7 @@ def test_select_refusals(lib):
     assert 0 == lib.kan_beam_select_workspace_bytes(2, 0, 9, 1) == lib.kan_beam_select_workspace_bytes(-1, 3, 9, 1) == lib.kan_beam_select_workspace_bytes(2, 65, 9, 1)
 
 
-def state(data=A, out=A, outer=1, inner=1, size=24, stride=(0, 24, 0), out_stride=None):
+def state(data=1 << 16, out=1 << 16, outer=1, inner=1, size=24, stride=(0, 24, 0), out_stride=None):
     three = ctypes.c_int64 * 3
     return net.KanStateRef(data, out, outer, inner, size, three(*stride), three(*(out_stride or stride)))
 
@@ -79,7 +81,9 @@ def test_reorder_refusals(lib):
     assert INVALID == run(state(data=1 << 20, stride=(0, 23, 0))) == run(state(data=1 << 20, inner=4, size=8, stride=(0, 24, 8))) == run(state(data=1 << 20, outer=2, stride=(100, 24, 0)))
     assert INVALID == run(state(data=1 << 20, stride=(0, 0, 0))) == run(state(data=1 << 20, stride=(0, -24, 0))) == run(state(data=1 << 20, outer=2, stride=(0, 24, 0)))
     # in place: as many rows as there were, where they were; and no tensor twice
-    assert INVALID == run(state(), top=2) == run(state(stride=(0, 24, 0), out_stride=(0, 32, 0))) == run(s, s) == run(state(), state(data=1 << 20, out=A + 240), state())
+    assert INVALID == run(state(), top=2) == run(state(stride=(0, 24, 0), out_stride=(0, 32, 0))) == run(s, s) == run(state(), state(data=1 << 20, out=(1 << 16) + 240), state())
+    # the parents among what is written
+    assert INVALID == run(state(data=1 << 20, out=A)) == run(state(data=1 << 20, out=A - 120)) == run(s, state(data=2 << 20, out=A + 40))
     # more pieces than a number of 32 bits counts
     assert UNSUPPORTED == run(state(data=1 << 20, size=1 << 36, stride=(0, 1 << 36, 0))) == run(state(data=1 << 20, outer=1 << 20, inner=1 << 12, size=1, stride=(1 << 20, 4096, 1)))
 
@@ -102,18 +106,17 @@ def test_front_ends_refuse_host_tensors_and_wrong_shapes():
 
 def test_states_lie_evenly_or_are_refused():
     """What a binding makes of a tensor's strides (addresses only: nothing is launched)."""
-    r = net.KanStateRef()
+    of = lambda t, o, dim: net._state(t.shape, t.stride(), o.stride(), t.element_size(), dim)
     t = torch.zeros((2, 6, 5, 8, 3))
-    net._state(r, t[:, :, :, :4], t[:, :, :, :4], 1, 4)
-    assert (r.outer, r.inner, r.bytes, list(r.stride)) == (2, 5, 48, [6 * 480, 480, 96])
-    net._state(r, t, t, 0, 4)
-    assert (r.outer, r.inner, r.bytes, r.stride[1]) == (1, 1, 6 * 5 * 8 * 3 * 4, 6 * 480)
-    net._state(r, t, t, 4, 4)
-    assert (r.outer, r.inner, r.bytes, list(r.stride)) == (480, 1, 4, [12, 4, 0])
+    cut = t[:, :, :, :4]
+    assert of(cut, cut, 1) == (2, 5, 48, 6 * 480, 480, 96, 6 * 480, 480, 96)
+    assert of(t, t, 0) == (1, 1, 6 * 5 * 8 * 3 * 4, 0, 6 * 480, 0, 0, 6 * 480, 0) and of(t, t, 4) == (480, 1, 4, 12, 4, 0, 12, 4, 0)
+    wide = torch.zeros((2, 6, 5, 16, 3))[:, :, :, 3:11]
+    assert of(t, wide, 0) == (1, 30, 96, 0, 6 * 480, 96, 0, 6 * 960, 192)
     with pytest.raises(AssertionError):
-        net._state(r, t[:, :, :3, :4], t[:, :, :3, :4], 0, 4)
+        of(t[:, :, :3, :4], t[:, :, :3, :4], 0)
     with pytest.raises(AssertionError):
-        net._state(r, t[:, :4].transpose(0, 1)[:, :, :4], t[:, :4].transpose(0, 1)[:, :, :4], 3, 4)
+        of(t[:, :4].transpose(0, 1)[:, :, :4], t[:, :4].transpose(0, 1)[:, :, :4], 3)
 
 
 # ---- the plain forms themselves, against other ways to the same values ----------------------
