@@ -4,7 +4,8 @@
 // change places with one another, so whoever writes a byte of one of them has to have read that byte of all: a thread has one piece of 16
 // bytes of every row of a search, reads it from the parents' rows, and writes it then.  Pieces of different threads do not overlap, a run's
 // last bytes are read and written as they are, hence no wait between threads, no buffer, and no order of the rows to find.  Rows that
-// stay are left out.  A launch takes up to kMost tensors from its arguments.
+// stay are left out.  A launch takes up to kMost tensors from its arguments.  What is written goes past the caches (24 x 6 rows of 117 x 771 bf16 into other buffers 68 us,
+// 75 through them; of 117 x 768, six rows read, 56 and 82).
 #include "net_device.hpp"
 
 namespace kannet {
@@ -38,8 +39,8 @@ typedef uint32_t u32_a1 __attribute__((aligned(1)));
 typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
 typedef u32x4 u32x4_a1 __attribute__((aligned(1)));
 
-// Rows that move, into[k] <- from[k], k < count <= K; the same for the whole workgroup.  Behind the last one comes the first once more, which is
-// read again, out of the cache, and not written.
+// Rows that move, into[k] <- from[k], k < count <= K; the same for the whole workgroup.  Behind the last one everybody reads the same few bytes, which are
+// not written (loads under a condition cost the registers of five of each).
 template <int K>
 struct Moves {
     int from[K], into[K], count;
@@ -50,31 +51,34 @@ __device__ __forceinline__ Moves<K> moves_of(int source)
 {
     Moves<K> m;
     uint64_t open = __ballot(source >= 0);
-    const int first = __ffsll((unsigned long long)open) - 1;
     m.count = __popcll(open);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        m.into[k] = open ? __ffsll((unsigned long long)open) - 1 : first;
+        m.into[k] = open ? __ffsll((unsigned long long)open) - 1 : 0;
         m.from[k] = __builtin_amdgcn_readlane(source, m.into[k]);
         open &= open - 1;
     }
     return m;
 }
 
-template <int K, class P>
-__device__ __forceinline__ void move(const Moves<K> &m, const char *from, int64_t stride, char *to, int64_t out_stride)
+template <int K, bool STREAM, class P>
+__device__ __forceinline__ void move(const Moves<K> &m, const char *idle, const char *from, int64_t stride, char *to, int64_t out_stride)
 {
     typedef const P *From;
     typedef P *To;
     P v[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = *(From)(from + m.from[k] * stride);
+    for (int k = 0; k < K; ++k) {
+        const From p = (From)(k < m.count ? from + m.from[k] * stride : idle);
+        if constexpr (STREAM) v[k] = __builtin_nontemporal_load(p);
+        else v[k] = *p;
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < m.count) *(To)(to + m.into[k] * out_stride) = v[k];
+        if (k < m.count) __builtin_nontemporal_store(v[k], (To)(to + m.into[k] * out_stride));
 }
 
-template <int K, class P>
+template <int K, bool STREAM, class P>
 __device__ __forceinline__ void move_item(const State &s, const ReorderCall &a, int64_t search, uint32_t item, int source)
 {
     const Moves<K> m = moves_of<K>(source);
@@ -83,27 +87,27 @@ __device__ __forceinline__ void move_item(const State &s, const ReorderCall &a, 
     const char *from = s.data + search * a.B * s.stride[1] + block * s.stride[0] + in * s.stride[2] + (int64_t)piece * (int)sizeof(P);
     char *to = s.out + search * a.top * s.out_stride[1] + block * s.out_stride[0] + in * s.out_stride[2] + (int64_t)piece * (int)sizeof(P);
     if (piece < s.whole) {
-        move<K, P>(m, from, s.stride[1], to, s.out_stride[1]);
+        move<K, STREAM, P>(m, s.data, from, s.stride[1], to, s.out_stride[1]);
         return;
     }
     // a run's last bytes
     if (sizeof(P) > 8 && (s.tail & 8)) {
-        move<K, u32x2_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        move<K, STREAM, u32x2_a1>(m, s.data, from, s.stride[1], to, s.out_stride[1]);
         from += 8, to += 8;
     }
     if (sizeof(P) > 4 && (s.tail & 4)) {
-        move<K, u32_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        move<K, STREAM, u32_a1>(m, s.data, from, s.stride[1], to, s.out_stride[1]);
         from += 4, to += 4;
     }
     if (s.tail & 2) {
-        move<K, u16_a1>(m, from, s.stride[1], to, s.out_stride[1]);
+        move<K, STREAM, u16_a1>(m, s.data, from, s.stride[1], to, s.out_stride[1]);
         from += 2, to += 2;
     }
-    if (s.tail & 1) move<K, uint8_t>(m, from, s.stride[1], to, s.out_stride[1]);
+    if (s.tail & 1) move<K, STREAM, uint8_t>(m, s.data, from, s.stride[1], to, s.out_stride[1]);
 }
 
-// MOST: rows of a search; P: a piece
-template <int MOST, class P>
+// MOST: rows of a search; P: a piece; STREAM: states that the caches do not hold anyway
+template <int MOST, bool STREAM, class P>
 __global__ __launch_bounds__(kThreads) void reorder_kernel(ReorderCall a)
 {
     int lo = 0, hi = a.n - 1;
@@ -124,11 +128,12 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(ReorderCall a)
     const int count = __popcll(__ballot(source >= 0));
     const uint32_t item = here % s.blocks * kThreads + threadIdx.x;
     if (count == 0) return;
-    if (MOST <= 4 || count <= 4) move_item<4, P>(s, a, search, item, source);
-    else if (MOST <= 8 || count <= 8) move_item<8, P>(s, a, search, item, source);
-    else if (MOST <= 16 || count <= 16) move_item<(MOST < 16 ? MOST : 16), P>(s, a, search, item, source);
-    else if (MOST <= 32 || count <= 32) move_item<(MOST < 32 ? MOST : 32), P>(s, a, search, item, source);
-    else move_item<MOST, P>(s, a, search, item, source);
+    if (count == 1) move_item<1, STREAM, P>(s, a, search, item, source);
+    else if (count <= 4) move_item<4, STREAM, P>(s, a, search, item, source);
+    else if (MOST <= 8 || count <= 8) move_item<8, STREAM, P>(s, a, search, item, source);
+    else if (MOST <= 16 || count <= 16) move_item<(MOST < 16 ? MOST : 16), STREAM, P>(s, a, search, item, source);
+    else if (MOST <= 32 || count <= 32) move_item<(MOST < 32 ? MOST : 32), STREAM, P>(s, a, search, item, source);
+    else move_item<MOST, STREAM, P>(s, a, search, item, source);
 }
 
 // whether no two runs overlap
@@ -192,14 +197,20 @@ int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, 
     return KAN_OK;
 }
 
-hipError_t launch(const ReorderCall &a, hipStream_t st)
+template <bool STREAM>
+void launch_kernel(const ReorderCall &a, unsigned grid, hipStream_t st)
+{
+    if (a.top <= 8) reorder_kernel<8, STREAM, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
+    else if (a.top <= 16) reorder_kernel<16, STREAM, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
+    else if (a.top <= 32) reorder_kernel<32, STREAM, u32x2_a1><<<grid, kThreads, 0, st>>>(a);
+    else reorder_kernel<64, STREAM, u32_a1><<<grid, kThreads, 0, st>>>(a);
+}
+
+hipError_t launch(const ReorderCall &a, bool past, hipStream_t st)
 {
     prof::Timed timed("beam_reorder", st);
-    const unsigned grid = a.first[a.n];
-    if (a.top <= 8) reorder_kernel<8, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
-    else if (a.top <= 16) reorder_kernel<16, u32x4_a1><<<grid, kThreads, 0, st>>>(a);
-    else if (a.top <= 32) reorder_kernel<32, u32x2_a1><<<grid, kThreads, 0, st>>>(a);
-    else reorder_kernel<64, u32_a1><<<grid, kThreads, 0, st>>>(a);
+    if (past) launch_kernel<true>(a, a.first[a.n], st);
+    else launch_kernel<false>(a, a.first[a.n], st);
     return hipGetLastError();
 }
 
@@ -215,12 +226,16 @@ extern "C" int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t
     if (N == 0 || n == 0) return KAN_OK;
     if (!parents || misplaced8(parents)) return KAN_ERR_INVALID_ARG;
     const int piece = piece_of(top);
+    // 4 x 8 rows of 16 states, 2.1 GB to move: 372 us with streaming loads, 378 without; 24 x 6 rows of 8, 312 MB: 78 and 68
+    double bytes = 0.0;
+    for (int i = 0; i < n; ++i) bytes += (double)list[i].outer * (double)list[i].inner * (double)list[i].bytes * (double)N * B;
+    const bool past = bytes >= 1e9;
     ReorderCall a = {};
     a.parents = parents;
     a.B = B;
     a.top = top;
     const auto flush = [&]() {
-        const hipError_t e = a.n ? launch(a, (hipStream_t)stream) : hipSuccess;
+        const hipError_t e = a.n ? launch(a, past, (hipStream_t)stream) : hipSuccess;
         a.n = 0;
         return e;
     };
