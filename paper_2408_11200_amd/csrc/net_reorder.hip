@@ -5,7 +5,8 @@
 // bytes of every row of a search, reads it from the parents' rows, and writes it then.  Pieces of different threads do not overlap, a run's
 // last bytes are read and written as they are, hence no wait between threads, no buffer, and no order of the rows to find.  Rows that
 // stay are left out.  A launch takes up to kMost tensors from its arguments.  What is written goes past the caches (24 x 6 rows of 117 x 771 bf16 into other buffers 68 us,
-// 75 through them; of 117 x 768, six rows read, 56 and 82).
+// 75 through them; of 117 x 768, six rows read, 56 and 82).  Measured: caches of 4 x 8 rows of 8 heads, 2000 of 2304 x 128 bf16, 16 of them, 2.1 GB to move, 355 us (5.9 TB/s); the
+// 24 x 6 x 117 x 771 above, 312 MB, 56 on the same states again and 66 on others (4.7 TB/s: rows that start anywhere in a line).
 #include "net_device.hpp"
 
 namespace kannet {
