@@ -205,8 +205,8 @@ typedef struct kan_state_ref {
 } kan_state_ref;
 
 /* Row n top + j of every out = row n B + parents[n][j] of its data, j < top <= KAN_BEAM_MAX; a parent outside 0 .. B-1 leaves row j as it was.  out may be data, with the
-   same strides, where top is B (in place: rows that are their own parents are not touched); other overlaps are not allowed, nor is an out that is in the list twice
-   or around the parents.  A tensor's rows of a search have less than 2^31 runs and
+   same strides, where top is B (in place: rows that are their own parents are not touched); other overlaps are not allowed, nor is an out that is in the list twice,
+   another entry's data, or around the parents.  A tensor's rows of a search have less than 2^31 runs and
    pieces of 16 bytes. */
 int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list, void *stream);
 

@@ -174,14 +174,16 @@ int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, 
     if (N < 0 || B < 1 || top < 1 || n < 0 || (n > 0 && !list)) return KAN_ERR_INVALID_ARG;
     if (B > KAN_BEAM_MAX || top > KAN_BEAM_MAX || N >= (1ll << 31) / KAN_BEAM_MAX) return KAN_ERR_UNSUPPORTED;
     uint64_t seen[64] = {};             // places of outputs, one bit each: the same tensor twice would change places twice, or half
+    const auto bit_of = [](const void *p) { return (uint64_t)(uintptr_t)p * 0x9E3779B97F4A7C15ull >> 52; };
+    const auto nothing = [N](const kan_state_ref &t) { return t.outer == 0 || t.inner == 0 || t.bytes == 0 || N == 0; };
     for (int i = 0; i < n; ++i) {
         const kan_state_ref &t = list[i];
         if (t.outer < 0 || t.inner < 0 || t.bytes < 0) return KAN_ERR_INVALID_ARG;
-        if (t.outer == 0 || t.inner == 0 || t.bytes == 0 || N == 0) continue;
+        if (nothing(t)) continue;
         if (!t.data || !t.out) return KAN_ERR_INVALID_ARG;
-        const uint64_t place = (uint64_t)(uintptr_t)t.out * 0x9E3779B97F4A7C15ull >> 52, bit = 1ull << place % 64;
+        const uint64_t place = bit_of(t.out), bit = 1ull << place % 64;
         for (int k = 0; (seen[place / 64] & bit) && k < i; ++k)
-            if (list[k].out == t.out && list[k].outer && list[k].inner && list[k].bytes) return KAN_ERR_INVALID_ARG;
+            if (list[k].out == t.out && !nothing(list[k])) return KAN_ERR_INVALID_ARG;
         seen[place / 64] |= bit;
         const int64_t rows[3] = {t.outer, N * top, t.inner};
         if (!apart(rows, t.out_stride, t.bytes)) return KAN_ERR_INVALID_ARG;
@@ -194,6 +196,13 @@ int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, 
                 if (rows[d] > 1 && t.stride[d] != t.out_stride[d]) return KAN_ERR_INVALID_ARG;
         }
         if ((__int128)t.outer * t.inner * pieces_of(t, piece_of(top > B ? top : B)) >= (1ll << 31)) return KAN_ERR_UNSUPPORTED;
+    }
+    // nor is one read that is another one's output
+    for (int i = 0; i < n; ++i) {
+        const uint64_t place = bit_of(list[i].data);
+        if (list[i].data == list[i].out || nothing(list[i]) || !(seen[place / 64] >> place % 64 & 1)) continue;
+        for (int k = 0; k < n; ++k)
+            if (list[k].out == list[i].data && !nothing(list[k])) return KAN_ERR_INVALID_ARG;
     }
     return KAN_OK;
 }

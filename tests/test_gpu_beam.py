@@ -260,6 +260,22 @@ def test_states_past_32_bit_offsets():
     assert torch.equal(t[4, -40:], (torch.arange(length - 40, length, device="cuda") % 251 + 3).to(torch.uint8))
 
 
+def test_one_state_into_several_outputs_and_two_that_would_change_places():
+    """A state is read into as many outputs as are asked for; states that are one another's outputs are refused, not half exchanged."""
+    N, B = 3, 4
+    p = torch.from_numpy(order(N, B, B, 2, outside=0.0)).cuda()
+    a, b = values((N * B, 5, 33), BF16, 1), values((N * B, 5, 33), BF16, 2)
+    rows = (p + B * torch.arange(N, device="cuda")[:, None]).view(-1)
+    outs = [torch.empty_like(a) for _ in range(3)]
+    net.kan_beam_reorder(p, [a, b, a], B, out=outs)
+    assert torch.equal(outs[0], a[rows]) and torch.equal(outs[1], b[rows]) and torch.equal(outs[2], a[rows])
+    kept = a.clone(), b.clone()
+    for call in (net.kan_beam_reorder, autograd.beam_reorder):
+        with pytest.raises(RuntimeError):
+            call(p, [a, b], B, out=[b, a])
+    assert torch.equal(a, kept[0]) and torch.equal(b, kept[1])
+
+
 def test_reordering_captured_replayed_and_on_another_stream():
     N, B = 4, 4
     p = torch.from_numpy(order(N, B, B, 9, outside=0.0)).cuda()

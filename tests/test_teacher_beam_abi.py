@@ -88,6 +88,17 @@ def test_reorder_refusals(lib):
     assert UNSUPPORTED == run(state(data=1 << 20, size=1 << 36, stride=(0, 1 << 36, 0))) == run(state(data=1 << 20, outer=1 << 20, inner=1 << 12, size=1, stride=(1 << 20, 4096, 1)))
 
 
+def test_reorder_refuses_a_state_that_is_written_as_another_ones_output(lib):
+    """Two states that would change places, and one that is read into an output while it is reordered in place: whoever comes first would decide."""
+    def run(*states, N=2, B=3, top=3):
+        return lib.kan_beam_reorder(N, B, top, A, len(states), (net.KanStateRef * len(states))(*states), None)
+    a, b, c = 1 << 20, 2 << 20, 3 << 20
+    assert INVALID == run(state(data=a, out=b), state(data=b, out=a)) == run(state(data=a, out=a), state(data=a, out=c)) == run(state(data=b, out=c), state(data=a, out=b))
+    assert INVALID == run(state(data=a, out=c), state(data=b, out=1 << 22), state(data=b, out=a))
+    # one that is not looked at is in nobody's way
+    assert run(state(data=a, out=b, size=0), state(data=b, out=a, outer=0)) == OK
+
+
 def test_front_ends_refuse_host_tensors_and_wrong_shapes():
     from paper_2408_11200_amd import autograd
     z, ids, v, s = torch.zeros((6, 9)), torch.zeros((6, 2), dtype=torch.int64), torch.zeros((6, 2)), torch.zeros((2, 3))
