@@ -10,9 +10,8 @@
 // logits; behind the row those that reach the bound of all of it, hardly more than `top` of them, are read again, and their logits that do are put in order.
 // (Logits picked from each piece as it passed took the waves through some hundred instructions a piece more where no tokens stand out: 64 x 8 x 131072 bf16 48 us.)
 //
-// Measured: 128 x 8 x 131072 bf16 with sixteen 51 us for the rows (268 MB, 5.3 TB/s; all workgroups begin together, so the first 4 us and the last 4 are latency) and 4.8 for
-// the second launch; 4 x 32 x 131072 with 64 17 and 8; 1 x 4 x 32768 with four 6.1 and 3.8, one latency after another: scores 0.3 us, logits 1.2-2, bound 0.8, pieces again
-// 1.2-2, order 0.3-0.7.
+// Measured: 128 x 8 x 131072 bf16 with sixteen 50-53 us for the rows (268 MB, 5.1-5.3 TB/s; half of the workgroups wait 5 us for their first logits, as all begin together, and
+// each has 4 left after its last ones) and 4.8 for the second launch; 4 x 32 x 131072 with 64 17 and 8; 1 x 4 x 32768 with four 6.1 and 3.8, one latency after another.
 #include "net_softmax.hpp"
 
 namespace kannet {

@@ -10,12 +10,12 @@
 // listed one g (q P - p) / temperature: both differences are taken in 64 bits, where student and teacher nearly agree in all 32 kept ones.  The forward
 // pass leaves them (K + 2 floats a row), the backward pass reads no teacher.
 //
-// A wave a row up to 8192 tokens (16384 x 8192 bf16 57 us, 86 with four), four up to 128 KB of logits, eight beyond (the step of 8192 x 131072 bf16 929 us with four, 898 so; 8192 x 32768
-// 211 and 236): what a row costs beside its logits, some 5 us of its list and its 64-bit sums by one wave, has to be hidden by other rows.  Measured: 4093 x 50001 fp32, an
-// eighth of the rows without a teacher, forward 123 us (717 MB, 5.8 TB/s), backward 298 (1.54 GB, 5.1); 8192 x 131072 bf16 forward 328-378 (2.15 GB, 5.7-6.5), backward 710 (4.3 GB, 6.05): HBM.
-// The step reads the logits twice as well, the second time from the row's end, where they have been read last: 858 us (with two calls 1085; from the row's start 1150), 3.8 GB from
-// HBM and the memory-side cache and 2.2 written.  It keeps neither busy, nor the vector instructions (15 issue slots an element, 420 us): two workgroups of a CU, by their registers, are in
-// one another's way, and three with spilled registers took 954.
+// A wave a row up to 8192 tokens (forward of 16384 x 8192 bf16 57 us, 86 with four), four up to 128 KB of logits, eight beyond (the step of
+// 8192 x 131072 bf16 927 us with four, 898 so; 4096 x 50001 fp32 393 and 364; 8192 x 32768 bf16, below the line, 211 and 236).  Measured: 4093 x 50001
+// fp32, an eighth of the rows without a teacher, forward 123 us (717 MB, 5.8 TB/s), backward 298 (1.54 GB, 5.1); 8192 x 131072 bf16 forward 328-378
+// (2.15 GB, 5.7-6.5), backward 710 (4.3 GB, 6.05): HBM.  The step reads the logits twice as well, the second time from the row's end, where they have
+// been read last: 860 us of 8192 x 131072 bf16, 3.8 GB read past the L2 caches (4.3 without what they still hold) and 2.2 written, 6.95 TB/s there.
+// It has 96 registers, two workgroups a CU; a build for three spills and took 954 where this took 927.
 #include "net_softmax.hpp"
 
 namespace kannet {
