@@ -10,7 +10,7 @@
 // listed one g (q P - p) / temperature: both differences are taken in 64 bits, where student and teacher nearly agree in all 32 kept ones.  The forward
 // pass leaves them (K + 2 floats a row), the backward pass reads no teacher.
 //
-// A wave a row up to 8192 tokens (forward of 16384 x 8192 bf16 57 us, 86 with four), four up to 128 KB of logits, eight beyond (the step of
+// Sixteen lanes a row where rows are short and many, a wave up to 8192 tokens (forward of 16384 x 8192 bf16 57 us, 86 with four), four up to 128 KB of logits, eight beyond (the step of
 // 8192 x 131072 bf16 927 us with four, 898 so; 4096 x 50001 fp32 393 and 364; 8192 x 32768 bf16, below the line, 211 and 236).  Measured: 4093 x 50001
 // fp32, an eighth of the rows without a teacher, forward 123 us (717 MB, 5.8 TB/s), backward 298 (1.54 GB, 5.1); 8192 x 131072 bf16 forward 328-378
 // (2.15 GB, 5.7-6.5), backward 710 (4.3 GB, 6.05): HBM.  The step reads the logits twice as well, the second time from the row's end, where they have
@@ -41,7 +41,7 @@ struct DistillCall {
     uint32_t chunks;        // workgroups of a row, in the backward pass
 };
 
-// The teacher's list of a row, over a wave: entry e * 64 + lane.
+// The teacher's list of a row, over W lanes: entry e * W + lane.
 template <int E>
 struct List {
     int32_t id[E];                  // -1: nothing
@@ -51,13 +51,21 @@ struct List {
     bool some;
 };
 
-template <class T, int E>
+// whether it is so in any lane of a group of W
+template <int W>
+__device__ __forceinline__ bool any_of(bool v)
+{
+    if constexpr (W == 64) return __any(v);
+    else return __ballot(v) >> (threadIdx.x & (64 - W)) & ((1ull << W % 64) - 1);
+}
+
+template <class T, int E, int W = 64>
 __device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, const T *z, int lane, List<E> &l)
 {
     float value[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const int k = e * 64 + lane;
+        const int k = e * W + lane;
         l.id[e] = -1;
         l.z[e] = value[e] = -INFINITY;
         if (k < a.K) {
@@ -74,19 +82,19 @@ __device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, con
         float m = -INFINITY;
 #pragma unroll
         for (int e = 0; e < E; ++e) m = fmaxf(m, value[e]);
-        most = (double)lane_max<64>(m);
+        most = (double)lane_max<W>(m);
         if (most == -(double)INFINITY) most = 0.0;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e * 64 < a.K && l.id[e] >= 0) sum += exp_of(((double)value[e] - most) * a.t.inverse);
-        log_sum = log_of(wave_sum(sum));
+            if (e * W < a.K && l.id[e] >= 0) sum += exp_of(((double)value[e] - most) * a.t.inverse);
+        log_sum = log_of(group_sum<W>(sum));
     }
     sum = 0.0;
     bool some = false;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         l.p[e] = l.log_p[e] = 0.0;
-        if (e * 64 < a.K && l.id[e] >= 0) {
+        if (e * W < a.K && l.id[e] >= 0) {
             const bool logits = a.teacher_form == KAN_TEACHER_LOGITS && value[e] != -INFINITY;
             l.log_p[e] = logits ? ((double)value[e] - most) * a.t.inverse - log_sum : (double)value[e];
             l.p[e] = exp_of(l.log_p[e]);
@@ -94,9 +102,9 @@ __device__ __forceinline__ void read_list(const DistillCall &a, int64_t row, con
             some = some || l.p[e] != 0.0;
         }
     }
-    l.p_sum = wave_sum(sum);
+    l.p_sum = group_sum<W>(sum);
     l.p_rest = a.teacher_form == KAN_TEACHER_LOGP ? fmax(0.0, 1.0 - l.p_sum) : 0.0;
-    l.some = __any(some);
+    l.some = any_of<W>(some);
 }
 
 // What a row's gradients are made of
@@ -121,8 +129,8 @@ __device__ __forceinline__ bool repeats(const List<E> &l, int K, int lane)
     return __any(again);
 }
 
-// A row's loss and gradients from its list and the sum over the other tokens, by one wave.  `twice`: a token is in the list more than once.
-template <int E>
+// A row's loss and gradients from its list and the sum over the other tokens, by W lanes.  `twice`: a token is in the list more than once.
+template <int E, int W = 64>
 __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E> &l, Mass others, bool twice, int lane, RowGradient<E> &g)
 {
     bool first[E];
@@ -137,14 +145,15 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
         for (int e = 0; e < E; ++e) p_all[e] = 0.0;
 #pragma unroll
         for (int of = 0; of < E; ++of)
-            for (int k = 0; k < 64 && of * 64 + k < a.K; ++k) {
-                const int32_t id = __builtin_amdgcn_readlane(l.id[of], k);
-                const double p = __builtin_bit_cast(double, of_lane(__builtin_bit_cast(uint64_t, l.p[of]), k));
+            for (int k = 0; k < W && of * W + k < a.K; ++k) {
+                const int32_t id = of_group<W>(l.id[of], k);
+                const uint64_t bits = __builtin_bit_cast(uint64_t, l.p[of]);
+                const double p = __builtin_bit_cast(double, (uint64_t)(uint32_t)of_group<W>((int)(bits >> 32), k) << 32 | (uint32_t)of_group<W>((int)(uint32_t)bits, k));
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     if (l.id[e] == id) {
                         p_all[e] += p;
-                        if (of * 64 + k < e * 64 + lane) first[e] = false;
+                        if (of * W + k < e * W + lane) first[e] = false;
                     }
             }
     }
@@ -158,30 +167,30 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
     float m = rest ? others.m : -INFINITY;
 #pragma unroll
     for (int e = 0; e < E; ++e) m = fmaxf(m, l.z[e]);
-    const double M = (double)lane_max<64>(m);
+    const double M = (double)lane_max<W>(m);
     const bool empty = M == -(double)INFINITY && !rest;
     double weight[E], sum = 0.0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         weight[e] = 0.0;
-        if (e * 64 < a.K && l.id[e] >= 0) {
+        if (e * W < a.K && l.id[e] >= 0) {
             weight[e] = exp_of(((double)l.z[e] - M) * a.t.inverse);
             if (first[e]) sum += weight[e];
         }
     }
     const double down = ((double)others.m - M) * a.t.inverse, off = rest ? rest_sum * exp_of(down) : 0.0;
-    const double total = wave_sum(sum) + off, inverse = 1.0 / total, log_total = log_of(total), q_rest = off * inverse;
+    const double total = group_sum<W>(sum) + off, inverse = 1.0 / total, log_total = log_of(total), q_rest = off * inverse;
     const double p_rest = q_rest >= kNothing ? l.p_rest : 0.0, P = l.p_sum + p_rest;
     double loss = 0.0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         g.listed[e] = 0.0f;
-        if (e * 64 < a.K && l.id[e] >= 0) {
+        if (e * W < a.K && l.id[e] >= 0) {
             if (l.p[e] != 0.0) loss += l.p[e] * (l.log_p[e] - (((double)l.z[e] - M) * a.t.inverse - log_total));
             if (l.some && !empty) g.listed[e] = (float)((weight[e] * inverse * P - p_all[e]) * a.t.inverse);
         }
     }
-    loss = wave_sum(loss);
+    loss = group_sum<W>(loss);
     if (p_rest > 0.0) loss += p_rest * (log_of(p_rest) - (down + log_of(rest_sum) - log_total));
     // (without others no token asks for the factor but the masked ones of a row with a NaN among the listed)
     g.m = rest && l.some ? others.m : 0.0f;
@@ -189,7 +198,7 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
     return !l.some ? 0.0 : empty ? (double)INFINITY : loss;
 }
 
-template <int E>
+template <int E, int W = 64>
 __device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, double loss, const RowGradient<E> &g, int lane)
 {
     if (lane == 0 && a.loss) a.loss[row] = (float)loss;
@@ -201,19 +210,19 @@ __device__ __forceinline__ void write_row(const DistillCall &a, int64_t row, dou
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        if (e * 64 + lane < a.K) s[2 + e * 64 + lane] = g.listed[e];
+        if (e * W + lane < a.K) s[2 + e * W + lane] = g.listed[e];
 }
 
-// What makes a row's gradients as if no token were listed, the same for a workgroup: 2^(v * scale - reference) * factor, as in a tally, or where the reference is
+// What makes a row's gradients as if no token were listed: 2^(v * scale - reference) * factor, as in a tally, or where the reference is
 // too large for that (a NaN) 2^((v - m) * scale) * factor; factor 0: zeros, whatever the logits are.
 struct RowFactor {
     float m, reference, factor;
 };
 
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
+
 __device__ __forceinline__ RowFactor row_factor(float m, float factor, float scale)
 {
-    m = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, m)));
-    factor = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, factor)));
     const float reference = m * scale;
     const bool near = fabsf(reference) <= kNear;
     return RowFactor{m, near ? reference : NAN, near ? factor * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, scale, -reference)) : factor};
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DistillCall a)
         Round<T, NT> r;
         read_round<true>(r, z, (rounds - 1) * (kRound * NT), pieces, n);
         __syncthreads();
-        const RowFactor rest = row_factor(of_row[0], of_row[1], scale);
+        const RowFactor rest = row_factor(uniform(of_row[0]), uniform(of_row[1]), scale);
         for (uint32_t i = rounds; i-- > 0;) {
             const Round<T, NT> now = r;
             if (i) read_round<true>(r, z, (i - 1) * (kRound * NT), pieces, n);
@@ -369,7 +378,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillCall a)
     if (lane < a.parts) sum = a.part_sums[row * a.parts + lane];
     List<E> list;
     read_list(a, row, (const T *)a.logits + row * a.row_stride, lane, list);
-    sum = join_wave(sum, a.t.scale);
+    sum = join_lanes<64>(sum, a.t.scale);
     RowGradient<E> g;
     const double loss = finish_row(a, list, sum, repeats(list, a.K, lane), lane, g);
     write_row(a, row, loss, g, lane);
@@ -386,7 +395,7 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
     T *to = (T *)a.glogits + row * a.V;
     const float *s = a.stats + row * (a.K + 2);
     const float g = a.g_loss[row];
-    const RowFactor rest = row_factor(s[0], s[1] == 0.0f ? 0.0f : s[1] * g, a.t.scale);
+    const RowFactor rest = row_factor(uniform(s[0]), uniform(s[1] == 0.0f ? 0.0f : s[1] * g), a.t.scale);
     Round<T, NT> r;
     read_round<STREAM>(r, z, first, pieces, rest.factor == 0.0f ? 0 : V);      // rows without a teacher are not read
     // the listed tokens that lie here, by every wave for itself: most workgroups have none, and nothing to wait for
@@ -412,6 +421,154 @@ __global__ __launch_bounds__(NT) void distill_back_kernel(DistillCall a)
             }
 }
 
+// Short rows: 16 lanes each, sixteen rows a workgroup, written through the caches (16384 x 501 fp32 backward 12.5 us, past them 18.2: rows begin and end within lines).  With a wave a
+// row, half of the time is what a row costs in 64 bits, on no more lanes than the list has entries, and 65536 workgroups take 25 us before they do anything.
+constexpr int kLanes = 16, kRowsOf = 256 / kLanes;
+
+// whose row a thread works on; a workgroup's threads behind the last row go with it, and write nothing
+struct ShortRow {
+    int64_t row;
+    uint32_t lane, group;
+    bool there;
+};
+
+__device__ __forceinline__ ShortRow short_row(int64_t R)
+{
+    const uint32_t group = threadIdx.x / kLanes;
+    const int64_t row = (int64_t)blockIdx.x * kRowsOf + group;
+    return ShortRow{row < R ? row : R - 1, threadIdx.x % kLanes, group, row < R};
+}
+
+// f(logits, piece) for a lane's pieces of a row of n, four on their way while four are worked on
+template <class T, class F>
+__device__ __forceinline__ void each_of_short(const T *z, uint32_t lane, uint32_t pieces, uint32_t n, Raw<T, 16 / sizeof(T)> (&next)[kRound], F f)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    for (uint32_t first = lane; first < pieces; first += kRound * kLanes) {
+        Raw<T, N> now[kRound];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) now[u] = next[u];
+        if (first + kRound * kLanes < pieces)
+#pragma unroll
+            for (int u = 0; u < kRound; ++u) next[u] = raw_at<N>(z, (int64_t)(first + (kRound + u) * kLanes) * N, (int64_t)n);
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t p = first + u * kLanes;
+            if (p >= pieces) break;
+            float v[N];
+            piece_logits<N>(now[u], p, n, v);
+            f(v, p);
+        }
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void first_of_short(const T *z, uint32_t lane, uint32_t n, Raw<T, 16 / sizeof(T)> (&next)[kRound])
+{
+    constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) next[u] = raw_at<N>(z, (int64_t)(lane + u * kLanes) * N, (int64_t)n);
+}
+
+template <class T, int E, bool STEP>
+__global__ __launch_bounds__(256) void distill_short_kernel(DistillCall a)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    extern __shared__ uint32_t all_marks[];
+    __shared__ uint32_t twice[kRowsOf];
+    const ShortRow of = short_row(a.R);
+    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N, words = (V + 31) / 32;
+    const T *z = (const T *)a.logits + of.row * a.row_stride;
+    const float scale = a.t.scale;
+    uint32_t *marks = all_marks + of.group * words;
+    Raw<T, N> next[kRound];
+    first_of_short(z, of.lane, V, next);
+    for (uint32_t w = of.lane; w < words; w += kLanes) marks[w] = 0;
+    if (of.lane == 0) twice[of.group] = 0;
+    List<E> list;
+    read_list<T, E, kLanes>(a, of.row, z, of.lane, list);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int32_t id = list.id[e];
+        if (id >= 0 && (atomicOr(&marks[id / 32], 1u << id % 32) >> id % 32 & 1)) twice[of.group] = 1;
+    }
+    __syncthreads();
+    Tally tally = no_tally();
+    each_of_short(z, of.lane, pieces, V, next, [&](float (&v)[N], uint32_t p) {
+        const uint32_t bits = N == 8 ? ((const uint8_t *)marks)[p] : ((const uint8_t *)marks)[p / 2] >> (p % 2 * 4) & 15;
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = bits >> k & 1 ? -INFINITY : v[k];
+        add_piece<N>(v, scale, tally);
+    });
+    const Mass sum = join_lanes<kLanes>(mass_of(tally, scale), scale);
+    RowGradient<E> g;
+    const double loss = finish_row<E, kLanes>(a, list, sum, twice[of.group] != 0, of.lane, g);
+    if (of.there) write_row<E, kLanes>(a, of.row, loss, g, of.lane);
+    if constexpr (STEP) {
+        T *to = (T *)a.glogits + of.row * a.V;
+        const float weight = a.g_loss[of.row];
+        const RowFactor rest = row_factor(g.m, g.factor == 0.0f ? 0.0f : g.factor * weight, scale);
+        const uint32_t n = of.there ? V : 0;
+        first_of_short(z, of.lane, n, next);
+        each_of_short(z, of.lane, of.there ? pieces : 0, n, next, [&](float (&v)[N], uint32_t p) {
+            gradients(v, rest, scale);
+            store_at<N>(to, (int64_t)p * N, (int64_t)V, v);
+        });
+        __syncthreads();        // the listed tokens' gradients go on top
+        if (!of.there) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (list.id[e] >= 0) put(to + list.id[e], g.listed[e] == 0.0f ? 0.0f : g.listed[e] * weight);
+    }
+}
+
+template <class T, int E>
+__global__ __launch_bounds__(256) void distill_short_back_kernel(DistillCall a)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const ShortRow of = short_row(a.R);
+    if (!of.there) return;      // no barrier that they would be missed at: rows lie within waves
+    const uint32_t V = (uint32_t)a.V, pieces = (V + N - 1) / N;
+    const T *z = (const T *)a.logits + of.row * a.row_stride;
+    T *to = (T *)a.glogits + of.row * a.V;
+    const float *s = a.stats + of.row * (a.K + 2);
+    Raw<T, N> next[kRound];
+    first_of_short(z, of.lane, V, next);
+    const float g = a.g_loss[of.row], factor = s[1];
+    const RowFactor rest = row_factor(s[0], factor == 0.0f ? 0.0f : factor * g, a.t.scale);
+    int64_t id[E];
+    float listed[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int k = e * kLanes + of.lane;
+        id[e] = k < a.K ? a.ids[of.row * a.K + k] : -1;
+        listed[e] = k < a.K ? s[2 + k] : 0.0f;
+    }
+    each_of_short(z, of.lane, pieces, V, next, [&](float (&v)[N], uint32_t p) {
+        gradients(v, rest, a.t.scale);
+        store_at<N>(to, (int64_t)p * N, (int64_t)V, v);
+    });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the listed tokens' gradients go on top
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (id[e] >= 0 && id[e] < a.V) put(to + id[e], listed[e] == 0.0f ? 0.0f : listed[e] * g);
+}
+
+// The shortest ones always, longer ones where they are many: with few, a lane's longer way counts.  us, 16 lanes a row and a wave, forward, step, backward:
+//   256 x 64 fp32, K = 8     4.8 5.6,   5.7 6.6,   3.4 3.4        16384 x 64      7.3 22.8,   9.1 27.2,  4.4 7.8
+//   1024 x 256 fp32          5.7 5.9,   7.3 7.0,   4.1 3.6        65536 x 256 bf16 24 81,     33 100,    18 26
+//   4096 x 512 fp32          7.5 9.3,  11.2 12.0,  6.1 5.3        16384 x 501    12.1 25.3,  20.3 33.2, 12.5 15.8
+//   4096 x 1000 bf16, K = 20 8.9 9.5,  12.8 13.0,  6.8 6.3        65536 x 1000     50 93,     88 122,    59 58
+//   8192 x 2000 bf16, K = 20 15.7 19.5, 26.5 29.5, 14.5 15.4      65536 x 2000     72 120,   174 177,   139 121
+//   1024 x 1000 fp32, K = 8  10.2 7.1, 15.3 9.6,   7.6 4.9        65536 x 1000 fp32, K = 64  88 114, 217 168, 160 202
+// The forward pass and the step go the same way, whose sums have to be the same bits.
+bool is_short(const DistillCall &a, size_t size, bool back)
+{
+    const double bytes = (double)a.V * (double)size;
+    return a.K <= 64 && (bytes <= 512.0 || ((double)a.R >= 2.0 * bytes && (bytes <= 2048.0 || (bytes <= 4096.0 && a.K <= 32 && !back))));
+}
+
 // Few long rows are shared among workgroups, two a CU, and joined by a launch more.  Whole and cut, us, twenty tokens: 1 x 65536 bf16 8.2 and 7.6, 1 x 131072 11.3 and
 // 7.7, 64 x 131072 12.0 and 9.9, 128 x 131072 16.0 and 18.1, 16 x 32768 7.7 and 9.2; fp32: 64 x 50001 9.6 and 10.0, 100 x 131072 18.9 and 16.8, 200 x 131072 20.4 and
 // 22.8, 128 x 262144 32 and 27, 1 x 1000000 82 and 10.
@@ -423,7 +580,7 @@ int parts_of(int64_t R, int64_t V, size_t size)
     return (int)(parts > 64 ? 64 : parts);
 }
 
-constexpr int64_t kRows = 1 << 21;      // of a launch: less than 2^32 threads
+constexpr int64_t kRows = 1 << 21, kShortRows = 1 << 27;        // of a launch: less than 2^32 threads
 
 DistillCall rows_from(DistillCall a, int64_t first, int64_t most, size_t size)
 {
@@ -459,6 +616,17 @@ hipError_t launch_backward(const DistillCall &all, hipStream_t st)
     const bool stream = passes_by(all, sizeof(T));
     const int threads = pieces <= 64 * kRound ? 64 : 256;
     const int64_t chunks = div_up(pieces, (int64_t)threads * kRound), most = (1ll << 23) / chunks > 1 ? (1ll << 23) / chunks : 1;
+    if (is_short(all, sizeof(T), true)) {
+        for (int64_t first = 0; first < all.R; first += kShortRows) {
+            const DistillCall a = rows_from(all, first, kShortRows, sizeof(T));
+            const unsigned grid = (unsigned)div_up(a.R, (int64_t)kRowsOf);
+            if (a.K <= kLanes) distill_short_back_kernel<T, 1><<<grid, 256, 0, st>>>(a);
+            else distill_short_back_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     for (int64_t first = 0; first < all.R; first += most) {
         DistillCall a = rows_from(all, first, most, sizeof(T));
         a.chunks = (uint32_t)chunks;
@@ -489,6 +657,18 @@ hipError_t launch_rows(const DistillCall &all, hipStream_t st)
     prof::Timed timed(STEP ? "token_distill_step" : "token_distill", st);
     constexpr uint32_t N = 16 / sizeof(T);
     const uint32_t tokens = all.part_pieces * N < kMarked ? all.part_pieces * N : kMarked, lds = (tokens + 31) / 32 * 4;
+    if (is_short(all, sizeof(T), false)) {
+        const unsigned room = (unsigned)((all.V + 31) / 32 * 4) * kRowsOf;
+        for (int64_t first = 0; first < all.R; first += kShortRows) {
+            const DistillCall a = rows_from(all, first, kShortRows, sizeof(T));
+            const unsigned rows = (unsigned)div_up(a.R, (int64_t)kRowsOf);
+            if (a.K <= kLanes) distill_short_kernel<T, 1, STEP><<<rows, 256, room, st>>>(a);
+            else distill_short_kernel<T, 4, STEP><<<rows, 256, room, st>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     for (int64_t first = 0; first < all.R; first += kRows) {
         const DistillCall a = rows_from(all, first, kRows, sizeof(T));
         const unsigned grid = (unsigned)(a.R * a.parts);

@@ -94,19 +94,28 @@ __device__ __forceinline__ bool add_whole_round(const Round<T, NT> &of, float sc
     return true;
 }
 
-// over a wave: everyone's sum brought to the largest logit first.  All lanes get the first one's bits: the product and the first sum become one fused
-// multiply-add, whose rounding is another one in either lane of a pair.
-__device__ __forceinline__ Mass join_wave(Mass a, float scale)
+// a value of lane k of each group of W, k the same in all of a group
+template <int W>
+__device__ __forceinline__ int of_group(int v, int k)
 {
-    const float m = lane_max<64>(a.m), s = lane_sum<64>(a.s * power(a.m, m, scale));
-    return Mass{m, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, s)))};
+    if constexpr (W == 64) return __builtin_amdgcn_readlane(v, k);
+    else return __shfl(v, k, W);
+}
+
+// over groups of W lanes: everyone's sum brought to the largest logit first.  All lanes get the first one's bits: the product and the first sum become one fused
+// multiply-add, whose rounding is another one in either lane of a pair.
+template <int W>
+__device__ __forceinline__ Mass join_lanes(Mass a, float scale)
+{
+    const float m = lane_max<W>(a.m), s = lane_sum<W>(a.s * power(a.m, m, scale));
+    return Mass{m, __builtin_bit_cast(float, of_group<W>(__builtin_bit_cast(int, s), 0))};
 }
 
 // over a workgroup, the same in all threads; the caller's LDS is free again behind the next barrier
 template <int NT>
 __device__ __forceinline__ Mass join_mass(Mass a, float scale, Mass *lds)
 {
-    a = join_wave(a, scale);
+    a = join_lanes<64>(a, scale);
     if constexpr (NT > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
         __syncthreads();
@@ -121,18 +130,22 @@ __device__ __forceinline__ Mass join_mass(Mass a, float scale, Mass *lds)
     return a;
 }
 
-// the sum over a wave, the same bits in all lanes (sums of two lanes each, whichever of them asks).  Between registers: through LDS six exchanges of two
-// halves are a microsecond.
-__device__ __forceinline__ double wave_sum(double v)
+// the sum over groups of W lanes, 16 or 64, the same bits in all of a group (sums of two lanes each, whichever of them asks).  Between registers: through LDS six
+// exchanges of two halves are a microsecond.
+template <int W>
+__device__ __forceinline__ double group_sum(double v)
 {
+    static_assert(W == 16 || W == 64, "lanes of a row");
     const int lane = threadIdx.x & 63;
     const auto with = [&](uint64_t partner) { v += __builtin_bit_cast(double, partner); };
     with(of_partner<1>(__builtin_bit_cast(uint64_t, v), lane));
     with(of_partner<2>(__builtin_bit_cast(uint64_t, v), lane));
     with(of_partner<7>(__builtin_bit_cast(uint64_t, v), lane));
     with(of_partner<15>(__builtin_bit_cast(uint64_t, v), lane));
-    with(of_partner<16>(__builtin_bit_cast(uint64_t, v), lane));
-    with(of_partner<32>(__builtin_bit_cast(uint64_t, v), lane));
+    if constexpr (W == 64) {
+        with(of_partner<16>(__builtin_bit_cast(uint64_t, v), lane));
+        with(of_partner<32>(__builtin_bit_cast(uint64_t, v), lane));
+    }
     return v;
 }
 

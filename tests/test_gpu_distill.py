@@ -7,6 +7,8 @@ the term itself (|y| <= 20 where terms have weight), and the exponential 2 u: de
 What follows from it: the loss has d loss / d log sum = q_r P - p_r, and half a second derivative of at most q_r P; a listed token's gradient q P q_r; the
 factor of the others q_r (1 - q_r) P, whose own term adds (2.1 |y| + 6) u.  Results are rounded once: half a step.
 """
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -108,6 +110,62 @@ def test_loss_and_gradient(R, V, K, options):
     assert torch.equal(loss, o["loss"]) and torch.equal(x.grad, gz)
     with torch.no_grad():
         assert torch.equal(autograd.token_distill(logits, ids, values, T, teacher), o["loss"])
+
+
+# many short rows, at the sizes where a lane's pieces, a row's marks and the rows of a workgroup end; lists of one entry a lane and of four, tokens twice
+SHORT = [(R, V, K, dict(dtype=dtype, teacher=teacher, pad=pad, T=T))
+         for R, V, K, dtype, teacher, pad, T in (
+             (17, 33, 2, F32, "logp", 0, 1.0), (31, 65, 16, BF16, "logits", 1, 0.5), (16, 128, 17, F32, "logp", 0, 1.0), (15, 127, 64, F32, "logits", 3, 2.0),
+             (1, 256, 20, BF16, "logp", 0, 1.0), (47, 255, 33, BF16, "logp", 2, 1.0), (4096, 257, 16, F32, "logp", 1, 1.0), (4099, 512, 64, F32, "logits", 0, 0.75),
+             (4097, 1000, 20, BF16, "logp", 5, 1.0), (8193, 1021, 32, F32, "logp", 0, 1.0), (8200, 2041, 16, BF16, "logits", 7, 3.0), (8192, 1024, 33, F32, "logp", 0, 1.0))]
+
+
+@pytest.mark.parametrize("R,V,K,options", SHORT)
+def test_short_rows(R, V, K, options):
+    """Rows of 16 lanes: against the formulas within the bound of as many additions a lane (V / 16), one call's bits and the two calls', in place, a token twice."""
+    T, teacher = options["T"], options["teacher"]
+    logits, ids, values, g = case(R, V, K, R + V + K, **options)
+    ids[2::7, K - 1] = ids[2::7, 0]
+    rows = np.unique(np.concatenate([np.arange(min(R, 20)), [R - 1, R // 2]]))
+    f = plain.token_distill(host(logits)[rows], ids.cpu().numpy()[rows], host(values)[rows], T, teacher)
+    o = net.kan_token_distill_forward(logits, ids, values, T, teacher)
+    check(f, T, 4 * V, loss=o["loss"][rows])            # which counts V / 64 additions
+    gz = net.kan_token_distill_backward(logits, ids, o, g, T)
+    check(f, T, 4 * V, glogits=gz[rows], g=g[rows])
+    loss, gs = net.kan_token_distill_step(logits, ids, values, g, T, teacher)
+    assert torch.equal(loss, o["loss"]) and torch.equal(gs, gz)
+    own = logits.contiguous().clone()
+    assert torch.equal(net.kan_token_distill_backward(own, ids, o, g, T, glogits=own), gz)
+    own = logits.contiguous().clone()
+    loss, same = net.kan_token_distill_step(own, ids, values, g, T, teacher, glogits=own)
+    assert torch.equal(loss, o["loss"]) and torch.equal(same, gz)
+
+
+@pytest.mark.parametrize("R", [6, 9000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [24, 100, 1000])
+def test_short_rows_keep_to_themselves(dtype, V, R):
+    """Rows without a teacher, masked throughout, with a NaN, an infinity or only listed tokens beside ordinary ones, which have the bits that they have alone; and nothing
+    written behind the last row."""
+    K = 8
+    logits, ids, values, g = case(R, V, K, V, dtype=dtype, short=False)
+    logits = logits.contiguous()
+    a, b = net.kan_token_distill_step(logits, ids, values, g)
+    odd = logits.clone()
+    oi = ids.clone()
+    odd[0::6] = -math.inf
+    odd[1::6, V - 1] = math.nan
+    odd[2::6, V // 2] = math.inf
+    oi[3::6] = -1
+    odd[3::6, 0] = math.nan
+    odd[4::6] = -math.inf
+    odd[4::6] = odd[4::6].scatter(1, ids[4::6], 1.0)
+    buffer = torch.full((R + 3, V), 7.0, dtype=dtype, device="cuda")
+    loss, gz = net.kan_token_distill_step(odd, oi, values, g, glogits=buffer[:R])
+    f = plain.token_distill(host(odd)[:6], oi.cpu().numpy()[:6], host(values)[:6])
+    check(f, 1.0, 4 * V, loss=loss[:6], glogits=gz[:6], g=g[:6])
+    assert torch.equal(loss[5::6], a[5::6]) and torch.equal(gz[5::6], b[5::6]) and bool((buffer[R:] == 7.0).all())
+    assert bool((loss[3::6] == 0).all()) and bool((gz[3::6] == 0).all()) and bool(torch.isnan(loss[1::6]).all())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
