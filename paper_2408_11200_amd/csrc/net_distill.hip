@@ -165,10 +165,14 @@ __device__ __forceinline__ double finish_row(const DistillCall &a, const List<E>
         rest_sum *= exp_of(((double)from - (double)others.m) * a.t.inverse);
     }
     float m = rest ? others.m : -INFINITY;
+    bool nan = false;               // a NaN hides in the maximum
 #pragma unroll
-    for (int e = 0; e < E; ++e) m = fmaxf(m, l.z[e]);
+    for (int e = 0; e < E; ++e) {
+        m = fmaxf(m, l.z[e]);
+        nan = nan || l.z[e] != l.z[e];
+    }
     const double M = (double)lane_max<W>(m);
-    const bool empty = M == -(double)INFINITY && !rest;
+    const bool empty = M == -(double)INFINITY && !rest && !any_of<W>(nan);
     double weight[E], sum = 0.0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {

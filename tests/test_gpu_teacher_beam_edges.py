@@ -1,0 +1,55 @@
+"""Calls of distillation, beam selection and search that the documentation allows and whose answers are easily lost: against the plain forms in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import net as plain
+from paper_2408_11200_amd import autograd, net
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def dev(a, dtype=F32):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda().to(dtype)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ---- distillation ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("teacher", ["logp", "logits"])
+@pytest.mark.parametrize("R,V,K,dtype", [(8, 24, 2, F32), (9000, 24, 2, BF16), (9000, 1000, 3, F32), (4000, 500, 40, F32), (8, 5000, 70, BF16), (8, 40000, 2, F32), (8, 140000, 3, F32), (8, 140000, 90, BF16),
+                                         (300, 140000, 2, BF16)])
+def test_a_nan_among_listed_logits_that_are_all_the_mask_leaves(R, V, K, dtype, teacher):
+    """Every other token masked, and among the listed ones a NaN alone or beside -infinity: loss and gradients are NaN, as with any NaN in a row that has a teacher."""
+    rng = np.random.default_rng(V + K)
+    ids = np.stack([rng.permutation(V)[:K] for _ in range(8)])
+    v = np.log(rng.dirichlet(np.ones(K + 1), 8)[:, :K]).astype(np.float32)
+    z = np.full((8, V), -np.inf, np.float32)
+    z[0, ids[0, 0]] = np.nan                            # the others of the list -infinity
+    z[1, ids[1]] = np.nan
+    z[2, ids[2, K - 1]], ids[2, :K - 1] = np.nan, -1    # the one listed token
+    z[3, ids[3, 0]], v[3, 0] = np.nan, -np.inf          # the NaN's token without a probability
+    z[4, ids[4]], z[4, ids[4, 0]] = 1.0, np.nan         # finite ones beside it
+    ids[5] = -1                                         # no teacher: 0, whatever the row holds
+    z[5] = np.nan                                       # 6: nothing left by the mask, +infinity and no gradient
+    z[7] = rng.standard_normal(V)
+    many = lambda a: dev(np.tile(a, (-(-R // 8), 1))[:R]) if a.dtype != np.int64 else torch.from_numpy(np.tile(a, (-(-R // 8), 1))[:R]).cuda()
+    logits, di, dv, g = many(z).to(dtype), many(ids), many(v), torch.ones(R, device="cuda")
+    f = plain.token_distill(host(logits[:8]), ids, host(dv[:8]), 1.0, teacher)
+    assert np.isnan(f["loss"][:5]).all() and f["loss"][5] == 0 and f["loss"][6] == np.inf and np.isnan(f["d"][:5]).all()
+    o = net.kan_token_distill_forward(logits, di, dv, 1.0, teacher)
+    gz = net.kan_token_distill_backward(logits, di, o, g)
+    loss, gs = net.kan_token_distill_step(logits, di, dv, g, 1.0, teacher)
+    kind = torch.arange(R, device="cuda") % 8
+    for l, d in ((o["loss"], gz), (loss, gs)):
+        assert bool(torch.isnan(l[kind < 5]).all()) and bool(torch.isnan(d[kind < 5]).all())
+        assert not l[kind == 5].any() and bool((l[kind == 6] == math.inf).all()) and not d[(kind == 5) | (kind == 6)].any()
+        assert bool(torch.isfinite(l[kind == 7]).all()) and bool(torch.isfinite(d[kind == 7]).all())
