@@ -69,10 +69,10 @@ __device__ __forceinline__ float add_piece(const float (&v)[N], float scale, Tal
     return m;
 }
 
-// A round of whole pieces without a look for their largest logits: the reference is one of the row's logits, so the sum is 1 at least, what it is short of the
-// largest one does not matter to 32 bits, and a sum past kHigh (or a NaN), which asks for a larger reference, is seen in the end.  masked(v, u) may take logits
-// out of piece u.
-constexpr float kHigh = 7.9e28f;        // 2^96
+// A round of whole pieces without a look for their largest logits: the reference is one of the row's logits, so the sum is 1 at least, and a sum past kHigh (or a
+// NaN), which asks for a larger reference, is seen in the end.  An exponent y is off by up to 2^-24 y, and its term by as much of itself: 2^-20 for terms of up to 2^20 (2^-17 for
+// terms of up to 2^96, which fit a float as well: a sum that is mostly one of them was off by 43 of its roundings).  masked(v, u) may take logits out of piece u.
+constexpr float kHigh = 1048576.0f;     // 2^20
 
 template <class T, int NT, class F>
 __device__ __forceinline__ bool add_whole_round(const Round<T, NT> &of, float scale, Tally &a, F masked)

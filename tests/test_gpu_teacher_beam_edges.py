@@ -53,3 +53,35 @@ def test_a_nan_among_listed_logits_that_are_all_the_mask_leaves(R, V, K, dtype, 
         assert bool(torch.isnan(l[kind < 5]).all()) and bool(torch.isnan(d[kind < 5]).all())
         assert not l[kind == 5].any() and bool((l[kind == 6] == math.inf).all()) and not d[(kind == 5) | (kind == 6)].any()
         assert bool(torch.isfinite(l[kind == 7]).all()) and bool(torch.isfinite(d[kind == 7]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [5000, 8192, 40000, 50001, 140000])
+@pytest.mark.parametrize("T", [1.0, 0.75])
+def test_one_token_stands_out_behind_the_first_pieces(dtype, V, T):
+    """One unlisted logit 50 to 66 above all that came before it makes up the others' sum.  Its term is an exponential of an exponent near 0 (2 u), what the reference's rounding
+    is off by an exponential and a product more (3 u), the other terms are below 2^-24 of it together: the sum is off by 10 u at most, so the loss by 10 u q_r (and its own rounding), and
+    the gradients, q_v of either kind, by 10 u, their own factors' 10 u and half a step."""
+    R = 48
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((R, V)).astype(np.float32)
+    at = rng.integers(V // 3 * 2, V, R)
+    listed = rng.integers(0, V // 2, R)
+    z[np.arange(R), at] = np.linspace(50, 66, R).astype(np.float32) * T
+    logits = dev(z, dtype)
+    z = host(logits)
+    z[np.arange(R), listed] = z[np.arange(R), at] + rng.integers(-2, 3, R)
+    logits = dev(z.astype(np.float32), dtype)
+    ids, v, g = torch.from_numpy(listed[:, None]).cuda(), torch.zeros((R, 1), device="cuda"), torch.ones(R, device="cuda")
+    f = plain.token_distill(host(logits), listed[:, None], host(v), T)
+    o = net.kan_token_distill_forward(logits, ids, v, T)
+    gz = net.kan_token_distill_backward(logits, ids, o, g, T)
+    loss, gs = net.kan_token_distill_step(logits, ids, v, g, T)
+    assert torch.equal(loss, o["loss"]) and torch.equal(gs, gz)
+    err = np.abs(host(loss) - f["loss"]) / (U * np.abs(f["loss"]) + 10 * U * f["q_rest"])
+    assert err.max() <= 1, float(err.max())
+    half = 2.0 ** -8 if dtype == BF16 else U
+    for token in (at, listed):
+        want = f["d"][np.arange(R), token]
+        err = np.abs(host(gz)[np.arange(R), token] - want) / ((20 * U + half) * np.abs(want) * (1 + 2.0 ** -7))
+        assert err.max() <= 1, float(err.max())
