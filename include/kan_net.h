@@ -183,8 +183,8 @@ size_t kan_token_distill_workspace_bytes(int64_t R, int64_t V, int32_t K);      
      score(b, end_id) = scores[n][b]                                        the one candidate of a beam with ended[n][b] != 0, whose logits are not read
    A beam has no candidates, and its logits are not read, if its score is not finite (-infinity: a place without a beam; before the first step all
    but one); nor has one that goes on with a NaN, a +infinity or nothing but -infinity among its logits.  Scores below a float's range are no candidates either.
-   Candidates are ordered by score * rank_scale[n][b] (NULL: 1; positive and finite, otherwise the beam has none), in 64 bits, equal ones by beam, and those of equal
-   logits by token.
+   Candidates are ordered by score * rank_scale[n][b] (NULL: 1; positive and finite, otherwise the beam has none), in 64 bits, equal ones by beam, those of a beam by
+   logit (logits that differ can have equal scores), and those of equal logits by token.
    out_scores[n][j] (without rank_scale), tokens[n][j], parents[n][j] (0 .. B-1), out_ended[n][j] = the parent has ended or the token is end_id; where there are fewer
    than `top` candidates -infinity, -1, 0, 0.  ended NULL: none has; out_ended may be NULL.  end_id is a token, or -1 for none (ended NULL then).  1 <= top <= KAN_TOP_MAX, top <= B V.
    Outputs must not overlap inputs. */

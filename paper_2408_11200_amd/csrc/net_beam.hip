@@ -174,13 +174,12 @@ __global__ __launch_bounds__(NT) void beam_rows_kernel(BeamCall a)
     if (place < (uint32_t)a.top) to[place] = mine;
 }
 
-// A candidate as one number: larger ones first.  The upper 48 bits are those of its rank, ordered like the values (36 bits of the mantissa: a hundredth of a thousandth of
-// what the sum's rounding leaves open), the lower ones its place in the rows' lists, from the end: these lie in the order of beams, parts and likely tokens,
-// so of equal ranks the lower beam is first, and in a beam the lower token.  0: none.
-__device__ __forceinline__ uint64_t candidate_of(double rank, uint32_t place)
+// A candidate: larger ones first.  Its rank in all 64 bits, ordered like the values; of equal ones the lower beam, of one beam the larger logit (at a high temperature, or beside
+// a large score, logits that differ can have one rank), and of equal logits the place in the rows' lists, which lie in the order of a beam's parts and so of its tokens.  Rank 0: none.
+__device__ __forceinline__ Ranked candidate_of(double rank, uint32_t beam, uint32_t logit, uint32_t place)
 {
-    const uint64_t b = __builtin_bit_cast(uint64_t, rank + 0.0), ordered = (b >> 63) ? ~b : b | 0x8000000000000000ull;     // both zeros are one value
-    return (ordered & ~0xFFFFull) | (0xFFFFu - place);
+    const uint64_t b = __builtin_bit_cast(uint64_t, rank + 0.0);        // both zeros are one value
+    return Ranked{(b >> 63) ? ~b : b | 0x8000000000000000ull, (uint64_t)(KAN_BEAM_MAX - 1 - beam) << 48 | (uint64_t)logit << 16 | (0xFFFFu - place)};
 }
 
 enum { kOut = 0, kGoesOn = 1, kEnded = 2 };
@@ -202,8 +201,8 @@ __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
     constexpr uint32_t kWaves = NT / 64;
     __shared__ Mass sums[kLists];
     __shared__ Beam beams[KAN_BEAM_MAX];
-    __shared__ uint64_t waves_best[kWaves][64];
-    __shared__ uint64_t bound;
+    __shared__ Ranked waves_best[kWaves][64];
+    __shared__ Ranked bound;
     __shared__ uint16_t open[kLists];
     __shared__ uint32_t count;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), top = a.top, parts = a.parts, lists = a.B * parts;
@@ -249,14 +248,15 @@ __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
         return there && finite((float)score) ? score : -(double)INFINITY;
     };
     // entry j of list l as a candidate
-    const auto entry = [&](uint32_t l, uint32_t j, uint64_t key) -> uint64_t {
+    const Ranked none = {0, 0};
+    const auto entry = [&](uint32_t l, uint32_t j, uint64_t key) {
         const uint32_t b = l / parts;
         const Beam beam = beams[b];
         const double score = score_of(beam, j, l == b * parts, key);
-        return score > -(double)INFINITY ? candidate_of(score * (double)beam.rank_scale, l * top + j) : 0;
+        return score > -(double)INFINITY ? candidate_of(score * (double)beam.rank_scale, b, (uint32_t)(key >> 32), l * top + j) : none;
     };
-    const uint64_t first = takes && j < top ? entry(l, j, key) : 0;
-    uint64_t best = sorted(first, lane);
+    const Ranked first = takes && j < top ? entry(l, j, key) : none;
+    Ranked best = sorted(first, lane);
     // two waves' lists at a time, to the first wave
     const auto join = [&]() {
 #pragma unroll 1
@@ -270,32 +270,33 @@ __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
     if (step < top) {
         // What is below `top` others, or below an entry of its list that is, leads to none: left are the rests of the lists whose layers reach the `top`-th best of
         // these, a wave each.  (All lists layer by layer: 34 us for 256 lists of 64, whose likely tokens are in every eighth one.)
-        const uint64_t seen = of_lane(best, top - 1);
+        const Ranked seen = of_lane(best, top - 1);
         if (tid == 0) {
             bound = seen;
             count = 0;
         }
         __syncthreads();
-        if (takes && j == step - 1 && first > bound) open[atomicAdd(&count, 1u)] = (uint16_t)l;
+        if (takes && j == step - 1 && above(first, bound)) open[atomicAdd(&count, 1u)] = (uint16_t)l;
         __syncthreads();
-        if (wave != 0) best = 0;
+        if (wave != 0) best = none;
         for (uint32_t i = wave; i < count; i += kWaves) {
             const uint32_t l = open[i], j = step + lane;
-            const uint64_t c = j < top ? entry(l, j, keys[l * top + j]) : 0;
+            const Ranked c = j < top ? entry(l, j, keys[l * top + j]) : none;
             best = best_of(best, of_partner<63>(c, lane), lane);
         }
         join();
     }
     if (wave != 0 || lane >= top) return;
     const int64_t at = (int64_t)blockIdx.x * top + lane;
-    const uint32_t place = best ? 0xFFFFu - (uint32_t)(best & 0xFFFF) : 0, list = place / top, b = list / parts;
+    const bool there = best.rank != 0;
+    const uint32_t place = there ? 0xFFFFu - (uint32_t)(best.tie & 0xFFFF) : 0, list = place / top, b = list / parts;
     const Beam parent = beams[b];
     const uint64_t found = keys[place];
     const int64_t token = parent.state == kEnded ? a.end_id : (int64_t)(uint32_t)~(uint32_t)found;
-    a.out_scores[at] = best ? (float)score_of(parent, place % top, list == b * parts, found) : -INFINITY;
-    a.tokens[at] = best ? token : -1;
-    a.parents[at] = best ? b : 0;
-    if (a.out_ended) a.out_ended[at] = best && (parent.state == kEnded || token == a.end_id);
+    a.out_scores[at] = there ? (float)score_of(parent, place % top, list == b * parts, found) : -INFINITY;
+    a.tokens[at] = there ? token : -1;
+    a.parents[at] = there ? b : 0;
+    if (a.out_ended) a.out_ended[at] = there && (parent.state == kEnded || token == a.end_id);
 }
 
 // How rows are cut: few rows are shared among workgroups, two a CU, of a round of pieces (16 KB) at least.  Both launches, us, whole rows, two workgroups

@@ -127,7 +127,7 @@ __device__ __forceinline__ float value_of_rank(float v, int top, int lane, float
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), top - 1));
 }
 
-// the same networks on keys
+// the same networks on keys, and on what else has of_partner and above
 template <int X>
 __device__ __forceinline__ uint64_t of_partner(uint64_t v, int lane)
 {
@@ -135,23 +135,37 @@ __device__ __forceinline__ uint64_t of_partner(uint64_t v, int lane)
     return (uint64_t)__builtin_bit_cast(uint32_t, hi) << 32 | __builtin_bit_cast(uint32_t, lo);
 }
 
-template <int X, int D>
-__device__ __forceinline__ uint64_t ordered(uint64_t v, int lane)
+__device__ __forceinline__ bool above(uint64_t a, uint64_t b) { return a > b; }
+
+// Two numbers, the second one where the first ones are equal
+struct Ranked {
+    uint64_t rank, tie;
+};
+
+template <int X>
+__device__ __forceinline__ Ranked of_partner(Ranked v, int lane) { return Ranked{of_partner<X>(v.rank, lane), of_partner<X>(v.tie, lane)}; }
+
+__device__ __forceinline__ bool above(Ranked a, Ranked b) { return (a.rank > b.rank) | ((a.rank == b.rank) & (a.tie > b.tie)); }
+
+__device__ __forceinline__ Ranked of_lane(Ranked v, int lane) { return Ranked{of_lane(v.rank, lane), of_lane(v.tie, lane)}; }
+
+template <int X, int D, class K>
+__device__ __forceinline__ K ordered(K v, int lane)
 {
-    const uint64_t o = of_partner<X>(v, lane);
-    return ((v > o) != ((lane & D) != 0)) ? v : o;
+    const K o = of_partner<X>(v, lane);
+    return (above(v, o) != ((lane & D) != 0)) ? v : o;
 }
 
-template <int D>
-__device__ __forceinline__ uint64_t merged(uint64_t v, int lane)
+template <int D, class K>
+__device__ __forceinline__ K merged(K v, int lane)
 {
     v = ordered<D, D>(v, lane);
     if constexpr (D > 1) v = merged<D / 2>(v, lane);
     return v;
 }
 
-template <int S = 64>
-__device__ __forceinline__ uint64_t sorted(uint64_t v, int lane)
+template <int S = 64, class K>
+__device__ __forceinline__ K sorted(K v, int lane)
 {
     if constexpr (S > 2) v = sorted<S / 2>(v, lane);
     v = ordered<S - 1, S / 2>(v, lane);
@@ -160,7 +174,8 @@ __device__ __forceinline__ uint64_t sorted(uint64_t v, int lane)
 }
 
 // of a wave's falling list and another one, backwards (entry 63 - lane), the first 64, falling
-__device__ __forceinline__ uint64_t best_of(uint64_t list, uint64_t backwards, int lane) { return merged<32>(list > backwards ? list : backwards, lane); }
+template <class K>
+__device__ __forceinline__ K best_of(K list, K backwards, int lane) { return merged<32>(above(list, backwards) ? list : backwards, lane); }
 
 // how many of `count` keys in LDS are above k
 __device__ __forceinline__ int above(const uint64_t *keys, uint32_t count, uint64_t k)

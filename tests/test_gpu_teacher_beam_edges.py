@@ -85,3 +85,51 @@ def test_one_token_stands_out_behind_the_first_pieces(dtype, V, T):
         want = f["d"][np.arange(R), token]
         err = np.abs(host(gz)[np.arange(R), token] - want) / ((20 * U + half) * np.abs(want) * (1 + 2.0 ** -7))
         assert err.max() <= 1, float(err.max())
+
+
+# ---- beam selection -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,top", [(8, 8), (64, 64), (64, 5), (33, 40)])
+def test_ranks_of_ended_beams_are_compared_in_64_bits(B, top):
+    """An ended beam's rank is the product of two floats, exact in 64 bits: products that agree to 2^-37 of themselves, and some that are equal, in the order of the products, then of the beams."""
+    rng = np.random.default_rng(B)
+    s = -np.float32(1.1 + rng.random(1 << 18) * 0.5)
+    scale = np.float32(1.37 / -s.astype(np.float64))
+    product = s.astype(np.float64) * scale
+    order = np.argsort(product)
+    gap = np.diff(product[order])
+    near = np.where((gap > 0) & (gap < 2.0 ** -37))[0]
+    N = 30
+    pick = np.stack([np.concatenate([order[near[rng.integers(len(near))]] + np.zeros(1, int), order[(a := near[rng.integers(len(near))]):a + 2], rng.integers(0, len(s), B - 3)]) for _ in range(N)])
+    pick[:, B // 2] = pick[:, 0]                        # one rank twice
+    pick = rng.permuted(pick, axis=1)
+    scores, scales = s[pick], scale[pick]
+    d = torch.from_numpy
+    z = torch.randn((N * B, 40), device="cuda")
+    o = net.kan_beam_select(z, d(scores).cuda(), top, torch.ones((N, B), dtype=torch.bool, device="cuda"), 7, d(scales).cuda())
+    want = np.argsort(-product[pick], axis=1, kind="stable")[:, :top]
+    there = min(top, B)
+    assert np.array_equal(o["parents"].cpu().numpy()[:, :there], want) and bool((o["tokens"][:, :there] == 7).all()) and bool((o["tokens"][:, there:] == -1).all())
+    assert np.array_equal(o["scores"].cpu().numpy()[:, :there], np.take_along_axis(scores, want, 1)) and bool(o["ended"][:, :there].all())
+
+
+@pytest.mark.parametrize("score,T", [(-1.0, 1e30), (-1e4, 1.0), (-1e6, 1.0), (-1e9, 1.0), (-3e4, 1e4), (0.0, 1e-3)])
+@pytest.mark.parametrize("N,V,top", [(1, 262144, 64), (2, 40000, 12), (300, 40000, 12), (5, 3000, 64), (3, 33, 33)])
+def test_a_beams_tokens_come_in_the_order_of_their_logits(score, T, N, V, top):
+    """Scores that differ in their last bits or not at all, at a high temperature or beside a large score of the beam: one beam's candidates are its largest logits, equal ones by token, however its
+    row is cut.  Where all are equal and scores of beams too, the first beam has them all."""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((min(N, 3), V)).astype(np.float32)
+    z[:, V // 3] = z[:, V - 1] = z.max(1)               # the largest one three times
+    if V > 100:
+        z[0, V // 2:V // 2 + 40] = z[0].max() - np.float32(2.0 ** -20) * np.arange(40)
+    want = np.argsort(-z, axis=1, kind="stable")[:, :top]
+    rows = np.arange(N) % len(z)
+    logits = dev(z[rows])
+    o = net.kan_beam_select(logits, torch.full((N, 1), score, device="cuda"), top, temperature=T)
+    got = o["tokens"].cpu().numpy()
+    there = host(o["scores"]) > -np.inf
+    assert np.array_equal(got, np.where(there, want[rows], -1)) and (T == 1e-3 or there.all())
+    if T == 1e30:
+        both = net.kan_beam_select(logits.repeat_interleave(2, 0), torch.full((N, 2), score, device="cuda"), top, temperature=T)
+        assert torch.equal(both["tokens"], o["tokens"]) and not both["parents"].any()
