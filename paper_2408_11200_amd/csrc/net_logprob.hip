@@ -88,7 +88,12 @@ __device__ __forceinline__ Sums join_all(Sums s, float scale, Sums *lds)
     rescale(s, m, scale);
     s.s = lane_sum<64>(s.s);
     s.t = lane_sum<64>(s.t);
-    if (NT == 64) return s;
+    if (NT == 64) {
+        // the first lane's bits for all, which take one way behind them: the product in rescale and the first sum become one fused multiply-add, whose rounding is another one
+        // in either lane of a pair
+        s.s = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, s.s)));
+        return s;
+    }
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
     __syncthreads();

@@ -145,6 +145,28 @@ def test_logprob_of_confident_rows(V, dtype, temperature, copies):
         assert (np.abs(got[:R] - want) <= tol).all(), (ga is None, gb is None, (np.abs(got[:R] - want) / tol).max())
 
 
+@pytest.mark.parametrize("V,temperature", [(64, 1.0), (100, 0.75), (257, 1.0), (1000, 1.0)])
+def test_logprob_of_rows_whose_sum_is_at_the_line_of_one_likely_token(V, temperature):
+    """Sums of exponentials of 5/4 to within 32 of their last places, where rows are told apart that are summed once more without the largest logit: a row of one wave goes one way as a whole.  Relative
+    errors as for confident rows: 1100 u."""
+    R, rng = 1 << 15, np.random.default_rng(V)
+    z = rng.standard_normal((R, V)) * 2
+    z[:, 0] = 0.0
+    z[:, 1:-1] += np.log(0.2 / np.exp(z[:, 1:-1]).sum(1, keepdims=True))
+    z = np.float32(z * temperature)
+    others = np.exp(z[:, 1:-1].astype(np.float64) / temperature).sum(1)
+    z[:, -1] = temperature * np.log(0.25 + (np.arange(R) % 64 - 32) * 2.0 ** -23 - others)
+    z[:, [0, V // 2]] = z[:, [V // 2, 0]]
+    ids = np.where(np.arange(R) % 2, V // 2, V - 1)
+    o = net.kan_token_logprob_forward(dev(z), dev(ids, torch.int64), temperature, 3)
+    ref = plain.token_logprob(z, ids, temperature, 3)
+    assert np.array_equal(o["top_ids"].cpu().numpy()[:, :1], ref["top_ids"][:, :1])
+    for name in ("logp", "entropy", "top_logp"):
+        off = np.abs(host(o[name]) - ref[name]) / np.abs(ref[name])
+        assert off.max() <= 1100 * U, (name, off.max() / U)
+    assert (np.abs(host(o["stats"])[:, 1] - (1.0 / ref["p"][np.arange(R), V // 2] - 1.0)) <= 1100 * U * 0.25).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("V,R", [(20, 3), (5000, 3), (40000, 3), (33000, 520)])
 @pytest.mark.parametrize("temperature", [1.0, 4.0, 1e10, 1e30])
