@@ -205,9 +205,9 @@ typedef struct kan_state_ref {
 } kan_state_ref;
 
 /* Row n top + j of every out = row n B + parents[n][j] of its data, j < top <= KAN_BEAM_MAX; a parent outside 0 .. B-1 leaves row j as it was.  out may be data, with the
-   same strides, where top is B (in place: rows that are their own parents are not touched); other overlaps are not allowed, nor is an out that is in the list twice,
-   another entry's data, or around the parents.  A tensor's rows of a search have less than 2^31 runs and
-   pieces of 16 bytes. */
+   same strides, where top is B (in place: rows that are their own parents are not touched).  No other byte of an out may be read or written by an entry of the list, nor lie around
+   the parents (KAN_ERR_INVALID_ARG; KAN_ERR_UNSUPPORTED for strides that do not lie within one another and take too long to tell); entries may lie between one another's runs.  A tensor's
+   rows of a search have less than 2^31 runs and pieces of 16 bytes (8 where top or B is above 16, 4 above 32). */
 int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list, void *stream);
 
 #ifdef __cplusplus

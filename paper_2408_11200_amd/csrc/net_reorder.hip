@@ -2,11 +2,12 @@
 //
 // A copy, bound by HBM: each row that moves is written once, the row in whose place it comes is read.  In place the rows of a search can
 // change places with one another, so whoever writes a byte of one of them has to have read that byte of all: a thread has one piece of 16
-// bytes of every row of a search, reads it from the parents' rows, and writes it then.  Pieces of different threads do not overlap, a run's
+// bytes (8 for more than 16 rows, 4 for more than 32) of every row of a search, reads it from the parents' rows, and writes it then.  Pieces of different threads do not overlap, a run's
 // last bytes are read and written as they are, hence no wait between threads, no buffer, and no order of the rows to find.  Rows that
 // stay are left out.  A launch takes up to kMost tensors from its arguments.  What is written goes past the caches (24 x 6 rows of 117 x 771 bf16 into other buffers 68 us,
 // 75 through them; of 117 x 768, six rows read, 56 and 82).  Measured: caches of 4 x 8 rows of 8 heads, 2000 of 2304 x 128 bf16, 16 of them, 2.1 GB to move, 355 us (5.9 TB/s); the
 // 24 x 6 x 117 x 771 above, 312 MB, 56 on the same states again and 66 on others (4.7 TB/s: rows that start anywhere in a line).
+#include <algorithm>
 #include "net_device.hpp"
 
 namespace kannet {
@@ -161,35 +162,145 @@ int piece_of(int top) { return top <= 16 ? 16 : top <= 32 ? 8 : 4; }
 
 int64_t pieces_of(const kan_state_ref &t, int piece) { return t.bytes / piece + (t.bytes % piece ? 1 : 0); }
 
-// from an output's first byte to its last one
-__int128 span(const int64_t (&count)[3], const int64_t (&stride)[3], int64_t bytes)
+// What an entry reads or writes: runs of `bytes` bytes, `count` of them `stride` apart in each dimension, from the lowest address on
+struct Region {
+    uint64_t first, last;               // bytes from the first one to behind the last one
+    int64_t count[3], stride[3], bytes;
+};
+
+// false: no memory is like that
+bool region_of(const void *at, const int64_t (&count)[3], const int64_t (&stride)[3], int64_t bytes, Region &r)
 {
-    __int128 n = bytes;
-    for (int d = 0; d < 3; ++d) n += count[d] > 1 ? (__int128)stride[d] * (count[d] - 1) : 0;
-    return n;
+    __int128 first = (uintptr_t)at, extent = bytes;
+    for (int d = 0; d < 3; ++d) {
+        const int64_t n = stride[d] ? count[d] : 1;     // rows that are one and the same
+        r.count[d] = n;
+        r.stride[d] = n > 1 ? stride[d] : 0;
+        const __int128 reach = (__int128)r.stride[d] * (n - 1);
+        if (reach < 0) {
+            first += reach;
+            r.stride[d] = -r.stride[d];
+        }
+        extent += reach < 0 ? -reach : reach;
+    }
+    r.bytes = bytes;
+    if (first < 0 || extent >= (__int128)1 << 62 || first + extent > (__int128)UINT64_MAX) return false;
+    r.first = (uint64_t)first;
+    r.last = (uint64_t)(first + extent);
+    return true;
+}
+
+// Whether two regions have a byte in common: a run of one and a run of the other begin at a distance from -bytes to +bytes of one another.  The distances are sums of multiples of the strides, one
+// range of factors for each different stride; for the largest one only the factors are looked at that the others can make up for, and so on.  Strides that lie within one another, as those of
+// views of one buffer do, leave one or two factors each.  `left` bounds what is tried; -1: it did not do.
+struct Steps {
+    int n;
+    int64_t stride[6], lo[6], hi[6];    // largest stride first
+    int64_t least[7], most[7];          // what the strides from here on can make
+};
+
+int reaches(const Steps &s, int d, int64_t least, int64_t most, int &left)
+{
+    if (d == s.n) return least <= 0 && most >= 0;
+    const int64_t stride = s.stride[d], from = least - s.most[d + 1], to = most - s.least[d + 1];
+    const int64_t lo = std::max(s.lo[d], from / stride + (from % stride > 0)), hi = std::min(s.hi[d], to / stride - (to % stride < 0));
+    for (int64_t k = lo; k <= hi; ++k) {
+        if (--left < 0) return -1;
+        const int found = reaches(s, d + 1, least - k * stride, most - k * stride, left);
+        if (found) return found;
+    }
+    return 0;
+}
+
+int meet(const Region &a, const Region &b)
+{
+    Steps s;
+    s.n = 0;
+    const auto add = [&](int64_t stride, int64_t lo, int64_t hi) {
+        if (!stride) return;
+        int at = 0;
+        while (at < s.n && s.stride[at] > stride) ++at;
+        if (at == s.n || s.stride[at] != stride) {
+            for (int k = s.n++; k > at; --k) s.stride[k] = s.stride[k - 1], s.lo[k] = s.lo[k - 1], s.hi[k] = s.hi[k - 1];
+            s.stride[at] = stride, s.lo[at] = s.hi[at] = 0;
+        }
+        s.lo[at] += lo, s.hi[at] += hi;
+    };
+    for (int d = 0; d < 3; ++d) {
+        add(a.stride[d], 0, a.count[d] - 1);
+        add(b.stride[d], 1 - b.count[d], 0);
+    }
+    s.least[s.n] = s.most[s.n] = 0;
+    for (int d = s.n; d-- > 0;) s.least[d] = s.least[d + 1] + s.lo[d] * s.stride[d], s.most[d] = s.most[d + 1] + s.hi[d] * s.stride[d];
+    int left = 1 << 16;
+    const int64_t apart = (int64_t)(b.first - a.first);
+    return reaches(s, 0, apart - a.bytes + 1, apart + b.bytes - 1, left);
+}
+
+// Whether anything that is written lies where something else is read or written: in the order of their first bytes, each against those that begin before it ends.  kTogether entries at a
+// time, and two times as many for the pairs among them, so that nothing is allocated.
+constexpr int kTogether = 128;
+
+struct Part {
+    Region region;
+    int entry;
+    bool written;
+};
+
+bool empty(const kan_state_ref &t) { return t.outer == 0 || t.inner == 0 || t.bytes == 0; }
+
+int overlaps(int64_t N, int32_t B, int32_t top, int32_t n, const kan_state_ref *list)
+{
+    Part part[4 * kTogether];
+    uint16_t order[4 * kTogether];
+    for (int one = 0; one < n; one += kTogether)
+        for (int other = one; other < n; other += kTogether) {
+            int m = 0;
+            const auto gather = [&](int first) {
+                for (int i = first; i < n && i < first + kTogether; ++i) {
+                    const kan_state_ref &t = list[i];
+                    if (empty(t)) continue;
+                    const int64_t rows[3] = {t.outer, N * top, t.inner}, from[3] = {t.outer, N * B, t.inner};
+                    part[m].entry = i;
+                    part[m].written = true;
+                    if (!region_of(t.out, rows, t.out_stride, t.bytes, part[m++].region)) return false;
+                    if (t.data == t.out) continue;      // in place
+                    part[m].entry = i;
+                    part[m].written = false;
+                    if (!region_of(t.data, from, t.stride, t.bytes, part[m++].region)) return false;
+                }
+                return true;
+            };
+            if (!gather(one) || (other != one && !gather(other))) return KAN_ERR_INVALID_ARG;
+            for (int i = 0; i < m; ++i) order[i] = (uint16_t)i;
+            std::sort(order, order + m, [&](uint16_t a, uint16_t b) { return part[a].region.first < part[b].region.first; });
+            for (int i = 0; i < m; ++i)
+                for (int k = i + 1; k < m && part[order[k]].region.first < part[order[i]].region.last; ++k) {
+                    const Part &a = part[order[i]], &b = part[order[k]];
+                    if ((!a.written && !b.written) || (other != one && a.entry / kTogether == b.entry / kTogether)) continue;
+                    const int found = meet(a.region, b.region);
+                    if (found) return found < 0 ? KAN_ERR_UNSUPPORTED : KAN_ERR_INVALID_ARG;
+                }
+        }
+    return KAN_OK;
 }
 
 int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, const kan_state_ref *list)
 {
     if (N < 0 || B < 1 || top < 1 || n < 0 || (n > 0 && !list)) return KAN_ERR_INVALID_ARG;
     if (B > KAN_BEAM_MAX || top > KAN_BEAM_MAX || N >= (1ll << 31) / KAN_BEAM_MAX) return KAN_ERR_UNSUPPORTED;
-    uint64_t seen[64] = {};             // places of outputs, one bit each: the same tensor twice would change places twice, or half
-    const auto bit_of = [](const void *p) { return (uint64_t)(uintptr_t)p * 0x9E3779B97F4A7C15ull >> 52; };
-    const auto nothing = [N](const kan_state_ref &t) { return t.outer == 0 || t.inner == 0 || t.bytes == 0 || N == 0; };
     for (int i = 0; i < n; ++i) {
         const kan_state_ref &t = list[i];
         if (t.outer < 0 || t.inner < 0 || t.bytes < 0) return KAN_ERR_INVALID_ARG;
-        if (nothing(t)) continue;
+        if (empty(t) || N == 0) continue;
         if (!t.data || !t.out) return KAN_ERR_INVALID_ARG;
-        const uint64_t place = bit_of(t.out), bit = 1ull << place % 64;
-        for (int k = 0; (seen[place / 64] & bit) && k < i; ++k)
-            if (list[k].out == t.out && !nothing(list[k])) return KAN_ERR_INVALID_ARG;
-        seen[place / 64] |= bit;
         const int64_t rows[3] = {t.outer, N * top, t.inner};
         if (!apart(rows, t.out_stride, t.bytes)) return KAN_ERR_INVALID_ARG;
         // the parents are read while rows are written
-        const __int128 from = (uintptr_t)t.out, order = (uintptr_t)parents;
-        if (parents && order < from + span(rows, t.out_stride, t.bytes) && from < order + (__int128)N * top * 8) return KAN_ERR_INVALID_ARG;
+        Region out;
+        if (!region_of(t.out, rows, t.out_stride, t.bytes, out)) return KAN_ERR_INVALID_ARG;
+        const uint64_t order = (uintptr_t)parents;
+        if (parents && order < out.last && out.first < order + (uint64_t)N * top * 8) return KAN_ERR_INVALID_ARG;
         if (t.data == t.out) {
             if (top != B) return KAN_ERR_INVALID_ARG;
             for (int d = 0; d < 3; ++d)
@@ -197,14 +308,7 @@ int check(int64_t N, int32_t B, int32_t top, const int64_t *parents, int32_t n, 
         }
         if ((__int128)t.outer * t.inner * pieces_of(t, piece_of(top > B ? top : B)) >= (1ll << 31)) return KAN_ERR_UNSUPPORTED;
     }
-    // nor is one read that is another one's output
-    for (int i = 0; i < n; ++i) {
-        const uint64_t place = bit_of(list[i].data);
-        if (list[i].data == list[i].out || nothing(list[i]) || !(seen[place / 64] >> place % 64 & 1)) continue;
-        for (int k = 0; k < n; ++k)
-            if (list[k].out == list[i].data && !nothing(list[k])) return KAN_ERR_INVALID_ARG;
-    }
-    return KAN_OK;
+    return N == 0 ? KAN_OK : overlaps(N, B, top, n, list);
 }
 
 template <bool STREAM>

@@ -133,3 +133,49 @@ def test_a_beams_tokens_come_in_the_order_of_their_logits(score, T, N, V, top):
     if T == 1e30:
         both = net.kan_beam_select(logits.repeat_interleave(2, 0), torch.full((N, 2), score, device="cuda"), top, temperature=T)
         assert torch.equal(both["tokens"], o["tokens"]) and not both["parents"].any()
+
+
+# ---- reordering -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N,B", [(3, 4), (1, 20), (2, 64)])
+def test_states_side_by_side_in_one_buffer(N, B):
+    """Layers' keys and values lie between one another's rows: nothing crosses, in place, or from one half of every row into the other; and many of them in a call."""
+    rng = np.random.default_rng(B)
+    p = rng.integers(0, B, (N, B))
+    parents = torch.from_numpy(p).cuda()
+    rows = torch.from_numpy((p + B * np.arange(N)[:, None]).ravel()).cuda()
+    for reorder in (net.kan_beam_reorder, autograd.beam_reorder):
+        buffer = torch.randn((N * B, 3, 2, 4, 30, 5), device="cuda")
+        before = buffer.clone()
+        reorder(parents, [buffer[:, l, k, :, :17] for l in range(3) for k in range(2)], B)
+        want = before.clone()
+        want[:, :, :, :, :17] = before[rows][:, :, :, :, :17]
+        assert torch.equal(buffer, want)
+        buffer.copy_(before)
+        reorder(parents, [buffer[:, l, 0, :, :17] for l in range(3)], B, out=[buffer[:, l, 1, :, 13:] for l in range(3)])
+        want = before.clone()
+        want[:, :, 1, :, 13:] = before[rows][:, :, 0, :, :17]
+        assert torch.equal(buffer, want)
+        wide = torch.randn((N * B, 300, 7), device="cuda", dtype=torch.float32).to(BF16)
+        before = wide.clone()
+        reorder(parents, [wide[:, k, :] for k in range(0, 300)], B)
+        assert torch.equal(wide, before[rows])
+        tall = torch.randn((6, N * B, 5), device="cuda")
+        before = tall.clone()
+        reorder(parents, [tall[::2], tall[1::2]], B, dim=1)
+        assert torch.equal(tall, before[:, rows])
+
+
+def test_states_that_cross_are_refused_and_left():
+    N, B = 2, 3
+    p = torch.tensor([[1, 0, 2], [2, 2, 0]], device="cuda")
+    t = torch.randn((6, 9, 4), device="cuda")
+    before = t.clone()
+    for reorder in (net.kan_beam_reorder, autograd.beam_reorder):
+        for data, out in (([t[:, 1:]], [t[:, :-1]]), ([t[:, :5]], [t[:, 4:]]), ([t[:, :3], t[:, 2:6]], None), ([before, before], [t[:, :], t.flatten(1)[:, 1:].unflatten(1, (5, 7))[:, :, :4]])):
+            if out and any(d.shape != o.shape for d, o in zip(data, out)):
+                data = [d[:, :o.shape[1]] for d, o in zip(data, out)]
+            with pytest.raises(RuntimeError):
+                reorder(p, data, B, out=out)
+        assert torch.equal(t, before)
+        reorder(p, [t[:, :5]], B, out=[t[:, 5:].new_empty((6, 5, 4))])

@@ -99,6 +99,67 @@ def test_reorder_refuses_a_state_that_is_written_as_another_ones_output(lib):
     assert run(state(data=a, out=b, size=0), state(data=b, out=a, outer=0)) == OK
 
 
+def test_reorder_refuses_outputs_that_cross(lib):
+    """A state shifted within its own buffer, outputs that begin at different bytes of one another, and one that is read behind its first row by another entry."""
+    def run(*states, N=2, B=3, top=3):
+        return lib.kan_beam_reorder(N, B, top, A, len(states), (net.KanStateRef * len(states))(*states), None)
+    a, b, row = 1 << 20, 2 << 20, 24
+    assert INVALID == run(state(data=a, out=a + 8, size=16)) == run(state(data=a + 8, out=a, size=16)) == run(state(data=a, out=a + row)) == run(state(data=a, out=a - 5 * row))
+    assert INVALID == run(state(data=a, out=b), state(data=a, out=b + 5 * row + 23)) == run(state(data=b, out=b), state(data=a, out=b + 8)) == run(state(data=a, out=b), state(data=b - 23, out=3 << 20))
+    # from the buffer's first half of a row into its second one, and a byte more; more rows out than in
+    assert INVALID == run(state(data=a, out=a + 12, size=13)) == run(state(data=a, out=a + 6 * row), state(data=b, out=a + 12 * row - 1))
+    assert INVALID == run(state(data=a, out=a + 2 * row, size=8, stride=(0, row, 0), out_stride=(0, row, 0)), top=2)
+    # blocks and runs: the other's row, run or block only
+    wide = dict(outer=3, inner=2, size=4)
+    assert INVALID == run(state(data=a, out=b, stride=(960, 96, 24), **wide), state(data=a, out=b + 960 + 96 * 4 + 24 + 3, stride=(960, 96, 24), **wide))
+    # many entries, the two that cross far from one another
+    many = [state(data=a, out=b + 1024 * k) for k in range(700)]
+    many[650] = state(data=a, out=b + 1024 * 7 + 143)
+    assert INVALID == run(*many)
+    # no memory is like that
+    assert INVALID == run(state(data=a, out=(1 << 64) - 100)) == run(state(data=a, out=b, outer=2, stride=(1 << 62, 24, 0))) == run(state(data=64, out=b, stride=(0, -24, 0), out_stride=(0, 24, 0)))
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are not refused would be launched, at addresses that are not there")
+def test_reorder_refuses_what_crosses_and_nothing_else(lib):
+    """Against a list of all bytes: strides that lie within one another and others, rows that are one and the same, rows backwards, entries in place and not."""
+    rng = np.random.default_rng(3)
+    three, base = ctypes.c_int64 * 3, 1 << 20
+
+    def touched(at, counts, strides, size):
+        where = at + sum(np.arange(n).reshape([-1 if k == d else 1 for k in range(4)]) * s for d, (n, s) in enumerate(zip((*counts, size), (*strides, 1))))
+        return np.unique(where.ravel())
+
+    refused = 0
+    for _ in range(6000):
+        N, B, top = int(rng.integers(1, 3)), int(rng.integers(1, 4)), int(rng.integers(1, 4))
+        entries, parts, fine = [], [], True
+        for _ in range(int(rng.integers(1, 4))):
+            outer, inner, size = (int(v) for v in rng.integers(1, 4, 3))
+            counts = (outer, N * top, inner)
+            out_stride, extent = [0, 0, 0], size
+            for d in rng.permutation(3):
+                out_stride[d] = int(extent + rng.integers(0, 12))
+                extent += out_stride[d] * (counts[d] - 1)
+            out = base + int(rng.integers(0, 400))
+            place = bool(rng.random() < 0.4) and top == B
+            stride = out_stride if place else list(out_stride if rng.random() < 0.5 else (int(v) for v in rng.integers(-9, 40, 3)))
+            data = out if place else base + int(rng.integers(0, 400))
+            if data == out and not place:
+                fine = False
+            entries.append(net.KanStateRef(data, out, outer, inner, size, three(*stride), three(*out_stride)))
+            parts.append((True, touched(out, counts, out_stride, size)))
+            if not place:
+                parts.append((False, touched(data, (outer, N * B, inner), stride, size)))
+        if not fine:
+            continue
+        cross = any((p[0] or q[0]) and len(np.intersect1d(p[1], q[1])) for i, p in enumerate(parts) for q in parts[:i])
+        refused += cross
+        rc = lib.kan_beam_reorder(N, B, top, A, len(entries), (net.KanStateRef * len(entries))(*entries), None)
+        assert rc == (INVALID if cross else binding.KAN_ERR_HIP), (N, B, top, [(e.data - base, e.out - base, e.outer, e.inner, e.bytes, list(e.stride), list(e.out_stride)) for e in entries])
+    assert 1000 < refused < 5000
+
+
 def test_front_ends_refuse_host_tensors_and_wrong_shapes():
     from paper_2408_11200_amd import autograd
     z, ids, v, s = torch.zeros((6, 9)), torch.zeros((6, 2), dtype=torch.int64), torch.zeros((6, 2)), torch.zeros((2, 3))
