@@ -87,7 +87,8 @@ class TokenNet:
             answers[:, at] = tokens.view(-1)
             window = torch.cat([window[:, 1:], tokens.view(-1, 1)], 1)
             ended = None if ended is None else now
-        return answers.view(N, beams, length), scores
+        # a place without an answer took the beginning of its row from the first beam
+        return answers.view(N, beams, length).masked_fill(torch.isneginf(scores)[..., None], -1), scores
 
 
 def train(net, ids, target, steps, batch=4096, lr=3e-3, max_norm=1.0, seed=0, log_every=0):

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import net as plain
-from paper_2408_11200_amd import autograd, net
+from paper_2408_11200_amd import autograd, net, tokens, workloads
 
 pytestmark = pytest.mark.gpu
 
@@ -179,3 +179,18 @@ def test_states_that_cross_are_refused_and_left():
                 reorder(p, data, B, out=out)
         assert torch.equal(t, before)
         reorder(p, [t[:, :5]], B, out=[t[:, 5:].new_empty((6, 5, 4))])
+
+
+# ---- the network that is taught and asked ---------------------------------------------------
+
+@pytest.mark.parametrize("vocab,length,beams,end_id", [(3, 2, 16, -1), (2, 3, 20, 1), (5, 1, 64, -1)])
+def test_places_without_an_answer_have_no_tokens(vocab, length, beams, end_id):
+    """More beams than there are answers: the places behind them are -1 throughout, not the beginning of another answer."""
+    model = tokens.TokenNet(vocab=vocab, embed=8, blocks=1, seed=1)
+    ids = torch.randint(0, vocab, (6, 2), device="cuda")
+    answers, scores = model.search(ids, length, beams, end_id)
+    none = torch.isneginf(scores)
+    count = vocab ** length if end_id < 0 else length + 1         # of two tokens, one of which ends an answer
+    assert bool((none.sum(1) == beams - count).all()) and not none[:, :count].any()
+    assert bool((answers[none] == -1).all()) and bool((answers[~none] >= 0).all())
+    assert all(len({tuple(a) for a in answers[n, :count].tolist()}) == count for n in range(6))
