@@ -65,7 +65,9 @@ class TokenNet:
     def distill_loss(self, ids, teacher_ids, values, temperature=1.0, teacher="logp"):
         """Mean divergence from what a teacher says of the rows (as autograd.token_distill takes it), rows without a teacher left out."""
         loss = autograd.token_distill(self.logits(ids), teacher_ids, values, temperature, teacher)
-        return loss.sum() / ((teacher_ids >= 0) & (teacher_ids < self.vocab)).any(-1).sum().clamp(min=1)
+        # a teacher has a token whose probability is above 0: below e^-745 nothing is left in 64 bits, and a list of logits gives some to its largest one
+        nothing = torch.isneginf(values) if teacher == "logits" else values < -745.0
+        return loss.sum() / ((teacher_ids >= 0) & (teacher_ids < self.vocab) & ~nothing).any(-1).sum().clamp(min=1)
 
     @torch.no_grad()
     def search(self, ids, length, beams=4, end_id=-1, length_power=0.0, temperature=1.0):

@@ -194,3 +194,30 @@ def test_places_without_an_answer_have_no_tokens(vocab, length, beams, end_id):
     assert bool((none.sum(1) == beams - count).all()) and not none[:, :count].any()
     assert bool((answers[none] == -1).all()) and bool((answers[~none] >= 0).all())
     assert all(len({tuple(a) for a in answers[n, :count].tolist()}) == count for n in range(6))
+
+
+@pytest.mark.parametrize("teacher", ["logp", "logits"])
+def test_the_mean_divergence_leaves_rows_out_whose_lists_have_no_probability(teacher):
+    """Rows without a teacher: no token of the vocabulary in the list, or none whose probability is above 0 in 64 bits (the most likely tokens of a row that is masked throughout have -infinity)."""
+    student = tokens.TokenNet(20, embed=8, blocks=1, seed=2)
+    ids = torch.from_numpy(workloads.token_task(20, n=64)[0]).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    listed = torch.stack([torch.randperm(20, generator=gen, device="cuda")[:4] for _ in range(64)])
+    values = torch.log_softmax(torch.randn((64, 5), generator=gen, device="cuda"), 1)[:, :4].contiguous()
+    values[0::8] = -math.inf
+    listed[1::8] = torch.tensor([-1, 20, 1 << 40, -7], device="cuda")
+    values[2::8, 1:], listed[2::8, 0] = -math.inf, -1           # what has a probability is no token
+    values[3::8] = -800.0                                       # as log probabilities nothing, as logits a quarter each
+    values[4::8, 1:] = -math.inf
+    with torch.no_grad():
+        z = student.logits(ids)
+        each = plain.token_distill(host(z), listed.cpu().numpy(), host(values), 1.0, teacher)["loss"]
+    taught = np.isin(np.arange(64) % 8, [4, 5, 6, 7] + ([3] if teacher == "logits" else []))
+    assert (each[~taught] == 0).all() and (each[taught] > 0).all()
+    loss = student.distill_loss(ids, listed, values, teacher=teacher)
+    assert abs(float(loss.detach()) - each[taught].mean()) < 1e-5 * each[taught].mean()
+    values[5, 0] = math.nan                                     # a NaN is not nothing
+    assert math.isnan(float(student.distill_loss(ids, listed, values, teacher=teacher).detach()))
+    none = student.distill_loss(ids[:3], listed[:3], values[:3], teacher=teacher)
+    none.backward()
+    assert float(none.detach()) == 0 and all(not t.grad.any() for t in student.tensors())
