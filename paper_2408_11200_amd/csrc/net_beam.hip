@@ -320,9 +320,7 @@ hipError_t launch(BeamCall &a, int64_t N, hipStream_t st)
     const unsigned grid = a.rows * (unsigned)a.parts;
     {
         prof::Timed timed("beam_rows", st);
-        // logits that the caches do not hold are read past them: both launches, us, with and without: 256 x 8 x 50001 fp32 (410 MB) 83 and 90, 256 x 16 x 131072 bf16 184 and 209,
-        // 128 x 8 x 131072 (268 MB) 56 and 60 (58 and 54 where one call follows another on the same logits)
-        const bool past = (double)a.rows * (double)a.V * sizeof(T) >= 256e6;
+        const bool past = (double)a.rows * (double)a.V * sizeof(T) >= kLastCache;
         if (a.V <= 4096) beam_rows_kernel<T, 64, false><<<grid, 64, 0, st>>>(a);
         else if (past) beam_rows_kernel<T, 256, true><<<grid, 256, 0, st>>>(a);
         else beam_rows_kernel<T, 256, false><<<grid, 256, 0, st>>>(a);

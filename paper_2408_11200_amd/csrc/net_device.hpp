@@ -18,6 +18,17 @@ inline bool known_type(int type) { return type == KAN_F32 || type == KAN_BF16; }
 inline bool misplaced(const void *p, int type) { return ((uintptr_t)p % size_of(type)) != 0; }
 inline bool misplaced8(const void *p) { return ((uintptr_t)p % 8) != 0; }
 inline int status_of(hipError_t e) { return e == hipSuccess ? KAN_OK : KAN_ERR_HIP; }
+
+// Bytes of the last cache.  Logits or states of as many, read once a call, do not stay there for the next one, and are read past it by the three kinds of call below.  us, past it and through it, on
+// data that were written right before (and on data that it had not); bf16, selection of 8 beams a search, distillation forward with backward, reordering into other buffers and in place:
+//   160 MB   selection 55, 53 (54, 54)       distillation  88,  84 ( 94,  90)
+//   256 MB             65, 67 (64, 65)                    138, 133 (132, 128)
+//   268 MB             67, 70 (65, 67)                    143, 150 (138, 139)
+//   352 MB             92, 104 (84, 89)                   186, 213 (181, 190)
+//   640 MB            131, 163 (127, 134)                 321, 362 (319, 336)
+//   384 MB   reordering 131, 177 (132, 139), in place 121, 139 (123, 107)       512 MB   188, 235 (176, 183), in place 172, 187 (165, 149)
+constexpr double kLastCache = 268435456.0;
+
 template <class I>
 constexpr I div_up(I a, I b) { return (a + b - 1) / b; }
 

@@ -599,9 +599,8 @@ DistillCall rows_from(DistillCall a, int64_t first, int64_t most, size_t size)
     return a;
 }
 
-// Whether the logits do not stay in the caches from one pass to the next: then they are read past them (8192 x 131072 bf16 backward 708 us, 754 through them; 2000 x 33000,
-// 132 MB, 57 and 52).
-bool passes_by(const DistillCall &a, size_t size) { return (double)a.R * (double)a.V * (double)size >= 512e6; }
+// whether the logits do not stay in the caches from one pass to the next (8192 x 131072 bf16 backward 708 us past them, 754 through them; 2000 x 33000, 132 MB, 57 and 52)
+bool passes_by(const DistillCall &a, size_t size) { return (double)a.R * (double)a.V * (double)size >= kLastCache; }
 
 template <class T, int E>
 void launch_back(const DistillCall &a, int threads, bool stream, unsigned grid, hipStream_t st)

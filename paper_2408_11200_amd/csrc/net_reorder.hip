@@ -340,10 +340,9 @@ extern "C" int kan_beam_reorder(int64_t N, int32_t B, int32_t top, const int64_t
     if (N == 0 || n == 0) return KAN_OK;
     if (!parents || misplaced8(parents)) return KAN_ERR_INVALID_ARG;
     const int piece = piece_of(top);
-    // 4 x 8 rows of 16 states, 2.1 GB to move: 372 us with streaming loads, 378 without; 24 x 6 rows of 8, 312 MB: 78 and 68
     double bytes = 0.0;
     for (int i = 0; i < n; ++i) bytes += (double)list[i].outer * (double)list[i].inner * (double)list[i].bytes * (double)N * B;
-    const bool past = bytes >= 1e9;
+    const bool past = bytes >= kLastCache;
     ReorderCall a = {};
     a.parents = parents;
     a.B = B;
