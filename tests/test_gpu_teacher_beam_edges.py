@@ -7,6 +7,8 @@ import torch
 
 from oracle import net as plain
 from paper_2408_11200_amd import autograd, net, tokens, workloads
+from test_gpu_beam import case as select_case, check as select_check
+from test_gpu_distill import case as distill_case, check as distill_check
 
 pytestmark = pytest.mark.gpu
 
@@ -87,6 +89,44 @@ def test_one_token_stands_out_behind_the_first_pieces(dtype, V, T):
         assert err.max() <= 1, float(err.max())
 
 
+@pytest.mark.parametrize("R,V,K,dtype,T", [(4200, 33001, 20, BF16, 1.0), (4500, 16001, 12, F32, 0.75), (1100, 64007, 20, F32, 1.0), (1100, 64007, 70, F32, 1.0), (2100, 65003, 8, BF16, 1.0)])
+def test_logits_that_the_caches_do_not_hold(R, V, K, dtype, T):
+    """Read past the caches, by four and by eight waves a row: against the formulas, and the bits of fewer rows that are read through them."""
+    few = 520
+    logits, ids, values, g = distill_case(few, V, K, R, dtype=dtype, T=T)
+    many = lambda t: t.repeat(-(-R // few), *[1] * (t.dim() - 1))[:R].contiguous()
+    big, bi, bv, bg = many(logits), many(ids), many(values), many(g)
+    assert big.numel() * big.element_size() >= 1 << 28 and few * V * big.element_size() < 1 << 28
+    o = net.kan_token_distill_forward(big, bi, bv, T)
+    gz = net.kan_token_distill_backward(big, bi, o, bg, T)
+    f = plain.token_distill(host(logits[:6]), ids[:6].cpu().numpy(), host(values[:6]), T)
+    distill_check(f, T, V, loss=o["loss"][:6], glogits=gz[:6], g=g[:6])
+    loss, gs = net.kan_token_distill_step(big, bi, bv, bg, T)
+    assert torch.equal(loss, o["loss"]) and torch.equal(gs, gz)
+    small = net.kan_token_distill_forward(logits, ids, values, T)
+    back = net.kan_token_distill_backward(logits, ids, small, g, T)
+    assert torch.equal(o["loss"], many(small["loss"])) and torch.equal(gz[:few], back) and torch.equal(gz[-(R % few):], back[:R % few])
+
+
+@pytest.mark.parametrize("R,V,K,dtype", [(5, 300, 70, F32), (700, 5000, 65, BF16), (9, 20000, 256, F32), (3, 140000, 100, BF16), (400, 140000, 128, F32), (2, 70001, 200, F32)])
+@pytest.mark.parametrize("teacher", ["logp", "logits"])
+def test_tokens_twice_in_long_lists(R, V, K, dtype, teacher):
+    """Lists of more than 64 tokens, some of them two and three times and among other lanes' and entries' tokens: one wave a row, more, and rows that are cut."""
+    logits, ids, values, g = distill_case(R, V, K, V, dtype=dtype, teacher=teacher, short=False)
+    ids[:, K - 1] = ids[:, 0]                           # another entry of the same lane or of another one
+    ids[::2, 64] = ids[::2, 0]
+    ids[1::2, 64] = ids[1::2, 63]
+    ids[:, K // 2] = ids[:, 3]
+    rows = np.unique(np.concatenate([np.arange(min(R, 4)), [R - 1]]))
+    f = plain.token_distill(host(logits)[rows] if R < 100 else host(logits[rows.tolist()]), ids.cpu().numpy()[rows], host(values)[rows], 1.0, teacher)
+    o = net.kan_token_distill_forward(logits, ids, values, 1.0, teacher)
+    distill_check(f, 1.0, V, loss=o["loss"][rows.tolist()])
+    gz = net.kan_token_distill_backward(logits, ids, o, g)
+    distill_check(f, 1.0, V, glogits=gz[rows.tolist()], g=g[rows.tolist()])
+    loss, gs = net.kan_token_distill_step(logits, ids, values, g, 1.0, teacher)
+    assert torch.equal(loss, o["loss"]) and torch.equal(gs, gz)
+
+
 # ---- beam selection -------------------------------------------------------------------------
 
 @pytest.mark.parametrize("B,top", [(8, 8), (64, 64), (64, 5), (33, 40)])
@@ -135,6 +175,19 @@ def test_a_beams_tokens_come_in_the_order_of_their_logits(score, T, N, V, top):
         assert torch.equal(both["tokens"], o["tokens"]) and not both["parents"].any()
 
 
+@pytest.mark.parametrize("N,B,V,top,dtype", [(140, 8, 62501, 16, F32), (300, 16, 16001, 64, F32), (130, 8, 131075, 8, BF16)])
+def test_selection_from_logits_that_the_caches_do_not_hold(N, B, V, top, dtype):
+    few = 40
+    logits, scores, _, _ = select_case(few, B, V, V, dtype=dtype)
+    assert N * B * V * logits.element_size() >= 1 << 28 > few * B * V * logits.element_size()
+    big = logits.repeat(-(-N // few), 1)[:N * B].contiguous()
+    s = torch.from_numpy(np.tile(scores, (-(-N // few), 1))[:N].copy()).cuda()
+    o = net.kan_beam_select(big, s, top)
+    select_check(o, plain.beam_select(host(logits[:2 * B]), scores[:2], top), V, rows=[0, 1])
+    small = net.kan_beam_select(logits, s[:few], top)
+    assert all(torch.equal(o[n][:few], small[n]) and torch.equal(o[n][few:2 * few], small[n]) for n in o)
+
+
 # ---- reordering -----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("N,B", [(3, 4), (1, 20), (2, 64)])
@@ -164,6 +217,25 @@ def test_states_side_by_side_in_one_buffer(N, B):
         before = tall.clone()
         reorder(parents, [tall[::2], tall[1::2]], B, dim=1)
         assert torch.equal(tall, before[:, rows])
+
+
+@pytest.mark.parametrize("N,B,dtype", [(3, 5, BF16), (2, 12, torch.uint8), (2, 20, F32), (1, 40, BF16), (1, 64, torch.uint8)])
+def test_states_that_the_caches_do_not_hold(N, B, dtype):
+    """Read past the caches, by every number of rows a thread has a piece of; in place and into other buffers."""
+    rng = np.random.default_rng(B)
+    p = rng.integers(0, B, (N, B))
+    parents = torch.from_numpy(p).cuda()
+    rows = torch.from_numpy((p + B * np.arange(N)[:, None]).ravel()).cuda()
+    size = torch.empty(0, dtype=dtype).element_size()
+    width = -(-(1 << 28) // (N * B * size)) | 1         # rows that start anywhere
+    state = torch.randint(0, 100, (N * B, width), device="cuda", dtype=torch.uint8).to(dtype)
+    assert state.numel() * size >= 1 << 28
+    want = state[rows]
+    out = torch.empty_like(state)
+    autograd.beam_reorder(parents, [state], B, out=[out])
+    assert torch.equal(out, want)
+    net.kan_beam_reorder(parents, [state], B)
+    assert torch.equal(state, want)
 
 
 def test_states_that_cross_are_refused_and_left():
