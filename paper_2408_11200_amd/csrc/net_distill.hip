@@ -566,11 +566,12 @@ __global__ __launch_bounds__(256) void distill_short_back_kernel(DistillCall a)
 //   4096 x 1000 bf16, K = 20 8.9 9.5,  12.8 13.0,  6.8 6.3        65536 x 1000     50 93,     88 122,    59 58
 //   8192 x 2000 bf16, K = 20 15.7 19.5, 26.5 29.5, 14.5 15.4      65536 x 2000     72 120,   174 177,   139 121
 //   1024 x 1000 fp32, K = 8  10.2 7.1, 15.3 9.6,   7.6 4.9        65536 x 1000 fp32, K = 64  88 114, 217 168, 160 202
-// The forward pass and the step go the same way, whose sums have to be the same bits.
+// The forward pass and the step go the same way, whose sums have to be the same bits: in the last line the step's 168 us decide, and the forward pass takes 114 where it could take 88.  The backward
+// pass needs more rows (K = 20, rows twice and four times their bytes): 250 fp32 3.9 3.8 and 4.2 4.6, 501 5.9 5.6 and 7.8 8.4; bf16 500 4.3 4.0 and 4.6 5.0, 1002 6.6 6.1 and 8.4 9.0.
 bool is_short(const DistillCall &a, size_t size, bool back)
 {
     const double bytes = (double)a.V * (double)size;
-    return a.K <= 64 && (bytes <= 512.0 || ((double)a.R >= 2.0 * bytes && (bytes <= 2048.0 || (bytes <= 4096.0 && a.K <= 32 && !back))));
+    return a.K <= 64 && (bytes <= 512.0 || ((double)a.R >= (back ? 4.0 : 2.0) * bytes && (bytes <= 2048.0 || (bytes <= 4096.0 && a.K <= 32 && !back))));
 }
 
 // Few long rows are shared among workgroups, two a CU, and joined by a launch more.  Whole and cut, us, twenty tokens: 1 x 65536 bf16 8.2 and 7.6, 1 x 131072 11.3 and

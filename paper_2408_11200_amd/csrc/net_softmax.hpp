@@ -171,7 +171,7 @@ __device__ __forceinline__ double log_of(double x)
     return __builtin_fma((double)e, 0.69314718055994531, half + half);
 }
 
-// e^x in 64 bits: x = n log 2 + r, |r| <= 0.3466, whose series is below 2^-53 behind thirteen terms; below e^-745 zero.  An infinity above gives a NaN.
+// e^x in 64 bits: x = n log 2 + r, |r| <= 0.3466, whose series is below 2^-51 of it behind thirteen terms; below e^-745 zero.  An infinity above gives a NaN.
 __device__ __forceinline__ double exp_of(double x)
 {
     const double n = __builtin_rint(x * 1.4426950408889634);

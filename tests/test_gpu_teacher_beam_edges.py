@@ -7,6 +7,7 @@ import torch
 
 from oracle import net as plain
 from paper_2408_11200_amd import autograd, net, tokens, workloads
+import test_gpu_distill
 from test_gpu_beam import case as select_case, check as select_check
 from test_gpu_distill import case as distill_case, check as distill_check
 
@@ -125,6 +126,13 @@ def test_tokens_twice_in_long_lists(R, V, K, dtype, teacher):
     distill_check(f, 1.0, V, glogits=gz[rows.tolist()], g=g[rows.tolist()])
     loss, gs = net.kan_token_distill_step(logits, ids, values, g, 1.0, teacher)
     assert torch.equal(loss, o["loss"]) and torch.equal(gs, gz)
+
+
+@pytest.mark.parametrize("R,V,K,options", [(4200, 257, 16, dict(dtype=F32, T=1.0)), (4111, 257, 20, dict(dtype=F32, T=1.0)), (8200, 512, 64, dict(dtype=F32, teacher="logits", T=0.75)), (8191, 512, 8, dict(dtype=F32, T=1.0)),
+                                           (8011, 1001, 20, dict(dtype=BF16, pad=5, T=1.0)), (8005, 1001, 33, dict(dtype=BF16, T=2.0)), (16390, 501, 20, dict(dtype=F32, pad=1, T=1.0))])
+def test_short_rows_on_both_sides_of_the_backward_line(R, V, K, options):
+    """As many rows as four times a row's bytes, and fewer."""
+    test_gpu_distill.test_short_rows(R, V, K, dict(dict(teacher="logp"), **options))
 
 
 # ---- beam selection -------------------------------------------------------------------------
