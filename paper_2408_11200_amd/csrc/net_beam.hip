@@ -11,7 +11,7 @@
 // (Logits picked from each piece as it passed took the waves through some hundred instructions a piece more where no tokens stand out: 64 x 8 x 131072 bf16 48 us.)
 //
 // Measured: 128 x 8 x 131072 bf16 with sixteen 50-53 us for the rows (268 MB, 5.1-5.3 TB/s; half of the workgroups wait 5 us for their first logits, as all begin together, and
-// each has 4 left after its last ones) and 4.8 for the second launch; 4 x 32 x 131072 with 64 17 and 8; 1 x 4 x 32768 with four 6.1 and 3.8, one latency after another.
+// each has 4 left after its last ones) and 5.3 for the second launch; 4 x 32 x 131072 with 64 16.4 and 10.7; 1 x 4 x 32768 with four 6.2 and 4.4, one latency after another.
 #include "net_softmax.hpp"
 
 namespace kannet {
@@ -194,7 +194,8 @@ constexpr uint32_t kLists = 1024;       // of a search: parts of its rows, or ro
 
 // A workgroup for each search: 256 threads where each has one of the lists' entries at most, 1024 otherwise.  What counts is latency: all there is to read
 // is on its way before any of it is looked at, and instead of counting for each candidate how many are above it (128 of them: 7 us) waves sort theirs in
-// registers and join them.
+// registers and join them.  Ranks cut to 48 bits beside the place, half the registers a candidate, took 0.5 to 0.7 us less (2.7 of 4 x 32 x 131072 with 64), and were equal where they are not;
+// compared as 64-bit floats they take as long.
 template <int NT>
 __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
 {
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(NT) void beam_join_kernel(BeamCall a)
 }
 
 // How rows are cut: few rows are shared among workgroups, two a CU, of a round of pieces (16 KB) at least.  Both launches, us, whole rows, two workgroups
-// a CU and four: 1 x 4 x 16384 bf16 11.1, 9.6, 9.5; 32 x 4 x 16384 12.3, 10.8, 10.8; 24 x 4 x 50001 fp32 with twelve -, 15.0, 18.4; 16 x 8 x 131072 bf16 with sixteen -, 19.3, 21.3; half
+// a CU and four (all with a second launch of 0.6 us less than now): 1 x 4 x 16384 bf16 11.1, 9.6, 9.5; 32 x 4 x 16384 12.3, 10.8, 10.8; 24 x 4 x 50001 fp32 with twelve -, 15.0, 18.4; 16 x 8 x 131072 bf16 with sixteen -, 19.3, 21.3; half
 // a round: 1 x 4 x 32768 bf16 10.3 for 9.7, 1 x 8 x 131072 16.5 for 14.7.
 int parts_of(int64_t rows, int64_t V, size_t size)
 {
