@@ -177,6 +177,7 @@ bool region_of(const void *at, const int64_t (&count)[3], const int64_t (&stride
         r.count[d] = n;
         r.stride[d] = n > 1 ? stride[d] : 0;
         const __int128 reach = (__int128)r.stride[d] * (n - 1);
+        if (reach <= -((__int128)1 << 62)) return false;
         if (reach < 0) {
             first += reach;
             r.stride[d] = -r.stride[d];

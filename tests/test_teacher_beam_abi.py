@@ -116,6 +116,10 @@ def test_reorder_refuses_outputs_that_cross(lib):
     many = [state(data=a, out=b + 1024 * k) for k in range(700)]
     many[650] = state(data=a, out=b + 1024 * 7 + 143)
     assert INVALID == run(*many)
+    # strides of which neither lies within the other: nothing crosses, but it takes too long to tell
+    uneven = state(data=a + 8, out=1 << 40, outer=100000, size=8, stride=(16 * 999, 1 << 34, 0), out_stride=(8, 1 << 34, 0))
+    assert UNSUPPORTED == run(uneven, state(data=1 << 41, out=a, outer=100000, size=8, stride=(16 * 1001, 1 << 35, 0)), N=1, B=1, top=1)
+    assert INVALID == run(state(data=a, out=b, stride=(0, -(1 << 63), 0), out_stride=(0, 24, 0)))
     # no memory is like that
     assert INVALID == run(state(data=a, out=(1 << 64) - 100)) == run(state(data=a, out=b, outer=2, stride=(1 << 62, 24, 0))) == run(state(data=64, out=b, stride=(0, -24, 0), out_stride=(0, 24, 0)))
 
